@@ -32,6 +32,10 @@ Contents
                    plain definitions, plus their single-pass (rolling) and
                    split-k forms.
 
+``serve``          rotary positions, the paged 4-bit cache and decode over it
+                   (include/rope.h, include/kv4.h): plain definitions, pinned
+                   by ``tests/test_serve_oracle.py``.
+
 Parity status: every function here is pinned by ``tests/test_oracle_pins.py``
 and ``tests/test_algorithms.py`` (invariants, closed forms, brute force and
 the CPU float64 ``scaled_dot_product_attention`` of PyTorch as a library
@@ -39,4 +43,4 @@ special case).  No function is "parity unpinned".
 """
 
 from .attention import attention, scores, softmax_probs  # noqa: F401
-from . import norms, rolling, splitk  # noqa: F401
+from . import norms, rolling, serve, splitk  # noqa: F401

@@ -1,6 +1,6 @@
 """Fused attention for AMD Instinct MI355X (gfx950) — Python binding of libattn.so.
 
-A thin layer over the C ABI declared in ``include/attn.h``: the functions
+A thin layer over the C ABI declared in ``include/*.h``: the functions
 below have the same names as the C entry points and only marshal arguments
 (device pointers, sizes, the current HIP stream).  Every step of the
 computation runs in the HIP kernels of ``libattn.so``; PyTorch only provides
@@ -24,6 +24,8 @@ __all__ = [
     "attn_decode_num_splits", "attn_decode_noalloc", "peaks_hbm_read", "peaks_mfma", "peaks_mfma_waves",
     "peaks_mfma_operand_bytes", "norm_chunks", "norm_kernels", "norm_workspace_bytes", "norm_l2", "rmsnorm_rowmax", "attn_fwd_kernels", "attn_fwd_call_kernels",
     "attn_decode_kernels",
+    "rope_frequencies", "rope_fwd", "rope_bwd", "kv4_page_bytes", "kv_slots", "kv4_append", "kv4_load",
+    "attn_decode_kv4", "attn_decode_kv4_workspace_bytes",
     "attn_status_string", "attn_last_hip_error", "library_path", "load_library", "AttnError",
     "ATTN_OK", "ATTN_ERR_NULL", "ATTN_ERR_SHAPE", "ATTN_ERR_UNSUPPORTED", "ATTN_ERR_WORKSPACE",
     "ATTN_ERR_HIP",
@@ -115,6 +117,24 @@ def load_library():
     lib.norm_l2.restype = ci
     lib.rmsnorm_rowmax.argtypes = [vp, vp, vp, ci, ci, cf, ci, ci, vp, cs, vp]
     lib.rmsnorm_rowmax.restype = ci
+    cd, cl = ctypes.c_double, ctypes.c_longlong
+    lib.rope_frequencies.argtypes = [ci, cd, ci, cd, cd, cd, cd, vp]
+    lib.rope_frequencies.restype = ci
+    for f in (lib.rope_fwd, lib.rope_bwd):
+        f.argtypes = [vp, vp, vp, ci, vp, vp, vp, ci, ci, ci, ci, vp, ci, cl, vp, ci, ci, cf, ci, vp]
+        f.restype = ci
+    lib.kv4_page_bytes.argtypes = [ci, ci]
+    lib.kv4_page_bytes.restype = cs
+    lib.kv_slots.argtypes = [vp, vp, vp, vp, ci, ci, ci, ci, ci, vp, vp, vp, vp, vp]
+    lib.kv_slots.restype = ci
+    lib.kv4_append.argtypes = [vp, vp, vp, vp, vp, vp, ci, ci, ci, ci, ci, ci, ci, vp]
+    lib.kv4_append.restype = ci
+    lib.kv4_load.argtypes = [vp, vp, vp, vp, vp, vp, ci, ci, ci, ci, ci, ci, ci, ci, vp]
+    lib.kv4_load.restype = ci
+    lib.attn_decode_kv4_workspace_bytes.argtypes = [ci, ci, ci, ci]
+    lib.attn_decode_kv4_workspace_bytes.restype = cs
+    lib.attn_decode_kv4.argtypes = [vp, vp, vp, vp, vp, ci, ci, ci, ci, ci, ci, ci, cf, vp, cf, ci, vp, cs, ci, vp]
+    lib.attn_decode_kv4.restype = ci
     lib.attn_status_string.argtypes = [ci]
     lib.attn_status_string.restype = ctypes.c_char_p
     lib.attn_last_hip_error.argtypes = []
@@ -132,6 +152,7 @@ class _NotBuilt:
         return None
 
     attn_fwd = attn_decode = attn_decode_noalloc = norm_l2 = rmsnorm_rowmax = _none
+    rope = kv_slots = kv4_append = kv4_load = attn_decode_kv4 = _none
 
 
 def _load_binding():
@@ -493,6 +514,312 @@ def rmsnorm_rowmax(x, y=None, rowmax=None, *, eps=1e-6, chunks=0, workspace=None
                                          int(chunks), _ptr(workspace), workspace.numel() * workspace.element_size(),
                                          _stream(stream)))
     return y, rowmax
+
+
+# Rotary positions, and the paged 4-bit cache with the decode that reads it.
+
+_ROPE_SCALING = {None: 0, "linear": 1, "base": 2, "parts": 3}
+
+
+def rope_frequencies(rotary_dim, base=10000.0, *, scaling=None, factor=1.0, original_length=0, slow=1.0, fast=32.0,
+                     device=None):
+    """Frequencies (radians per position, float64 [rotary_dim / 2]) for rope_fwd.
+
+    ``scaling`` adapts them to contexts longer than the trained one by
+    ``factor``: None, "linear" (positions interpolated), "base" (a larger
+    base) or "parts" (pairs that make fewer than ``slow`` turns over
+    ``original_length`` tokens are interpolated, those over ``fast`` are not,
+    with a ramp between).
+    """
+    _require(scaling in _ROPE_SCALING, "scaling must be None, 'linear', 'base' or 'parts'")
+    n = int(rotary_dim)
+    f = torch.empty(max(n // 2, 1), dtype=torch.float64)
+    _check(load_library().rope_frequencies(n, float(base), _ROPE_SCALING[scaling], float(factor),
+                                           float(original_length), float(slow), float(fast), _ptr(f)))
+    return f if device is None else f.to(device)
+
+
+def _on_device(t, stream):
+    """Stream and device of a call on t: t's device becomes the current one for
+    the call, and a stream that is given has to be on it."""
+    if stream is None:
+        stream = torch.cuda.current_stream(t.device)
+    _require(getattr(stream, "device", t.device) == t.device, "stream must be on the tensors' device")
+    return stream
+
+
+def _same_device(first, **tensors):
+    _require(first.is_cuda, "tensors must be on the GPU")
+    for name, t in tensors.items():
+        _require(t.device == first.device, f"{name} must be on the same GPU as the other tensors")
+
+
+def _ints(name, t, dtype, shape):
+    _require(t.dtype == dtype and tuple(t.shape) == tuple(shape) and t.is_contiguous(),
+             f"{name} must be a contiguous {str(dtype)[6:]} tensor of shape {list(shape)}")
+
+
+def _strides(t):
+    """Strides of batches, heads and tokens; 0 where there is one alone."""
+    return (ctypes.c_longlong * 3)(*(s if n > 1 else 0 for s, n in zip(t.stride()[:3], t.shape)))
+
+
+def _rows(name, t, shape=None):
+    _require(t.dim() == 4, f"{name} must be 4-D [B, H, L, D]")
+    _require(t.shape[3] == 1 or t.stride(3) == 1, f"{name} must have contiguous rows (the last dim)")
+    _require(shape is None or tuple(t.shape) == tuple(shape), f"{name} must have shape {list(shape or [])}")
+
+
+def _allocate(shape, like, stream, dtype=None):
+    """An output, in the pool of the stream that it is written on."""
+    if isinstance(stream, torch.cuda.Stream):
+        with torch.cuda.stream(stream):
+            return torch.empty(shape, dtype=dtype or like.dtype, device=like.device)
+    return torch.empty(shape, dtype=dtype or like.dtype, device=like.device)
+
+
+def _overlaps(a, b):
+    """Whether two contiguous tensors share memory."""
+    return (a.data_ptr() < b.data_ptr() + b.numel() * b.element_size()
+            and b.data_ptr() < a.data_ptr() + a.numel() * a.element_size())
+
+
+def _rope(bwd, q, k, positions, freqs, q_out, k_out, interleaved, magnitude, stream):
+    r = (_BINDING or _load_binding()).rope(q, k, positions, freqs, q_out, k_out, interleaved, magnitude, bwd, stream)
+    if r is not None:
+        return _result(r)
+    _rows("q", q)
+    B, Hq, L, D = q.shape
+    _require(q.dtype in _NORM_CODE, "dtype must be float16, bfloat16 or float32")
+    _same_device(q, positions=positions, freqs=freqs)
+    if k is None:
+        _require(k_out is None, "k_out needs k")
+    else:
+        _rows("k", k)
+        _same_device(q, k=k)
+        _require(k.dtype == q.dtype and (k.shape[0], *k.shape[2:]) == (B, L, D),
+                 "k must have q's dtype, batch, length and head dim")
+    _require(freqs.dtype == torch.float64 and freqs.dim() == 1 and freqs.is_contiguous(),
+             "freqs must be a contiguous float64 tensor [rotary_dim / 2]")
+    _require(positions.dtype in (torch.int32, torch.int64) and tuple(positions.shape) in ((B, L), (L,))
+             and positions.is_contiguous(), "positions must be a contiguous int32 or int64 tensor [B, L] or [L]")
+    stream = _on_device(q, stream)
+    outs = []
+    for name, x, o in (("q", q, q_out), ("k", k, k_out)):
+        if o is None and x is not None:
+            o = _allocate(x.shape, x, stream)
+        elif o is not None:
+            _same_device(q, **{name + "_out": o})
+            _require(o.shape == x.shape and o.dtype == x.dtype and o.is_contiguous(),
+                     f"{name}_out must be a contiguous tensor shaped like {name}")
+            _require(o.data_ptr() != x.data_ptr() or x.is_contiguous(),
+                     f"{name}_out may be {name} itself only if that is contiguous")
+        outs.append(o)
+    lib = load_library()
+    fn = lib.rope_bwd if bwd else lib.rope_fwd
+    with torch.cuda.device(q.device):
+        _check(fn(_ptr(q), _strides(q), _ptr(outs[0]), Hq, _ptr(k), None if k is None else _strides(k), _ptr(outs[1]),
+                  0 if k is None else k.shape[1], B, L, D, _ptr(positions), positions.element_size() * 8,
+                  L if positions.dim() == 2 else 0, _ptr(freqs), 2 * freqs.numel(), int(bool(interleaved)),
+                  float(magnitude), _NORM_CODE[q.dtype], _stream(stream)))
+    return outs[0], outs[1]
+
+
+def rope_fwd(q, k, positions, freqs, q_out=None, k_out=None, *, interleaved=False, magnitude=1.0, stream=None):
+    """Rotate q [B, Hq, L, D] and k [B, Hkv, L, D] (or None) by their positions.
+
+    float16, bfloat16 or float32; strided views with contiguous rows are taken
+    as they are (a projection's [B, L, H, D] transposed).  ``positions``: int32 or
+    int64 [B, L] or [L]; ``freqs``: float64 [rotary_dim / 2] on the GPU
+    (rope_frequencies); the first rotary_dim dims are rotated in pairs
+    (i, i + rotary_dim / 2), or (2 i, 2 i + 1) if ``interleaved``, and the
+    rest copied.  ``magnitude`` scales the rotated dims.  Outputs are contiguous;
+    q_out may be q itself, and k_out k.  Returns (q_out, k_out).
+    """
+    return _rope(False, q, k, positions, freqs, q_out, k_out, interleaved, magnitude, stream)
+
+
+def rope_bwd(dq, dk, positions, freqs, q_out=None, k_out=None, *, interleaved=False, magnitude=1.0, stream=None):
+    """Gradients of rope_fwd's q and k from those of its outputs (the transposed
+    rotation), with the same arguments."""
+    return _rope(True, dq, dk, positions, freqs, q_out, k_out, interleaved, magnitude, stream)
+
+
+def kv4_page_bytes(page, D):
+    """Bytes of a page of `page` tokens of one head in the 4-bit cache (0 if not supported)."""
+    return load_library().kv4_page_bytes(page, D)
+
+
+def kv_slots(lens, counts, table, free_pages, page, L, *, slots=None, positions=None, new_lens=None, taken=None,
+             stream=None):
+    """Pages and slots of the new tokens of B requests, on the GPU.
+
+    ``lens`` and ``counts`` (int32 [B]): tokens in the cache, and new ones (at
+    most L of them are taken).  Pages that they need are taken off the front
+    of ``free_pages`` (int32 [F]) request by request and written into ``table``
+    (int32 [B, max_pages], in place).  Returns (slots [B, L] int64, -1 for no
+    token; positions [B, L] int32; new_lens [B] int32; taken [1] int32, the number
+    of pages taken); see kv4.h.
+    """
+    r = (_BINDING or _load_binding()).kv_slots(lens, counts, table, free_pages, page, L, slots, positions, new_lens,
+                                               taken, stream)
+    if r is not None:
+        return _result(r)
+    page, L = int(page), int(L)
+    _require(lens.dim() == 1 and table.dim() == 2 and free_pages.dim() == 1,
+             "lens must be [B], table [B, max_pages] and free_pages [F]")
+    B, M = lens.shape[0], table.shape[1]
+    _same_device(lens, counts=counts, table=table, free_pages=free_pages)
+    _ints("lens", lens, torch.int32, (B,))
+    _ints("counts", counts, torch.int32, (B,))
+    _ints("table", table, torch.int32, (B, M))
+    _ints("free_pages", free_pages, torch.int32, (free_pages.shape[0],))
+    _require(L >= 1, "L must be at least 1")
+    stream = _on_device(lens, stream)
+    outs = []
+    for name, t, dtype, shape in (("slots", slots, torch.int64, (B, L)), ("positions", positions, torch.int32, (B, L)),
+                                  ("new_lens", new_lens, torch.int32, (B,)), ("taken", taken, torch.int32, (1,))):
+        if t is None:
+            t = _allocate(shape, lens, stream, dtype)
+        else:
+            _same_device(lens, **{name: t})
+            _ints(name, t, dtype, shape)
+            _require(not any(_overlaps(t, x) for x in (lens, counts, table, free_pages)),
+                     f"{name} must not share memory with what is read")
+        outs.append(t)
+    with torch.cuda.device(lens.device):
+        _check(load_library().kv_slots(_ptr(lens), _ptr(counts), _ptr(table), _ptr(free_pages), free_pages.shape[0], B,
+                                       M, page, L, *(_ptr(t) for t in outs), _stream(stream)))
+    return tuple(outs)
+
+
+def _cache_page(cache, D):
+    """Tokens of a page of a cache [pages, Hkv, bytes] of head dim D."""
+    _require(cache.dtype == torch.uint8 and cache.dim() == 3 and cache.is_contiguous(),
+             "cache must be a contiguous uint8 tensor [pages, Hkv, kv4_page_bytes(page, D)]")
+    _require(D in (64, 128), "head dim must be 64 or 128")
+    page = cache.shape[2] * 16 // (17 * D)
+    _require(page > 0 and kv4_page_bytes(page, D) == cache.shape[2],
+             "the cache's rows must be kv4_page_bytes(page, D) of a power of two from 16 to 32768")
+    return page
+
+
+def kv4_append(k, v, cache, slots, *, stream=None):
+    """Round k and v [B, Hkv, L, D] (float16 or bfloat16, rows contiguous) to 4
+    bits and write them into ``cache`` (uint8 [pages, Hkv, kv4_page_bytes(page,
+    D)]) at ``slots`` (int64 [B, L], distinct; others than 0 .. pages * page - 1
+    are skipped).  Returns ``cache``."""
+    r = (_BINDING or _load_binding()).kv4_append(k, v, cache, slots, stream)
+    if r is not None:
+        return _result(r)
+    _rows("k", k)
+    _rows("v", v, k.shape)
+    B, H, L, D = k.shape
+    _require(k.dtype == v.dtype and k.dtype in _DTYPE_CODE, "k and v must both be float16 or bfloat16")
+    _same_device(k, v=v, cache=cache, slots=slots)
+    page = _cache_page(cache, D)
+    _require(cache.shape[1] == H, "cache and k must have the same number of heads")
+    _ints("slots", slots, torch.int64, (B, L))
+    stream = _on_device(k, stream)
+    with torch.cuda.device(k.device):
+        _check(load_library().kv4_append(_ptr(k), _strides(k), _ptr(v), _strides(v), _ptr(cache), _ptr(slots), B, H, L,
+                                         D, cache.shape[0], page, _DTYPE_CODE[k.dtype], _stream(stream)))
+    return cache
+
+
+def _paged(cache, table, lens):
+    _require(table.dim() == 2, "table must be [B, max_pages]")
+    _same_device(cache, table=table, lens=lens)
+    B, M = table.shape
+    _ints("table", table, torch.int32, (B, M))
+    _ints("lens", lens, torch.int32, (B,))
+    return B, M
+
+
+def kv4_load(cache, table, lens, L, D, dtype, k=None, v=None, *, starts=None, stream=None):
+    """k and v [B, Hkv, L, D] of tokens starts[b] .. starts[b] + L - 1 (default:
+    from token 0) of each sequence of a 4-bit cache, as held; zeros from
+    token lens[b] on.  ``table`` int32 [B, max_pages], ``lens`` and
+    ``starts`` int32 [B].  Returns (k, v), which attn_fwd takes."""
+    r = (_BINDING or _load_binding()).kv4_load(cache, table, lens, L, D, dtype, k, v, starts, stream)
+    if r is not None:
+        return _result(r)
+    L, D = int(L), int(D)
+    _require(dtype in _DTYPE_CODE, "dtype must be float16 or bfloat16")
+    page = _cache_page(cache, D)
+    B, M = _paged(cache, table, lens)
+    _require(L >= 1, "L must be at least 1")
+    if starts is not None:
+        _same_device(cache, starts=starts)
+        _ints("starts", starts, torch.int32, (B,))
+    stream = _on_device(cache, stream)
+    outs = []
+    for name, t in (("k", k), ("v", v)):
+        shape = (B, cache.shape[1], L, D)
+        if t is None:
+            t = _allocate(shape, cache, stream, dtype)
+        else:
+            _same_device(cache, **{name: t})
+            _require(tuple(t.shape) == shape and t.dtype == dtype and t.is_contiguous(),
+                     f"{name} must be a contiguous {str(dtype)[6:]} tensor of shape {list(shape)}")
+        outs.append(t)
+    with torch.cuda.device(cache.device):
+        _check(load_library().kv4_load(_ptr(cache), _ptr(table), _ptr(starts), _ptr(lens), _ptr(outs[0]),
+                                       _ptr(outs[1]), B, cache.shape[1], L, D, cache.shape[0], page, M,
+                                       _DTYPE_CODE[dtype], _stream(stream)))
+    return outs[0], outs[1]
+
+
+def attn_decode_kv4_workspace_bytes(B, Hq, Hkv, D):
+    return load_library().attn_decode_kv4_workspace_bytes(B, Hq, Hkv, D)
+
+
+def attn_decode_kv4(q, cache, table, lens, o=None, *, scale=None, alibi_slopes=None, softcap=None, window=None,
+                    workspace=None, stream=None):
+    """Single-token decode against a 4-bit cache: q [B, Hq, 1, D] (float16 or
+    bfloat16, what the cache was written from) is token lens[b] - 1 of its
+    sequence and sees the tokens up to itself, or the last ``window`` of them.
+
+    ``cache`` uint8 [pages, Hkv, kv4_page_bytes(page, D)], ``table`` int32 [B,
+    max_pages], ``lens`` int32 [B].  ``scale`` defaults to 1/sqrt(D);
+    ``alibi_slopes`` and ``softcap`` as for attn_decode.  ``workspace`` (uint8
+    GPU tensor of attn_decode_kv4_workspace_bytes) is allocated when not given.
+    Returns ``o`` [B, Hq, 1, D], 0 for a sequence that sees nothing.
+    """
+    r = (_BINDING or _load_binding()).attn_decode_kv4(q, cache, table, lens, o, scale, alibi_slopes, softcap, window,
+                                                      workspace, stream)
+    if r is not None:
+        return _result(r)
+    _require(q.dim() == 4 and q.is_contiguous() and q.shape[2] == 1, "q must be contiguous [B, Hq, 1, D]")
+    _require(q.dtype in _DTYPE_CODE, "dtype must be float16 or bfloat16")
+    B, Hq, _, D = q.shape
+    _same_device(q, cache=cache)
+    page = _cache_page(cache, D)
+    _require(_paged(cache, table, lens)[0] == B, "table and lens must have one row for each of q's sequences")
+    if alibi_slopes is not None:
+        _same_device(q, alibi_slopes=alibi_slopes)
+        _require(alibi_slopes.dtype == torch.float32 and alibi_slopes.is_contiguous() and alibi_slopes.numel() == Hq,
+                 "alibi_slopes must be a contiguous float32 tensor with one value per query head")
+    stream = _on_device(q, stream)
+    if o is None:
+        o = _allocate(q.shape, q, stream)
+    _same_device(q, o=o)
+    _require(o.shape == q.shape and o.dtype == q.dtype and o.is_contiguous(),
+             "o must be a contiguous GPU tensor shaped like q")
+    if workspace is None:
+        _require(isinstance(stream, torch.cuda.Stream), "a stream of this kind needs a workspace of the caller's")
+        workspace = _allocate((max(attn_decode_kv4_workspace_bytes(B, Hq, cache.shape[1], D), 16),), q, stream,
+                              torch.uint8)
+    _same_device(q, workspace=workspace)
+    _require(workspace.is_contiguous(), "workspace must be contiguous")
+    sc = 1.0 / math.sqrt(D) if scale is None else float(scale)
+    with torch.cuda.device(q.device):
+        _check(load_library().attn_decode_kv4(_ptr(q), _ptr(cache), _ptr(table), _ptr(lens), _ptr(o), B, Hq,
+                                              cache.shape[1], D, cache.shape[0], page, table.shape[1], sc,
+                                              _ptr(alibi_slopes), float(softcap or 0.0), int(window or 0),
+                                              _ptr(workspace), workspace.numel() * workspace.element_size(),
+                                              _DTYPE_CODE[q.dtype], _stream(stream)))
+    return o
 
 
 def norm_partials(workspace, N, chunks):

@@ -53,7 +53,9 @@ UNITS = [(f"prefill{k}", "prefill.hip", ["-fno-honor-nans", f"-DATTN_PREFILL_SHA
          for k in range(4)] + [("decode", "decode.hip", ["-save-temps"]), ("peaks", "peaks.hip", ["-save-temps"]),
             ("norms", "norms.hip", ["-save-temps"]),
             ("prefill_split", "prefill_split.hip", ["-fno-honor-nans", "-save-temps"]),
-            ("attn_api", "attn_api.cpp", [])]
+            ("rope", "rope.hip", ["-save-temps"]), ("kv4", "kv4.hip", ["-save-temps"]),
+            ("decode_kv4", "decode_kv4.hip", ["-save-temps"]),
+            ("attn_api", "attn_api.cpp", []), ("serve_api", "serve_api.cpp", [])]
 
 
 def unit_dir(name):
@@ -62,9 +64,14 @@ def unit_dir(name):
 
 
 def device_asm_files():
-    """Device assembly of every kernel unit written by the last build()."""
+    """Device assembly of every attention and norm kernel unit written by the last build()."""
     return prefill_asm_files() + [os.path.join(unit_dir(u), f"{u}-hip-amdgcn-amd-amdhsa-{ARCH}.s")
                                   for u in ("prefill_split", "decode", "peaks", "norms")]
+
+
+def serve_asm_files():
+    """Device assembly of the kernels around the 4-bit cache (rope.h, kv4.h)."""
+    return [os.path.join(unit_dir(u), f"{u}-hip-amdgcn-amd-amdhsa-{ARCH}.s") for u in ("rope", "kv4", "decode_kv4")]
 
 
 def prefill_asm_files():

@@ -41,6 +41,10 @@ bool sizes_fit(int B, int Hq, int Hkv, int Lq, int Lk, int D) {
   return q < (int64_t(1) << 40) && k < (int64_t(1) << 40);
 }
 
+}  // namespace
+
+namespace attn {
+
 int hip_fail(hipError_t e) {
   g_last_hip_error = (int)e;
   return ATTN_ERR_HIP;
@@ -60,6 +64,13 @@ int compute_units() {
   if (dev < 64) cached[dev].store(n, std::memory_order_relaxed);
   return n;
 }
+
+}  // namespace attn
+
+using attn::compute_units;
+using attn::hip_fail;
+
+namespace {
 
 // Query heads that one decode workgroup serves (the grid divides the group by it).
 int decode_heads_per_block(int group) {

@@ -16,14 +16,19 @@
 #include <algorithm>
 #include <climits>
 #include <cmath>
+#include <initializer_list>
+#include <utility>
 
 #include <ATen/ATen.h>
 #include <c10/hip/HIPStream.h>
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "../../include/attn.h"
+#include "../../include/kv4.h"
 #include "../../include/norms.h"
+#include "../../include/rope.h"
 
 namespace {
 
@@ -307,6 +312,250 @@ PyObject* py_rmsnorm_rowmax(PyObject*, PyObject* const* x, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
+// A tensor on the current device, contiguous unless `strided`; nullptr otherwise.
+const at::Tensor* here(PyObject* obj, bool strided = false) {
+  if (!THPVariable_CheckExact(obj)) return nullptr;
+  const at::Tensor& t = THPVariable_Unpack(obj);
+  if (t.layout() != c10::kStrided || !t.is_cuda() || (!strided && !t.is_contiguous()) || !ints(t)) return nullptr;
+  return t.device().index() == c10::hip::getCurrentHIPStream().device_index() ? &t : nullptr;
+}
+
+// The same, of a type and shape.
+const at::Tensor* here(PyObject* obj, at::ScalarType type, at::IntArrayRef shape) {
+  const at::Tensor* t = here(obj);
+  return t && t->scalar_type() == type && t->sizes() == shape ? t : nullptr;
+}
+
+// [B, H, L, D] whose rows are contiguous, and its strides of batches, heads and
+// tokens (0 where there is one alone).
+const at::Tensor* rows(PyObject* obj, long long (&strides)[3]) {
+  const at::Tensor* t = here(obj, true);
+  if (!t || t->dim() != 4 || (t->size(3) != 1 && t->stride(3) != 1)) return nullptr;
+  for (int i = 0; i < 3; ++i) strides[i] = t->size(i) > 1 ? t->stride(i) : 0;
+  return t;
+}
+
+// The given output of that type and shape, or a new one; false if the given one is not plain.
+bool output(PyObject* obj, const at::Tensor& like, at::ScalarType type, at::IntArrayRef shape, at::Tensor& out) {
+  if (obj == Py_None) {
+    out = at::empty(shape, like.options().dtype(type));
+    return true;
+  }
+  const at::Tensor* t = here(obj, type, shape);
+  if (t) out = *t;
+  return t != nullptr;
+}
+
+bool overlap(const at::Tensor& a, const at::Tensor& b) {
+  const char *p = static_cast<const char*>(a.data_ptr()), *q = static_cast<const char*>(b.data_ptr());
+  return p < q + b.nbytes() && q < p + a.nbytes();
+}
+
+// A tuple of outputs, or the error status.
+PyObject* results(int rc, std::initializer_list<std::pair<PyObject*, at::Tensor*>> outs) {
+  if (rc != ATTN_OK) return PyLong_FromLong(rc);
+  PyObject* r = PyTuple_New((Py_ssize_t)outs.size());
+  if (!r) return nullptr;
+  Py_ssize_t i = 0;
+  for (const auto& [given, made] : outs) {
+    PyObject* o = made ? result(rc, given, std::move(*made)) : none();
+    if (!o) {
+      Py_DECREF(r);
+      return nullptr;
+    }
+    PyTuple_SET_ITEM(r, i++, o);
+  }
+  return r;
+}
+
+// (q, k, positions, freqs, q_out, k_out, interleaved, magnitude, bwd, stream) -> (q_out, k_out)
+PyObject* py_rope(PyObject*, PyObject* const* x, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  bool inter, bwd;
+  float magnitude;
+  long long qs[3], ks[3];
+  if (n != 10 || x[9] != Py_None || !truth(x[6], inter) || !truth(x[8], bwd) || !number(x[7], magnitude)) return none();
+  const at::Tensor* q = rows(x[0], qs);
+  if (!q) return none();
+  const at::Tensor* k = nullptr;
+  if (x[1] != Py_None && !(k = rows(x[1], ks))) return none();
+  if (!k && x[5] != Py_None) return none();
+  const auto type = q->scalar_type();
+  rope_dtype dtype;
+  if (type == at::kHalf) dtype = ROPE_F16;
+  else if (type == at::kBFloat16) dtype = ROPE_BF16;
+  else if (type == at::kFloat) dtype = ROPE_F32;
+  else return none();
+  const int64_t B = q->size(0), L = q->size(2), D = q->size(3);
+  if (k && (k->scalar_type() != type || k->size(0) != B || k->size(2) != L || k->size(3) != D)) return none();
+  const at::Tensor *pos = here(x[2]), *freqs = here(x[3]);
+  if (!pos || !freqs || freqs->scalar_type() != at::kDouble || freqs->dim() != 1) return none();
+  if (pos->scalar_type() != at::kInt && pos->scalar_type() != at::kLong) return none();
+  const bool each = pos->dim() == 2 && pos->size(0) == B && pos->size(1) == L;
+  if (!each && !(pos->dim() == 1 && pos->size(0) == L)) return none();
+  if (freqs->size(0) > INT_MAX / 2) return none();
+  at::Tensor qo, ko;
+  if (!output(x[4], *q, type, q->sizes(), qo) || (k && !output(x[5], *q, type, k->sizes(), ko))) return none();
+  if (qo.data_ptr() == q->data_ptr() && !q->is_contiguous()) return none();
+  if (k && ko.data_ptr() == k->data_ptr() && !k->is_contiguous()) return none();
+  const void *qp = q->data_ptr(), *kp = k ? k->data_ptr() : nullptr, *pp = pos->data_ptr();
+  void *qop = qo.data_ptr(), *kop = k ? ko.data_ptr() : nullptr;
+  const double* fp = static_cast<const double*>(freqs->data_ptr());
+  const int Hq = (int)q->size(1), Hkv = k ? (int)k->size(1) : 0, R = 2 * (int)freqs->size(0);
+  const int bits = pos->scalar_type() == at::kLong ? 64 : 32;
+  const hipStream_t s = stream();
+  const int rc = unlocked([&] {
+    return (bwd ? rope_bwd : rope_fwd)(qp, qs, qop, Hq, kp, k ? ks : nullptr, kop, Hkv, (int)B, (int)L, (int)D, pp,
+                                       bits, each ? L : 0, fp, R, inter, magnitude, dtype, s);
+  });
+  return results(rc, {{x[4], &qo}, {x[5], k ? &ko : nullptr}});
+  END_HANDLE_TH_ERRORS
+}
+
+// (lens, counts, table, free_pages, page, L, slots, positions, new_lens, taken, stream) -> the last four
+PyObject* py_kv_slots(PyObject*, PyObject* const* x, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  int page, L;
+  if (n != 11 || x[10] != Py_None || !whole(x[4], page) || !whole(x[5], L) || L < 1) return none();
+  const at::Tensor *lens = here(x[0]), *counts = here(x[1]), *table = here(x[2]), *pages = here(x[3]);
+  if (!lens || !counts || !table || !pages || lens->dim() != 1 || table->dim() != 2 || pages->dim() != 1) return none();
+  const int64_t B = lens->size(0), M = table->size(1);
+  if (counts->sizes() != lens->sizes() || table->size(0) != B) return none();
+  for (const at::Tensor* t : {lens, counts, table, pages})
+    if (t->scalar_type() != at::kInt) return none();
+  at::Tensor out[4];
+  if (!output(x[6], *lens, at::kLong, {B, L}, out[0]) || !output(x[7], *lens, at::kInt, {B, L}, out[1]) ||
+      !output(x[8], *lens, at::kInt, {B}, out[2]) || !output(x[9], *lens, at::kInt, {1}, out[3]))
+    return none();
+  for (int i = 0; i < 4; ++i)
+    if (x[6 + i] != Py_None)
+      for (const at::Tensor* t : {lens, counts, table, pages})
+        if (overlap(out[i], *t)) return none();
+  const int* pt[3] = {static_cast<const int*>(lens->data_ptr()), static_cast<const int*>(counts->data_ptr()),
+                      static_cast<const int*>(pages->data_ptr())};
+  int* tp = static_cast<int*>(table->data_ptr());
+  long long* sp = static_cast<long long*>(out[0].data_ptr());
+  int* op[3] = {static_cast<int*>(out[1].data_ptr()), static_cast<int*>(out[2].data_ptr()),
+                static_cast<int*>(out[3].data_ptr())};
+  const int F = (int)pages->size(0);
+  const hipStream_t s = stream();
+  const int rc = unlocked(
+      [&] { return kv_slots(pt[0], pt[1], tp, pt[2], F, (int)B, (int)M, page, L, sp, op[0], op[1], op[2], s); });
+  return results(rc, {{x[6], &out[0]}, {x[7], &out[1]}, {x[8], &out[2]}, {x[9], &out[3]}});
+  END_HANDLE_TH_ERRORS
+}
+
+// Tokens of a page of a cache [pages, H, bytes], 0 if it is none of head dim D.
+int cache_page(const at::Tensor& cache, int D) {
+  if (cache.scalar_type() != at::kByte || cache.dim() != 3 || (D != 64 && D != 128)) return 0;
+  const int64_t page = cache.size(2) * 16 / (17 * D);
+  return page > 0 && page <= INT_MAX && kv4_page_bytes((int)page, D) == (size_t)cache.size(2) ? (int)page : 0;
+}
+
+// (k, v, cache, slots, stream) -> cache
+PyObject* py_kv4_append(PyObject*, PyObject* const* x, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  long long ks[3], vs[3];
+  if (n != 5 || x[4] != Py_None) return none();
+  const at::Tensor *k = rows(x[0], ks), *v = rows(x[1], vs), *cache = here(x[2]);
+  if (!k || !v || !cache || k->sizes() != v->sizes()) return none();
+  const auto type = k->scalar_type();
+  if ((type != at::kHalf && type != at::kBFloat16) || v->scalar_type() != type) return none();
+  const int B = (int)k->size(0), H = (int)k->size(1), L = (int)k->size(2), D = (int)k->size(3);
+  const int page = cache_page(*cache, D);
+  const at::Tensor* slots = here(x[3], at::kLong, {B, L});
+  if (!page || cache->size(1) != H || !slots) return none();
+  const void *kp = k->data_ptr(), *vp = v->data_ptr();
+  void* cp = cache->data_ptr();
+  const long long* sp = static_cast<const long long*>(slots->data_ptr());
+  const hipStream_t s = stream();
+  const int rc = unlocked([&] {
+    return kv4_append(kp, ks, vp, vs, cp, sp, B, H, L, D, (int)cache->size(0), page,
+                      type == at::kHalf ? ATTN_F16 : ATTN_BF16, s);
+  });
+  if (rc != ATTN_OK) return PyLong_FromLong(rc);
+  Py_INCREF(x[2]);
+  return x[2];
+  END_HANDLE_TH_ERRORS
+}
+
+// (cache, table, lens, L, D, dtype, k, v, starts, stream) -> (k, v)
+PyObject* py_kv4_load(PyObject*, PyObject* const* x, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  int L, D;
+  if (n != 10 || x[9] != Py_None || !whole(x[3], L) || !whole(x[4], D) || L < 1 || !THPDtype_Check(x[5])) return none();
+  const auto type = reinterpret_cast<THPDtype*>(x[5])->scalar_type;
+  if (type != at::kHalf && type != at::kBFloat16) return none();
+  const at::Tensor *cache = here(x[0]), *table = here(x[1]);
+  if (!cache || !table || table->dim() != 2 || table->scalar_type() != at::kInt) return none();
+  const int page = cache_page(*cache, D);
+  const int64_t B = table->size(0);
+  const at::Tensor *lens = here(x[2], at::kInt, {B}), *starts = nullptr;
+  if (!page || !lens || (x[8] != Py_None && !(starts = here(x[8], at::kInt, {B})))) return none();
+  at::Tensor k, v;
+  const int64_t shape[4] = {B, cache->size(1), L, D};
+  if (!output(x[6], *cache, type, shape, k) || !output(x[7], *cache, type, shape, v)) return none();
+  const void* cp = cache->data_ptr();
+  const int *tp = static_cast<const int*>(table->data_ptr()), *lp = static_cast<const int*>(lens->data_ptr()),
+            *sp = starts ? static_cast<const int*>(starts->data_ptr()) : nullptr;
+  void *kp = k.data_ptr(), *vp = v.data_ptr();
+  const hipStream_t s = stream();
+  const int rc = unlocked([&] {
+    return kv4_load(cp, tp, sp, lp, kp, vp, (int)B, (int)shape[1], L, D, (int)cache->size(0), page,
+                    (int)table->size(1), type == at::kHalf ? ATTN_F16 : ATTN_BF16, s);
+  });
+  return results(rc, {{x[6], &k}, {x[7], &v}});
+  END_HANDLE_TH_ERRORS
+}
+
+// (q, cache, table, lens, o, scale, alibi_slopes, softcap, window, workspace, stream)
+PyObject* py_attn_decode_kv4(PyObject*, PyObject* const* x, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  float cap = 0.f, scale;
+  int window = 0;
+  if (n != 11 || x[10] != Py_None) return none();
+  if (x[7] != Py_None && !number(x[7], cap)) return none();
+  if (x[8] != Py_None && !whole(x[8], window)) return none();
+  const at::Tensor *q = here(x[0]), *cache = here(x[1]), *table = here(x[2]);
+  if (!q || !cache || !table || q->dim() != 4 || q->size(2) != 1 || table->dim() != 2) return none();
+  const auto type = q->scalar_type();
+  if ((type != at::kHalf && type != at::kBFloat16) || table->scalar_type() != at::kInt) return none();
+  const int64_t B = q->size(0);
+  const int Hq = (int)q->size(1), D = (int)q->size(3), page = cache_page(*cache, D);
+  const at::Tensor* lens = here(x[3], at::kInt, {B});
+  if (!page || !lens || table->size(0) != B) return none();
+  const float* slopes = nullptr;
+  if (x[6] != Py_None) {
+    const at::Tensor* t = here(x[6]);
+    if (!t || t->scalar_type() != at::kFloat || t->numel() != Hq) return none();
+    slopes = static_cast<const float*>(t->data_ptr());
+  }
+  if (x[5] == Py_None) scale = (float)(1.0 / std::sqrt((double)D));
+  else if (!number(x[5], scale)) return none();
+  at::Tensor o, ws;
+  if (!output(x[4], *q, type, q->sizes(), o)) return none();
+  if (x[9] != Py_None) {
+    const at::Tensor* t = here(x[9]);
+    if (!t) return none();
+    ws = *t;
+  } else {
+    const size_t need = attn_decode_kv4_workspace_bytes((int)B, Hq, (int)cache->size(1), D);
+    ws = at::empty({(int64_t)std::max<size_t>(need, 16)}, q->options().dtype(at::kByte));
+  }
+  const void *qp = q->data_ptr(), *cp = cache->data_ptr();
+  const int *tp = static_cast<const int*>(table->data_ptr()), *lp = static_cast<const int*>(lens->data_ptr());
+  void *op = o.data_ptr(), *wp = ws.data_ptr();
+  const size_t bytes = ws.nbytes();
+  const hipStream_t s = stream();
+  const int rc = unlocked([&] {
+    return attn_decode_kv4(qp, cp, tp, lp, op, (int)B, Hq, (int)cache->size(1), D, (int)cache->size(0), page,
+                           (int)table->size(1), scale, slopes, cap, window, wp, bytes,
+                           type == at::kHalf ? ATTN_F16 : ATTN_BF16, s);
+  });
+  return result(rc, x[4], std::move(o));
+  END_HANDLE_TH_ERRORS
+}
+
 template <PyObject* (*F)(PyObject*, PyObject* const*, Py_ssize_t)>
 PyCFunction fast() {
   return reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(F));
@@ -318,6 +567,11 @@ PyMethodDef methods[] = {
     {"attn_decode_noalloc", fast<py_attn_decode_noalloc>(), METH_FASTCALL, nullptr},
     {"norm_l2", fast<py_norm_l2>(), METH_FASTCALL, nullptr},
     {"rmsnorm_rowmax", fast<py_rmsnorm_rowmax>(), METH_FASTCALL, nullptr},
+    {"rope", fast<py_rope>(), METH_FASTCALL, nullptr},
+    {"kv_slots", fast<py_kv_slots>(), METH_FASTCALL, nullptr},
+    {"kv4_append", fast<py_kv4_append>(), METH_FASTCALL, nullptr},
+    {"kv4_load", fast<py_kv4_load>(), METH_FASTCALL, nullptr},
+    {"attn_decode_kv4", fast<py_attn_decode_kv4>(), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

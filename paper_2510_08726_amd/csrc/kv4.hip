@@ -1,0 +1,246 @@
+// The paged 4-bit cache (include/kv4.h): where new tokens go, writing them, and
+// reading them back.  The conversions between E2M1 and 16 bits are gfx950
+// instructions, which take the block's power of two as an operand.
+
+#include "kernel_common.h"
+#include "kv4_common.h"
+#include "launch.h"
+
+namespace attn {
+
+namespace {
+
+constexpr int kThreads = 256;
+
+// Inclusive sum over the workgroup; every thread must call.  `total` is the
+// last one's.  sh: one int per wave.
+__device__ __forceinline__ int block_scan(int x, int* sh, int& total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int y = __shfl_up(x, d, 64);
+    if (lane >= d) x += y;
+  }
+  __syncthreads();                       // sh is free
+  if (lane == 63) sh[wave] = x;
+  __syncthreads();
+  int before = 0, all = 0;
+#pragma unroll
+  for (int w = 0; w < kThreads / 64; ++w) {
+    const int y = sh[w];
+    before += w < wave ? y : 0;
+    all += y;
+  }
+  total = all;
+  return x + before;
+}
+
+struct Need {
+  int n, count, held, need;   // tokens now and new, pages now and new
+};
+
+__device__ __forceinline__ Need need_of(const SlotsParams& p, int b) {
+  const int page = 1 << p.shift, room = p.M << p.shift;
+  Need r;
+  r.n = min(max(p.lens[b], 0), room);
+  r.count = min(max(p.counts[b], 0), p.L);
+  r.held = (int)(((int64_t)r.n + page - 1) >> p.shift);
+  const int64_t want = min((int64_t)r.n + r.count, (int64_t)room);
+  r.need = (int)((want + page - 1) >> p.shift) - r.held;
+  return r;
+}
+
+// A workgroup takes kItems consecutive (sequence, token) items.  It sums the needs
+// of the sequences before its first, scans those of its own, and writes each
+// item's slot; the item in a new page's first row writes the page into the
+// table.  (No workgroup waits for another: each reads the lengths before it,
+// which the caches hold.)
+constexpr int kItems = 512;
+
+__global__ __launch_bounds__(kThreads) void kv_slots_kernel(SlotsParams p) {
+  __shared__ int wave_sum[kThreads / 64];
+  __shared__ int start[kItems], held[kItems], stored[kItems], len[kItems];
+  const int64_t items = (int64_t)p.B * p.L, i0 = (int64_t)blockIdx.x * kItems;
+  const int64_t i1 = min(i0 + kItems, items);
+  const int b0 = (int)(i0 / p.L), b1 = (int)((i1 - 1) / p.L);
+  int before = 0;
+  for (int b = threadIdx.x; b < b0; b += kThreads) before += need_of(p, b).need;
+  int base;
+  block_scan(before, wave_sum, base);
+  for (int c = b0; c <= b1; c += kThreads) {
+    const int b = c + threadIdx.x;
+    Need r{};
+    if (b <= b1) r = need_of(p, b);
+    int total;
+    const int from = base + block_scan(r.need, wave_sum, total) - r.need;
+    if (b <= b1) {
+      const int got = min(max(p.nfree - from, 0), r.need);
+      const int64_t fit = ((int64_t)(r.held + got) << p.shift) - r.n;
+      start[b - b0] = from;
+      held[b - b0] = r.held;
+      stored[b - b0] = (int)min(fit, (int64_t)r.count);
+      len[b - b0] = r.n;
+    }
+    base += total;
+  }
+  __syncthreads();
+  if (i1 == items && threadIdx.x == 0) *p.taken = min(base, p.nfree);
+  const int mask = (1 << p.shift) - 1;
+  for (int64_t i = i0 + threadIdx.x; i < i1; i += kThreads) {
+    const int b = (int)(i / p.L), l = (int)(i - (int64_t)b * p.L), k = b - b0;
+    const int64_t pos = (int64_t)len[k] + l;
+    int64_t slot = -1;
+    if (l < stored[k]) {
+      const int pi = (int)(pos >> p.shift), row = (int)pos & mask;
+      int* entry = p.table + (int64_t)b * p.M + pi;
+      int page;
+      if (pi >= held[k]) {
+        page = p.free_pages[start[k] + pi - held[k]];
+        if (row == 0) *entry = page;
+      } else page = *entry;
+      slot = ((int64_t)page << p.shift) + row;
+      if (page < 0) slot = -1;
+    }
+    p.slots[i] = slot;
+    p.positions[i] = (int)pos;
+    if (l == 0) p.new_lens[b] = len[k] + stored[k];
+  }
+}
+
+// Four lanes hold a block of 32 dims, 8 each: 16 bytes in, 4 bytes out.  K and V
+// of a row in one thread; neighbouring lanes hold a row, then the next token's.
+template <int D, typename T>
+__global__ __launch_bounds__(kThreads) void kv4_append_kernel(Kv4AppendParams p) {
+  constexpr int LPR = D / 8;                 // lanes per row
+  constexpr int kTop = sizeof(T) == 2 && __is_same(T, _Float16) ? 13 : 125;
+  const int64_t idx = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  const int lig = (int)(idx % LPR);
+  int64_t row = idx / LPR;
+  const int l = (int)(row % p.L);
+  row /= p.L;
+  const int h = (int)(row % p.H), b = (int)(row / p.H);
+  if (b >= p.B) return;
+  const int64_t slot = p.slots[(int64_t)b * p.L + l];
+  if (slot < 0 || slot >= (int64_t)p.pages << p.shift) return;    // the lanes of a row agree
+  const int page = 1 << p.shift, r = (int)slot & (page - 1);
+  unsigned char* base = p.cache + ((slot >> p.shift) * p.H + h) * (int64_t)kv4_block_bytes<D>(p.shift);
+  u32x4 x[2];
+#pragma unroll
+  for (int k = 0; k < 2; ++k)
+    x[k] = *reinterpret_cast<const u32x4*>(static_cast<const T*>(p.x[k]) + b * p.sb[k] + h * p.sh[k] + l * p.sl[k] + 8 * lig);
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    float f[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      f[2 * i] = Elem<T>::lo(x[k][i]);
+      f[2 * i + 1] = Elem<T>::hi(x[k][i]);
+    }
+    // The largest magnitude as bits: ordered as the values are, infinities
+    // and NaN above them.
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float v = f[i];
+      top = max(top, __builtin_bit_cast(uint32_t, v) & 0x7fffffffu);
+    }
+    top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0xB1, 0xf, 0xf, false));   // quad_perm [1,0,3,2]
+    top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0x4E, 0xf, 0xf, false));   // quad_perm [2,3,0,1]
+    const bool fine = top < 0x7f800000u;
+    // 2^e with a <= 7 2^e: the exponent of a less 2, one more over 1.75 of its binade.
+    int e = (int)((top + 0x1fffffu) >> 23) - 129;
+    e = min(max(e, -kTop), kTop);
+    const uint32_t inv = (uint32_t)(127 - e) << 23;
+    const float s = __builtin_bit_cast(float, inv);
+    uint32_t code = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {            // scaled first: the products are exact
+      const float a = f[2 * i] * s, c = f[2 * i + 1] * s;
+      switch (i) {
+        case 0: code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, a, c, 1.f, 0); break;
+        case 1: code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, a, c, 1.f, 1); break;
+        case 2: code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, a, c, 1.f, 2); break;
+        default: code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, a, c, 1.f, 3);
+      }
+    }
+    if (!fine) code = 0;
+    *reinterpret_cast<uint32_t*>(base + k * kv4_code_bytes<D>(p.shift) + (int64_t)r * (D / 2) + 4 * lig) = code;
+    if ((lig & 3) == 0)
+      base[2 * kv4_code_bytes<D>(p.shift) + k * kv4_scale_bytes<D>(p.shift) + ((lig >> 2) << p.shift) + r] =
+          (unsigned char)(fine ? e + 127 : 255);
+  }
+}
+
+// 8 dims a lane: 4 bytes of codes and a scale byte in, 16 bytes out.
+template <int D, typename T>
+__global__ __launch_bounds__(kThreads) void kv4_load_kernel(Kv4LoadParams p) {
+  constexpr int LPR = D / 8;
+  const int64_t idx = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  const int lig = (int)(idx % LPR);
+  const int64_t row = idx / LPR;
+  const int l = (int)(row % p.L);
+  const int64_t bh = row / p.L;
+  const int h = (int)(bh % p.H), b = (int)(bh / p.H);
+  if (b >= p.B) return;
+  const int64_t t = (int64_t)(p.starts ? max(p.starts[b], 0) : 0) + l;
+  const int64_t n = min((int64_t)p.lens[b], (int64_t)p.M << p.shift);
+  const int pg = t < n ? p.table[(int64_t)b * p.M + (t >> p.shift)] : -1;
+  const bool there = (unsigned)pg < (unsigned)p.pages;
+  uint32_t code[2] = {0u, 0u}, scale[2] = {0u, 0u};
+  if (there) {
+    const int r = (int)t & ((1 << p.shift) - 1);
+    const unsigned char* base = p.cache + ((int64_t)pg * p.H + h) * (int64_t)kv4_block_bytes<D>(p.shift);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      code[k] = *reinterpret_cast<const uint32_t*>(base + k * kv4_code_bytes<D>(p.shift) + (int64_t)r * (D / 2) + 4 * lig);
+      scale[k] = base[2 * kv4_code_bytes<D>(p.shift) + k * kv4_scale_bytes<D>(p.shift) + ((lig >> 2) << p.shift) + r];
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const uint32_t bits = scale[k] << 23;
+    const float s = __builtin_bit_cast(float, bits);
+    u32x4 out;
+    out[0] = Fp4<T>::template cvt<0>(code[k], s);
+    out[1] = Fp4<T>::template cvt<1>(code[k], s);
+    out[2] = Fp4<T>::template cvt<2>(code[k], s);
+    out[3] = Fp4<T>::template cvt<3>(code[k], s);
+    *reinterpret_cast<u32x4*>(static_cast<T*>(p.y[k]) + row * D + 8 * lig) = out;
+  }
+}
+
+template <int D, typename T>
+hipError_t append(const Kv4AppendParams& p, hipStream_t stream) {
+  const int64_t threads = (int64_t)p.B * p.H * p.L * (D / 8);
+  hipLaunchKernelGGL((kv4_append_kernel<D, T>), dim3((unsigned)((threads + kThreads - 1) / kThreads)), dim3(kThreads),
+                     0, stream, p);
+  return hipGetLastError();
+}
+
+template <int D, typename T>
+hipError_t load(const Kv4LoadParams& p, hipStream_t stream) {
+  const int64_t threads = (int64_t)p.B * p.H * p.L * (D / 8);
+  hipLaunchKernelGGL((kv4_load_kernel<D, T>), dim3((unsigned)((threads + kThreads - 1) / kThreads)), dim3(kThreads), 0,
+                     stream, p);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_slots(const SlotsParams& p, hipStream_t stream) {
+  const int64_t blocks = ((int64_t)p.B * p.L + kItems - 1) / kItems;
+  hipLaunchKernelGGL(kv_slots_kernel, dim3((unsigned)blocks), dim3(kThreads), 0, stream, p);
+  return hipGetLastError();
+}
+
+hipError_t launch_kv4_append(const Kv4AppendParams& p, hipStream_t stream) {
+  if (p.D == 64) return p.bf16 ? append<64, __bf16>(p, stream) : append<64, _Float16>(p, stream);
+  return p.bf16 ? append<128, __bf16>(p, stream) : append<128, _Float16>(p, stream);
+}
+
+hipError_t launch_kv4_load(const Kv4LoadParams& p, hipStream_t stream) {
+  if (p.D == 64) return p.bf16 ? load<64, __bf16>(p, stream) : load<64, _Float16>(p, stream);
+  return p.bf16 ? load<128, __bf16>(p, stream) : load<128, _Float16>(p, stream);
+}
+
+}  // namespace attn

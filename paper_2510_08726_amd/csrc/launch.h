@@ -133,6 +133,89 @@ inline bool norm_one_kernel(bool rms, long long M, int elem, int chunks) {
   return chunks == 1 && (!rms || M * elem <= kNormRowBytes);
 }
 
+// Rotary positions (rope.hip).
+struct RopeParams {
+  const void* x[2];     // queries, keys (or nullptr)
+  void* y[2];
+  int64_t sb[2], sh[2], sl[2];   // strides in elements of x
+  int H[2];
+  int B, L, D, R;       // R: rotary dim
+  const void* pos;
+  int64_t pos_stride;
+  const double* freqs;
+  float magnitude, sign;   // sign -1: the transposed rotation
+  bool pos64, interleaved;
+  int dtype;            // 0 fp16, 1 bf16, 2 fp32
+  int heads;            // heads per thread, set by the launcher
+};
+hipError_t launch_rope(const RopeParams& p, hipStream_t stream);
+
+// The paged 4-bit cache (kv4.hip).
+struct SlotsParams {
+  const int* lens;
+  const int* counts;
+  int* table;
+  const int* free_pages;
+  int64_t* slots;
+  int* positions;
+  int* new_lens;
+  int* taken;
+  int nfree, B, M, L, shift;   // shift: log2 of the page size
+};
+hipError_t launch_slots(const SlotsParams& p, hipStream_t stream);
+
+struct Kv4AppendParams {
+  const void* x[2];     // K, V
+  int64_t sb[2], sh[2], sl[2];   // strides in elements
+  unsigned char* cache;
+  const int64_t* slots;
+  int B, H, L, D, pages, shift;
+  bool bf16;
+};
+hipError_t launch_kv4_append(const Kv4AppendParams& p, hipStream_t stream);
+
+struct Kv4LoadParams {
+  const unsigned char* cache;
+  const int* table;
+  const int* starts;    // or nullptr
+  const int* lens;
+  void* y[2];           // K, V
+  int B, H, L, D, pages, shift, M;
+  bool bf16;
+};
+hipError_t launch_kv4_load(const Kv4LoadParams& p, hipStream_t stream);
+
+// Decode attention over it (decode_kv4.hip).
+struct Kv4DecodeParams {
+  const void* q;
+  const unsigned char* cache;
+  const int* table;
+  const int* lens;
+  void* o;
+  const float* slopes;  // device, [Hq], or nullptr
+  float* ws_o;          // [2 * shares, columns, D]
+  float* ws_m;          // [2 * shares, columns], log2 units
+  float* ws_l;
+  int B, Hq, Hkv, D, group;
+  int pages, shift, M;
+  int window;           // 0 for none
+  int head_tiles;       // column tiles of the query heads of a KV head
+  int shares;           // most workgroups
+  int bf16;
+  float c;              // scale * log2(e)
+  float cap_k2, cap_cl; // as DecodeParams
+};
+// Query heads that one workgroup serves: 16 or 32 matrix columns.
+constexpr int kv4_columns(int group) { return group <= 16 ? 16 : 32; }
+// Workgroups of the split kernel on a device of `cus` compute units.
+int kv4_shares(int group, int cus);
+hipError_t launch_decode_kv4(const Kv4DecodeParams& p, hipStream_t stream);
+
+// Compute units of the current device, 256 if it cannot be queried (attn_api.cpp).
+int compute_units();
+// Keeps the error for attn_last_hip_error; returns ATTN_ERR_HIP (attn_api.cpp).
+int hip_fail(hipError_t e);
+
 // Achievable-peak probes (peaks.hip).
 hipError_t launch_hbm_read(const void* buf, size_t bytes, float* sink, hipStream_t stream);
 int hbm_read_sink_floats();
