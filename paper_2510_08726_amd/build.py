@@ -54,7 +54,7 @@ UNITS = [(f"prefill{k}", "prefill.hip", ["-fno-honor-nans", f"-DATTN_PREFILL_SHA
             ("norms", "norms.hip", ["-save-temps"]),
             ("prefill_split", "prefill_split.hip", ["-fno-honor-nans", "-save-temps"]),
             ("rope", "rope.hip", ["-save-temps"]), ("kv4", "kv4.hip", ["-save-temps"]),
-            ("decode_kv4", "decode_kv4.hip", ["-save-temps"]),
+            ("decode_kv4", "decode_kv4.hip", ["-mllvm", "-amdgpu-mfma-vgpr-form=1", "-save-temps"]),
             ("attn_api", "attn_api.cpp", []), ("serve_api", "serve_api.cpp", [])]
 
 

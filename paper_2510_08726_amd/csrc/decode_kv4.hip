@@ -3,21 +3,22 @@
 //
 // Work.  A row is (sequence b, KV head, column tile of its query heads); its
 // tiles are those of the tokens that b sees.  All tiles of all rows, row
-// after row, are one list, and workgroup w of W takes the tiles from w T / W to
-// (w + 1) T / W: equal shares whatever the lengths.  A row inside one share is
-// finished there; others leave a partial (O, max, sum) for each share that they
-// lie in, and the second kernel joins those.
+// after row, are one list, and workgroup w of W takes an equal share of it, whatever
+// the lengths.  A row inside one share is finished there; others leave a
+// partial (O, max, sum) for each share that they lie in, and the second kernel joins
+// those.
 //
-// Tile.  The wave's lanes are n = lane % 16 and g = lane / 16.  S^T = K Q^T runs on
-// 16x16x32 MFMAs over the heads as columns: lane (n, g) holds dims [g D / 4, (g + 1) D / 4)
-// of token n as the A operand and the same dims of head n as B (the order
-// of the summed dims is free), so K goes from its rows to registers
-// in one load a lane, with the lane's scale (one at D = 128, half of one at D = 64), and the result has tokens 4 g + r of
-// head n in lane (n, g).  That is the B operand of O^T += V^T P^T if the summed
-// tokens are taken as 4 g + r of both 16-token halves; for its A operand lane (i, g) loads
-// dims [i D / 16, (i + 1) D / 16) of those eight tokens, and pairs of tokens are
-// permuted together after conversion.  No LDS and no cross-lane move in the
-// loop but for a new maximum.
+// Tile.  Each wave copies its tiles from HBM straight to LDS, kRing ahead, and
+// needs no other wave until the end of a row.  The wave's lanes are n = lane % 16 and g =
+// lane / 16.  S^T = K Q^T runs on 16x16x32 MFMAs over the heads as columns: lane (n, g)
+// holds dims [g D / 4, (g + 1) D / 4) of a token as the A operand and the same dims of head
+// n as B (the order of the summed dims is free), so the codes of a lane are
+// neighbours and have one scale.  MFMA row 4 g + r is token 4 r + g of its 16: the result
+// has tokens 4 r + g of head n in lane (n, g), which is the B operand of O^T += V^T P^T
+// if the summed tokens are taken in that order; for its A operand lane (i, g) reads dims
+// [i D / 16, (i + 1) D / 16) of its eight tokens, which at one r are four rows in line,
+// and pairs of tokens are permuted together after conversion.  No lane
+// needs another's values in the loop, but for a new maximum.
 //
 // Bound: 17 / 32 bytes a value and 4 flops a value and head leave it an HBM
 // stream; conversion is a VALU instruction for two values of K and two for two of V.
@@ -36,7 +37,13 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
 constexpr int kTile = 32;          // tokens
-constexpr int kLeast = kWaves;     // tiles a share holds at least: one for each wave
+constexpr int kStart = 8;          // units of a row's start and end
+constexpr int kLeast = 8;          // units a share holds at least
+
+// How many workgroups share a compute unit, and the tiles that a wave has in LDS
+// (160 KB hold 16 waves of 2 tiles at D = 128): what the registers allow.
+constexpr int per_unit(int D, int cols) { return cols == 16 ? 4 : D == 64 ? 3 : 2; }
+constexpr int ring_tiles(int D, int cols) { return D == 128 && cols == 16 ? 2 : 4; }
 constexpr float kLazy = 8.f;       // log2 units that a score may exceed its reference by
 
 template <typename T> struct Mfma16;
@@ -64,121 +71,158 @@ __device__ __forceinline__ Seen seen_of(const Kv4DecodeParams& p, int n) {
   return s;
 }
 
-// The list of all tiles and its shares: the first `more` hold one tile more
-// than the others.  (The entry point keeps the list below 2^31 tiles.)
+// Inclusive sum over the wave's lanes, by DPP: within rows of 16 lanes, then the
+// last lane of a row to the rows behind it.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int dpp_add(int x) {
+  return x + __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false);
+}
+__device__ __forceinline__ int wave_scan(int x) {
+  x = dpp_add<0x111, 0xf>(x);   // row_shr:1
+  x = dpp_add<0x112, 0xf>(x);   // row_shr:2
+  x = dpp_add<0x114, 0xf>(x);   // row_shr:4
+  x = dpp_add<0x118, 0xf>(x);   // row_shr:8
+  x = dpp_add<0x142, 0xa>(x);   // row_bcast:15
+  x = dpp_add<0x143, 0xc>(x);   // row_bcast:31
+  return x;
+}
+
+// The list of all rows' tiles.  A row counts kStart more: what its start
+// and end cost a workgroup beside its tiles, so that shares of many short rows take as long
+// as shares of one long one.  (The entry point keeps the list below 2^31.)
+__device__ __forceinline__ int units_of(const Seen& s) { return s.tiles ? s.tiles + kStart : 0; }
+
+// The shares of a list of `total`: the first `more` hold one unit more than the others.
 struct Shares {
-  int total, count, each, more;
+  int count, each, more;
   __device__ __forceinline__ int begin(int w) const { return w * each + min(w, more); }
-  __device__ __forceinline__ int of(int tile) const {
+  __device__ __forceinline__ int of(int unit) const {
     const int big = more * (each + 1);
-    return tile < big ? tile / (each + 1) : more + (tile - big) / each;
+    return unit < big ? unit / (each + 1) : more + (unit - big) / each;
   }
 };
 
 __device__ __forceinline__ Shares shares_of(const Kv4DecodeParams& p, int total) {
   Shares s;
-  s.total = total;
   s.count = min(p.shares, (total + kLeast - 1) / kLeast);
   s.each = s.count ? total / s.count : 0;
   s.more = total - s.each * s.count;
   return s;
 }
 
-// Tiles of one row of all sequences, and of those before sequence b; by one wave.
-__device__ __forceinline__ int row_tiles(const Kv4DecodeParams& p, int lane, int b, int& before) {
-  int all = 0, some = 0;
-  for (int i = lane; i < p.B; i += 64) {
-    const int t = seen_of(p, p.lens[i]).tiles;
-    all += t;
-    some += i < b ? t : 0;
-  }
-#pragma unroll
-  for (int d = 32; d > 0; d >>= 1) {
-    all += __shfl_xor(all, d, 64);
-    some += __shfl_xor(some, d, 64);
-  }
-  before = __builtin_amdgcn_readfirstlane(some);
-  return __builtin_amdgcn_readfirstlane(all);
-}
+// A tile in LDS: the codes of K and of V, row by row, with the 16-byte chunks of
+// a row in an order that keeps the reads free of bank conflicts (chunk c of row r at c ^ chunk_xor(r)),
+// then the scale bytes [K, V][D / 32][32].
+template <int D> struct Tile {
+  static constexpr int kRow = D / 2, kChunks = kRow / 16;
+  static constexpr int kCodes = kTile * kRow, kScales = 2 * kCodes, kBytes = kScales + 256;
+  static constexpr int kCopies = D == 128 ? 5 : 3;      // instructions that fill it
+  static __device__ __forceinline__ int chunk_xor(int r) { return (r >> 2) & (kChunks - 1); }
+};
 
-// What a lane loads of a tile: of both 16-token halves its token's dims of K and
-// their scale, and of eight tokens its dims of V and their scales (a byte each).
-template <int D> struct Raw;
-template <> struct Raw<128> {
-  typedef u32x4 kvec;
-  typedef uint32_t vvec;
-  kvec k[2];
-  vvec v[8];
-  uint32_t ks[2], vs[2];
-};
-template <> struct Raw<64> {
-  typedef uint32_t kvec __attribute__((ext_vector_type(2)));
-  typedef uint16_t vvec;
-  kvec k[2];
-  vvec v[8];
-  uint32_t ks[2], vs[2];
-};
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+// Read through the scalar cache: uniform addresses, not written by the kernel.
+typedef const __attribute__((address_space(4))) int* ScalarInts;
+__device__ __forceinline__ ScalarInts scalar(const int* p) {
+  return (ScalarInts)reinterpret_cast<uintptr_t>(p);
+}
 
 __device__ __forceinline__ float as_float(uint32_t bits) { return __builtin_bit_cast(float, bits); }
 
 template <int D, typename T, int NC, bool ALIBI, bool CAP>
-__global__ __launch_bounds__(kThreads) void decode_kv4_kernel(Kv4DecodeParams p) {
+__global__ __launch_bounds__(kThreads, per_unit(D, 16 * NC)) void decode_kv4_kernel(Kv4DecodeParams p) {
   typedef typename Elem<T>::vec8 vec8;
-  typedef typename Raw<D>::kvec kvec;
-  typedef typename Raw<D>::vvec vvec;
+  typedef Tile<D> TL;
   constexpr int COLS = 16 * NC;
   constexpr int KS = D / 32;          // MFMA steps of K Q^T
   constexpr int DL = D / 16;          // dims of V that a lane holds, and MFMAs of O^T
-  __shared__ __attribute__((aligned(16))) float sh_o[kWaves][COLS][D];
-  __shared__ float sh_m[kWaves][COLS], sh_l[kWaves][COLS];
+  // The waves' rings; at the end of a row their states, 16 columns at a time.
+  constexpr int kRing = ring_tiles(D, COLS);
+  constexpr int kLds = kWaves * kRing * TL::kBytes;
+  static_assert(kWaves * 16 * (D + 2) * 4 <= kLds, "the states fit into the rings");
+  __shared__ __attribute__((aligned(1024))) char lds[kLds];
+  float (*sh_o)[16][D] = reinterpret_cast<float (*)[16][D]>(lds);
+  float (*sh_m)[16] = reinterpret_cast<float (*)[16]>(lds + kWaves * 16 * D * 4);
+  float (*sh_l)[16] = sh_m + kWaves;
 
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n = lane & 15, g = lane >> 4;
   const int rows_b = p.Hkv * p.head_tiles;
+  char* const ring = lds + wave * (kRing * TL::kBytes);
+  const uint32_t ring_at = (uint32_t)(uintptr_t)(lds_void*)ring;
 
-  int none;
-  const Shares shares = shares_of(p, row_tiles(p, lane, 0, none) * rows_b);
+  // What a lane copies: a 16-byte chunk of K and of V (of both halves at D =
+  // 64), and four scale bytes (at D = 64 by half the lanes, the others again).
+  const int copy_row = lane / TL::kChunks;
+  const uint32_t copy_codes =
+      (uint32_t)((copy_row & 15) * TL::kRow + (((lane % TL::kChunks) ^ TL::chunk_xor(copy_row)) * 16));
+  const int copy_kv = (lane / (D / 4)) & 1, copy_blk = (lane >> 3) & (D / 32 - 1), copy_word = lane & 7;
+  const uint32_t copy_scales = (uint32_t)(2 * kv4_code_bytes<D>(p.shift) + copy_kv * kv4_scale_bytes<D>(p.shift) +
+                                          (copy_blk << p.shift) + 4 * (copy_word & 3));
+  // What it reads: its token's chunk of K and the scale, and its dims of V and
+  // the scales of their block.
+  const int tok_k = 4 * (n & 3) + (n >> 2);
+  const int read_k = tok_k * TL::kRow + (D == 128 ? (g ^ TL::chunk_xor(tok_k)) * 16
+                                                  : ((g >> 1) ^ TL::chunk_xor(tok_k)) * 16 + (g & 1) * 8);
+  const int read_ks = TL::kScales + (g * (D / 4) / 32) * kTile + tok_k;
+  const int read_vs = TL::kScales + (D / 32 + n * DL / 32) * kTile;
+  int read_v[4];
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    const int row = 4 * r + g, at = n * (D / 32);         // the byte of its row
+    read_v[r] = TL::kCodes + row * TL::kRow + ((at >> 4) ^ TL::chunk_xor(row)) * 16 + (at & 15);
+  }
+  const uint32_t scale_turn = (uint32_t)(8 * g + 9) & 31;   // rotates byte g into the exponent's place
+
+  // The list's length, and the sequence in which this share begins: the
+  // first whose units end behind its first.  64 lengths at a time, a lane each.
   const int w = blockIdx.x;
+  const int len0 = lane < p.B ? p.lens[lane] : 0;
+  const int mine0 = units_of(seen_of(p, len0)), upto0 = wave_scan(mine0);
+  int total = __builtin_amdgcn_readlane(upto0, 63);
+  for (int i = 64; i < p.B; i += 64)
+    total += __builtin_amdgcn_readlane(wave_scan(i + lane < p.B ? units_of(seen_of(p, p.lens[i + lane])) : 0), 63);
+  const Shares shares = shares_of(p, total * rows_b);
   if (w >= shares.count) return;
   int at = shares.begin(w);
   const int end = shares.begin(w + 1);
-
-  // The sequence of the first tile: the first whose tiles end behind it.
   int b = -1, before = 0;
-  for (int c = 0; c < p.B; c += 64) {
-    const int i = c + lane;
-    const int mine = i < p.B ? seen_of(p, p.lens[i]).tiles * rows_b : 0;
-    int upto = mine;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const int y = __shfl_up(upto, d, 64);
-      if (lane >= d) upto += y;
-    }
-    upto += before;
-    const uint64_t past = __ballot(upto > at);
+  Seen seen;
+  for (int i = 0; i < p.B; i += 64) {
+    const int len = i ? (i + lane < p.B ? p.lens[i + lane] : 0) : len0;
+    const int mine = i ? units_of(seen_of(p, len)) : mine0;
+    const int upto = before + (i ? wave_scan(mine) : upto0);
+    const uint64_t past = __ballot(upto * rows_b > at);
     if (past) {
       const int k = __builtin_ctzll(past);
-      b = c + k;
+      b = i + k;
       before = __builtin_amdgcn_readlane(upto - mine, k);
+      seen = seen_of(p, __builtin_amdgcn_readlane(len, k));
       break;
     }
     before = __builtin_amdgcn_readlane(upto, 63);
   }
   if (b < 0) return;
-  Seen seen = seen_of(p, __builtin_amdgcn_readfirstlane(p.lens[b]));
-  int row = (at - before) / max(seen.tiles, 1);    // of the sequence
-  int t0 = (at - before) - row * seen.tiles;
+  int row = (at - before * rows_b) / max(units_of(seen), 1);    // of the sequence
+  int u0 = (at - before * rows_b) - row * units_of(seen);
 
-  // (The lengths are read again for each sequence; were they changed meanwhile,
+  // (The lengths are read again for further sequences; were they changed meanwhile,
   // the conditions on row and b still keep every access in bounds.)
-  for (bool first = true; row < rows_b; first = false) {
-    const int t1 = min(seen.tiles, t0 + (end - at));
+  for (bool wrote = false; row < rows_b;) {
+    const int u1 = min(units_of(seen), u0 + (end - at));
+    const int t0 = max(u0 - kStart, 0), t1 = max(u1 - kStart, 0);
+    if (t0 < t1) {
+    if (wrote) __syncthreads();        // the states of the row before have been read
+    wrote = true;
     const int hk = row / p.head_tiles, ht = row - hk * p.head_tiles;
     const int hq0 = hk * p.group + ht * COLS;
     const int heads = min(p.group - ht * COLS, COLS);
     const int tok0 = seen.lo & ~(kTile - 1);
-    const int* table = p.table + (int64_t)b * p.M;
+    const ScalarInts table = scalar(p.table + (int64_t)b * p.M);
+    const uint32_t page_bytes = (uint32_t)p.Hkv * (uint32_t)kv4_block_bytes<D>(p.shift);    // under 2^31
+    const uint64_t head = reinterpret_cast<uint64_t>(p.cache) + (uint32_t)(hk * kv4_block_bytes<D>(p.shift));
 
     vec8 q[NC][KS];
     float slope[NC];
@@ -205,74 +249,150 @@ __global__ __launch_bounds__(kThreads) void decode_kv4_kernel(Kv4DecodeParams p)
       for (int j = 0; j < DL; ++j) o[c][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
 
-    // The pages of a tile's halves, -1 for none.
+    // What the table has for a tile's halves (past its end: the last entry again).
     auto pages = [&](int t, int (&pg)[2]) __attribute__((always_inline)) {
 #pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        const int pi = (tok0 + t * kTile + 16 * s) >> p.shift;
-        const int x = table[min(pi, p.M - 1)];
-        pg[s] = pi < p.M && (unsigned)x < (unsigned)p.pages ? x : -1;
-      }
+      for (int s = 0; s < 2; ++s) pg[s] = table[min((tok0 + t * kTile + 16 * s) >> p.shift, p.M - 1)];
     };
-    // A half without a page is read from page 0, and masked.
-    auto fetch = [&](int t, const int (&pg)[2], Raw<D>& x) __attribute__((always_inline)) {
+    // Start the copies of a tile into a slot of the ring.  A half without a page
+    // is read from page 0, and masked: returns bit s for it.
+    auto copy = [&](int t, const int (&pg)[2], int slot) __attribute__((always_inline)) {
+      uint64_t codes[2], scales[2];
+      uint32_t none = 0;
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
-        const int r = (tok0 + t * kTile + 16 * s) & ((1 << p.shift) - 1);
-        const int page = __builtin_amdgcn_readfirstlane(max(pg[s], 0));
-        const unsigned char* base = p.cache + ((int64_t)page * p.Hkv + hk) * (int64_t)kv4_block_bytes<D>(p.shift);
-        const unsigned char* vc = base + kv4_code_bytes<D>(p.shift);
-        const unsigned char* ks = vc + kv4_code_bytes<D>(p.shift);
-        const unsigned char* vs = ks + kv4_scale_bytes<D>(p.shift);
-        x.k[s] = *reinterpret_cast<const kvec*>(base + (uint32_t)((r + n) * (D / 2) + g * (D / 8)));
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          x.v[4 * s + i] = *reinterpret_cast<const vvec*>(vc + (uint32_t)((r + 4 * g + i) * (D / 2) + n * (D / 32)));
-        x.ks[s] = ks[(uint32_t)(((g * (D / 4) / 32) << p.shift) + r + n)];
-        x.vs[s] = *reinterpret_cast<const uint32_t*>(vs + (uint32_t)(((n * DL / 32) << p.shift) + r + 4 * g));
+        const int first = tok0 + t * kTile + 16 * s;
+        const int r = first & ((1 << p.shift) - 1);
+        const bool there = (unsigned)pg[s] < (unsigned)p.pages && (first >> p.shift) < p.M;
+        none |= there ? 0u : 1u << s;
+        const uint64_t base = head + (uint64_t)(uint32_t)(there ? pg[s] : 0) * page_bytes;
+        codes[s] = base + (uint32_t)(r * TL::kRow);
+        scales[s] = base + (uint32_t)r;
       }
+      const uint32_t to = ring_at + (uint32_t)(slot * TL::kBytes);
+#pragma unroll
+      for (int kv = 0; kv < 2; ++kv) {
+        const uint32_t off = copy_codes + (uint32_t)(kv * kv4_code_bytes<D>(p.shift));
+        if constexpr (D == 128) {
+#pragma unroll
+          for (int s = 0; s < 2; ++s)
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" " nt"
+                         : : "s"(to + (uint32_t)(kv * TL::kCodes + s * 1024)), "v"(off), "s"(codes[s]) : "memory", "m0");
+        } else {
+          const uint64_t at = (lane < 32 ? codes[0] : codes[1]) + off;
+          asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" " nt"
+                       : : "s"(to + (uint32_t)(kv * TL::kCodes)), "v"(at) : "memory", "m0");
+        }
+      }
+      const uint64_t at = (copy_word < 4 ? scales[0] : scales[1]) + copy_scales;
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" " nt"
+                   : : "s"(to + (uint32_t)TL::kScales), "v"(at) : "memory", "m0");
+      return none;
     };
 
-    auto compute = [&](int t, const int (&pg)[2], Raw<D>& x) __attribute__((always_inline)) {
-      const int tok = tok0 + t * kTile;
-      const bool whole = tok >= seen.lo && tok + kTile <= seen.hi && (pg[0] | pg[1]) >= 0;
-      // Scores.
-      float sc[NC][8];
+    // The wave's tiles: t0 + wave, and every kWaves-th from there.
+    const int mine = t1 > t0 + wave ? (t1 - t0 - wave + kWaves - 1) / kWaves : 0;
+    uint32_t missing = 0;           // two bits for each tile in flight, the next one's lowest
+    int far[2] = {0, 0};
+    int near[kRing][2];
+#pragma unroll
+    for (int k = 0; k < kRing; ++k) pages(t0 + wave + k * kWaves, near[k]);
+    pages(t0 + wave + kRing * kWaves, far);
+    // The loop's waits count copies alone: what was loaded above is here first.
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+#pragma unroll
+      for (int s = 0; s < KS; ++s) asm volatile("" : "+v"(q[c][s]));
+      if (ALIBI) asm volatile("" : "+v"(slope[c]));
+    }
+#pragma unroll
+    for (int k = 0; k < kRing; ++k)
+      if (k < mine) missing |= copy(t0 + wave + k * kWaves, near[k], k) << (2 * k);
+    int slot = 0;
+    for (int k = 0; k < mine; ++k) {
+      const int t = t0 + wave + k * kWaves;
+      // This tile has arrived when only those behind it are in flight.
+      const int behind = min(mine - 1 - k, kRing - 1);
+      if (behind >= 3) asm volatile("s_waitcnt vmcnt(%0)" : : "n"(3 * TL::kCopies) : "memory");
+      else if (behind == 2) asm volatile("s_waitcnt vmcnt(%0)" : : "n"(2 * TL::kCopies) : "memory");
+      else if (behind == 1) asm volatile("s_waitcnt vmcnt(%0)" : : "n"(TL::kCopies) : "memory");
+      else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      static_assert(kRing <= 4, "the cases above");
+
+      const char* tile = ring + slot * TL::kBytes;
+      uint32_t kw[2][KS], vw[8], ks[2];
+      u32x4 vs[2];
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
-        const float scale = as_float(x.ks[s] << 23);
+        if constexpr (D == 128) {
+          const u32x4 x = *reinterpret_cast<const u32x4*>(tile + read_k + s * 16 * TL::kRow);
+#pragma unroll
+          for (int i = 0; i < KS; ++i) kw[s][i] = x[i];
+        } else {
+          const u32x2 x = *reinterpret_cast<const u32x2*>(tile + read_k + s * 16 * TL::kRow);
+#pragma unroll
+          for (int i = 0; i < KS; ++i) kw[s][i] = x[i];
+        }
+        ks[s] = *reinterpret_cast<const uint8_t*>(tile + read_ks + 16 * s);
+        vs[s] = *reinterpret_cast<const u32x4*>(tile + read_vs + 16 * s);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const char* at = tile + read_v[r] + s * 16 * TL::kRow;
+          if constexpr (D == 128) vw[4 * s + r] = *reinterpret_cast<const uint32_t*>(at);
+          else vw[4 * s + r] = *reinterpret_cast<const uint16_t*>(at);
+        }
+      }
+      const uint32_t lost = missing & 3;
+      missing >>= 2;
+      if (k + kRing < mine) {
+        // The slot is free once its reads have returned.
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        missing |= copy(t + kRing * kWaves, far, slot) << (2 * (kRing - 1));
+        pages(t + (kRing + 1) * kWaves, far);
+      }
+      if (++slot == kRing) slot = 0;
+
+      const int tok = tok0 + t * kTile;
+      // Scores: element 4 s + r is token 16 s + 4 r + g of the tile.
+      float sc[NC][8], vscale[8];
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        const float scale = as_float(ks[s] << 23);
         f32x4 acc[NC];
 #pragma unroll
         for (int c = 0; c < NC; ++c) acc[c] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int st = 0; st < KS; ++st) {
-          const uint32_t word = x.k[s][st];
+          const uint32_t word = kw[s][st];
           const u32x4 a = {Fp4<T>::template cvt<0>(word, scale), Fp4<T>::template cvt<1>(word, scale),
                            Fp4<T>::template cvt<2>(word, scale), Fp4<T>::template cvt<3>(word, scale)};
 #pragma unroll
           for (int c = 0; c < NC; ++c) acc[c] = Mfma16<T>::mul(__builtin_bit_cast(vec8, a), q[c][st], acc[c]);
         }
 #pragma unroll
-        for (int c = 0; c < NC; ++c)
+        for (int r = 0; r < 4; ++r) {
+          const uint32_t word = vs[s][r];
+          vscale[4 * s + r] = as_float(__builtin_amdgcn_alignbit(word, word, scale_turn));
 #pragma unroll
-          for (int r = 0; r < 4; ++r) {
+          for (int c = 0; c < NC; ++c) {
             float v = acc[c][r] * p.c;
             if (CAP) v = soft_cap(v, p.cap_k2, p.cap_cl);
-            if (ALIBI) v = __builtin_fmaf(slope[c], (float)(tok + 16 * s + 4 * g + r - (seen.hi - 1)), v);
+            if (ALIBI) v = __builtin_fmaf(slope[c], (float)(tok + 16 * s + 4 * r + g - (seen.hi - 1)), v);
             sc[c][4 * s + r] = v;
           }
+        }
       }
-      if (!whole) {
+      if (tok < seen.lo || tok + kTile > seen.hi || lost) {
         // What is not seen: no weight, and no NaN from what its bytes hold.
 #pragma unroll
         for (int s = 0; s < 2; ++s)
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            const int key = tok + 16 * s + 4 * g + r;
-            if (key < seen.lo || key >= seen.hi || pg[s] < 0) {
+            const int key = tok + 16 * s + 4 * r + g;
+            if (key < seen.lo || key >= seen.hi || (lost >> s & 1)) {
 #pragma unroll
               for (int c = 0; c < NC; ++c) sc[c][4 * s + r] = kNegInf;
-              x.vs[s] &= ~(0xffu << (8 * r));
+              vscale[4 * s + r] = 0.f;
             }
           }
       }
@@ -306,21 +426,13 @@ __global__ __launch_bounds__(kThreads) void decode_kv4_kernel(Kv4DecodeParams p)
       }
       // O^T: byte h of a lane's dims of tokens 2 i and 2 i + 1 gives word i of
       // the operands of dims 2 h and 2 h + 1.
-      float vscale[8];
-#pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        vscale[4 * s] = as_float(x.vs[s] << 23);
-        vscale[4 * s + 1] = as_float(x.vs[s] << 15);
-        vscale[4 * s + 2] = as_float(x.vs[s] << 7);
-        vscale[4 * s + 3] = as_float(x.vs[s] >> 1);
-      }
       auto block = [&](auto byte) __attribute__((always_inline)) {
         constexpr int h = decltype(byte)::value;
         u32x4 a0, a1;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const uint32_t u = Fp4<T>::template cvt<h>(x.v[2 * i], vscale[2 * i]);
-          const uint32_t v = Fp4<T>::template cvt<h>(x.v[2 * i + 1], vscale[2 * i + 1]);
+          const uint32_t u = Fp4<T>::template cvt<h>(vw[2 * i], vscale[2 * i]);
+          const uint32_t v = Fp4<T>::template cvt<h>(vw[2 * i + 1], vscale[2 * i + 1]);
           a0[i] = __builtin_amdgcn_perm(v, u, 0x05040100u);
           a1[i] = __builtin_amdgcn_perm(v, u, 0x07060302u);
         }
@@ -336,38 +448,20 @@ __global__ __launch_bounds__(kThreads) void decode_kv4_kernel(Kv4DecodeParams p)
         block(std::integral_constant<int, 2>{});
         block(std::integral_constant<int, 3>{});
       }
-    };
-
-    // A tile ahead in registers, its pages two ahead.
-    int t = t0 + wave;
-    if (t < t1) {
-      Raw<D> x;
-      int pg[2], next_pg[2];
-      pages(t, pg);
-      pages(t + kWaves, next_pg);
-      fetch(t, pg, x);
-      for (; t < t1; t += kWaves) {
-        Raw<D> next = x;
-        int far[2];
-        pages(t + 2 * kWaves, far);
-        if (t + kWaves < t1) fetch(t + kWaves, next_pg, next);
-        compute(t, pg, x);
-        x = next;
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          pg[s] = next_pg[s];
-          next_pg[s] = far[s];
-        }
-      }
     }
 
-    // The waves' states, through LDS.  Lane (n, g) holds dims DL (4 g + r) + j of
-    // head n in element r of block j.
+    // The waves' states, through LDS, 16 columns at a time.  Lane (n, g) holds
+    // dims DL (4 g + r) + j of head n in element r of block j.
+    const bool done = t0 == 0 && t1 == seen.tiles;
+    const int64_t part = 2 * (int64_t)w + (t0 == 0 ? 1 : 0);    // the share's last row, or its first
+    if (t0 == 0 && threadIdx.x == 0)   // the shares of the row: this one to the one of its last tile
+      p.ws_rows[b * rows_b + row] = make_int2(w, done ? w : shares.of(at - u0 + units_of(seen) - 1));
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
       l[c] += __shfl_xor(l[c], 16, 64);
       l[c] += __shfl_xor(l[c], 32, 64);
-      float* to = sh_o[wave][16 * c + n];
+      __syncthreads();                 // every wave is done with its ring, or with the columns before
+      float* to = sh_o[wave][n];
 #pragma unroll
       for (int r = 0; r < 4; ++r)
 #pragma unroll
@@ -375,49 +469,47 @@ __global__ __launch_bounds__(kThreads) void decode_kv4_kernel(Kv4DecodeParams p)
           *reinterpret_cast<f32x4*>(to + DL * (4 * g + r) + j) =
               f32x4{o[c][j][r], o[c][j + 1][r], o[c][j + 2][r], o[c][j + 3][r]};
       if (g == 0) {
-        sh_m[wave][16 * c + n] = m[c];
-        sh_l[wave][16 * c + n] = l[c];
+        sh_m[wave][n] = m[c];
+        sh_l[wave][n] = l[c];
       }
-    }
-    __syncthreads();
-    const bool done = t0 == 0 && t1 == seen.tiles;
-    const int64_t part = 2 * (int64_t)w + (first ? 0 : 1);
-    for (int idx = threadIdx.x; idx < heads * (D / 4); idx += kThreads) {
-      const int h = idx / (D / 4), d = idx % (D / 4) * 4;
-      float M = kNegInf;
+      __syncthreads();
+      for (int idx = threadIdx.x; idx < min(heads - 16 * c, 16) * (D / 4); idx += kThreads) {
+        const int in = idx / (D / 4), d = idx % (D / 4) * 4, h = 16 * c + in;
+        float M = kNegInf;
 #pragma unroll
-      for (int i = 0; i < kWaves; ++i) M = fmaxf(M, sh_m[i][h]);
-      float L = 0.f;
-      f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+        for (int i = 0; i < kWaves; ++i) M = fmaxf(M, sh_m[i][in]);
+        float L = 0.f;
+        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int i = 0; i < kWaves; ++i) {
-        const float f = sh_m[i][h] == kNegInf ? 0.f : fast_exp2(sh_m[i][h] - M);
-        L = __builtin_fmaf(sh_l[i][h], f, L);
-        acc += f * *reinterpret_cast<const f32x4*>(&sh_o[i][h][d]);
-      }
-      if (done) {
-        const float r = L == 0.f ? 0.f : 1.f / L;
-        uint2 out;
-        out.x = Elem<T>::pack2(acc[0] * r, acc[1] * r);
-        out.y = Elem<T>::pack2(acc[2] * r, acc[3] * r);
-        *reinterpret_cast<uint2*>(static_cast<T*>(p.o) + ((int64_t)b * p.Hq + hq0 + h) * D + d) = out;
-      } else {
-        *reinterpret_cast<f32x4*>(p.ws_o + (part * COLS + h) * D + d) = acc;
-        if (d == 0) {
-          p.ws_m[part * COLS + h] = M;
-          p.ws_l[part * COLS + h] = L;
+        for (int i = 0; i < kWaves; ++i) {
+          const float f = sh_m[i][in] == kNegInf ? 0.f : fast_exp2(sh_m[i][in] - M);
+          L = __builtin_fmaf(sh_l[i][in], f, L);
+          acc += f * *reinterpret_cast<const f32x4*>(&sh_o[i][in][d]);
+        }
+        if (done) {
+          const float r = L == 0.f ? 0.f : 1.f / L;
+          uint2 out;
+          out.x = Elem<T>::pack2(acc[0] * r, acc[1] * r);
+          out.y = Elem<T>::pack2(acc[2] * r, acc[3] * r);
+          *reinterpret_cast<uint2*>(static_cast<T*>(p.o) + ((int64_t)b * p.Hq + hq0 + h) * D + d) = out;
+        } else {
+          *reinterpret_cast<f32x4*>(p.ws_o + (part * COLS + h) * D + d) = acc;
+          if (d == 0) {
+            p.ws_m[part * COLS + h] = M;
+            p.ws_l[part * COLS + h] = L;
+          }
         }
       }
     }
-    at += t1 - t0;
+    }
+    at += u1 - u0;
     if (at >= end) break;
-    __syncthreads();
-    t0 = 0;
+    u0 = 0;
     if (++row == rows_b) {
       row = 0;
       do {
         if (++b == p.B) return;
-        seen = seen_of(p, __builtin_amdgcn_readfirstlane(p.lens[b]));
+        seen = seen_of(p, scalar(p.lens)[b]);
       } while (seen.tiles == 0);
     }
   }
@@ -427,39 +519,53 @@ __global__ __launch_bounds__(kThreads) void decode_kv4_kernel(Kv4DecodeParams p)
 // hold a row's dims, and the lane groups take its parts in turn.
 template <int D, typename T>
 __global__ __launch_bounds__(kThreads) void decode_kv4_combine_kernel(Kv4DecodeParams p) {
-  constexpr int CH = D / 4, NG = kThreads / CH;
+  constexpr int CH = D / 4, NG = kThreads / CH, kBatch = 4;
   __shared__ float sh_m[NG], sh_l[NG];
   __shared__ f32x4 sh_o[NG][CH];
-  const int lane = threadIdx.x & 63;
   const int b = blockIdx.x / p.Hq, hq = blockIdx.x - b * p.Hq;
   const int cols = kv4_columns(p.group);
   const int hk = hq / p.group, in = hq - hk * p.group, ht = in / cols, h = in - ht * cols;
-  const int rows_b = p.Hkv * p.head_tiles;
-  int before;
-  const Shares shares = shares_of(p, row_tiles(p, lane, b, before) * rows_b);
-  const int tiles = seen_of(p, __builtin_amdgcn_readfirstlane(p.lens[b])).tiles;
   const int ch = threadIdx.x % CH, g = threadIdx.x / CH;
+  const int2 span = p.ws_rows[(b * p.Hkv + hk) * p.head_tiles + ht];   // (of a row without tiles: not looked at)
   T* out = static_cast<T*>(p.o) + (int64_t)blockIdx.x * D + 4 * ch;
-  if (tiles == 0) {
+  if (p.lens[b] <= 0) {
     if (g == 0) *reinterpret_cast<uint2*>(out) = make_uint2(0u, 0u);
     return;
   }
-  const int from = before * rows_b + (hk * p.head_tiles + ht) * tiles;
-  const int w0 = shares.of(from), w1 = shares.of(from + tiles - 1);
-  if (w0 == w1) return;                       // the split kernel has written it
+  if (span.x == span.y) return;               // the split kernel has written it
 
   float M = kNegInf, L = 0.f;
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-  for (int w = w0 + g; w <= w1; w += NG) {
-    // A share's first row is its part 0, its last (if another) part 1.
-    const int64_t at = (2 * (int64_t)w + (w == w0 && shares.begin(w) < from ? 1 : 0)) * cols + h;
-    const float m = p.ws_m[at], l = p.ws_l[at];
-    const f32x4 v = *reinterpret_cast<const f32x4*>(p.ws_o + at * D + 4 * ch);
-    const float mn = fmaxf(M, m);
-    const float f = M == kNegInf ? 0.f : fast_exp2(M - mn), e = m == kNegInf ? 0.f : fast_exp2(m - mn);
-    L = L * f + l * e;
-    acc = acc * f + v * e;
+  for (int w0 = span.x + g; w0 <= span.y; w0 += NG * kBatch) {
+    float m[kBatch], l[kBatch];
+    f32x4 v[kBatch];
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {   // past the last part: that part again, left out below
+      const int w = min(w0 + u * NG, span.y);
+      const int64_t at = (2 * (int64_t)w + (w == span.x ? 1 : 0)) * cols + h;
+      m[u] = p.ws_m[at];
+      l[u] = p.ws_l[at];
+      v[u] = *reinterpret_cast<const f32x4*>(p.ws_o + at * D + 4 * ch);
+    }
+    // (Not loaded under the conditions below, one after another.)
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) asm volatile("" : "+v"(v[u]), "+v"(l[u]), "+v"(m[u]));
+    float mn = M;
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) mn = fmaxf(mn, m[u]);
+    if (mn == kNegInf) continue;         // parts of missing pages only
+    const float a = M == kNegInf ? 0.f : fast_exp2(M - mn);
+    L *= a;
+    acc *= a;
     M = mn;
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+      if (w0 + u * NG <= span.y) {
+        const float e = m[u] == kNegInf ? 0.f : fast_exp2(m[u] - mn);
+        L = __builtin_fmaf(e, l[u], L);
+        acc += e * v[u];
+      }
+    }
   }
   sh_o[g][ch] = acc;
   if (ch == 0) {
@@ -508,11 +614,11 @@ hipError_t launch_cols(const Kv4DecodeParams& p, int64_t blocks, hipStream_t str
 
 }  // namespace
 
-int kv4_shares(int group, int cus) { return cus * (kv4_columns(group) == 16 ? 4 : 2); }
+int kv4_shares(int D, int group, int cus) { return cus * per_unit(D, kv4_columns(group)); }
 
 hipError_t launch_decode_kv4(const Kv4DecodeParams& p, hipStream_t stream) {
   // No more workgroups than the longest contexts that the tables hold could use.
-  const int64_t most = (((int64_t)p.M << p.shift) / kTile + 2) * p.B * p.Hkv * p.head_tiles;
+  const int64_t most = (((int64_t)p.M << p.shift) / kTile + 2 + kStart) * p.B * p.Hkv * p.head_tiles;
   const int64_t blocks = std::min<int64_t>(p.shares, (most + kLeast - 1) / kLeast);
   if (p.D == 64) return p.bf16 ? launch_cols<64, __bf16>(p, blocks, stream) : launch_cols<64, _Float16>(p, blocks, stream);
   return p.bf16 ? launch_cols<128, __bf16>(p, blocks, stream) : launch_cols<128, _Float16>(p, blocks, stream);

@@ -2,6 +2,7 @@
 #pragma once
 
 #include <hip/hip_runtime_api.h>
+#include <hip/hip_vector_types.h>
 #include <stddef.h>
 #include <stdint.h>
 
@@ -196,6 +197,7 @@ struct Kv4DecodeParams {
   float* ws_o;          // [2 * shares, columns, D]
   float* ws_m;          // [2 * shares, columns], log2 units
   float* ws_l;
+  int2* ws_rows;        // [B, Hkv, head_tiles]: a row's first and last share
   int B, Hq, Hkv, D, group;
   int pages, shift, M;
   int window;           // 0 for none
@@ -208,7 +210,7 @@ struct Kv4DecodeParams {
 // Query heads that one workgroup serves: 16 or 32 matrix columns.
 constexpr int kv4_columns(int group) { return group <= 16 ? 16 : 32; }
 // Workgroups of the split kernel on a device of `cus` compute units.
-int kv4_shares(int group, int cus);
+int kv4_shares(int D, int group, int cus);
 hipError_t launch_decode_kv4(const Kv4DecodeParams& p, hipStream_t stream);
 
 // Compute units of the current device, 256 if it cannot be queried (attn_api.cpp).

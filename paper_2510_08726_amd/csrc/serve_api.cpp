@@ -174,8 +174,9 @@ int kv4_load(const void* cache, const int* table, const int* starts, const int* 
 
 size_t attn_decode_kv4_workspace_bytes(int B, int Hq, int Hkv, int D) {
   if (B < 1 || Hq < 1 || Hkv < 1 || Hq % Hkv || (D != 64 && D != 128)) return 0;
-  const size_t parts = 2 * (size_t)attn::kv4_shares(Hq / Hkv, attn::compute_units());
-  const size_t bytes = parts * attn::kv4_columns(Hq / Hkv) * (size_t)(D + 2) * sizeof(float);
+  const size_t parts = 2 * (size_t)attn::kv4_shares(D, Hq / Hkv, attn::compute_units());
+  const size_t cols = attn::kv4_columns(Hq / Hkv), tiles = (Hq / Hkv + cols - 1) / cols;
+  const size_t bytes = parts * cols * (size_t)(D + 2) * sizeof(float) + (size_t)B * Hkv * tiles * sizeof(int2);
   return (bytes + 255) & ~(size_t)255;
 }
 
@@ -192,9 +193,9 @@ int attn_decode_kv4(const void* Q, const void* cache, const int* table, const in
   if (misaligned(Q) || misaligned(cache) || misaligned(O)) return ATTN_ERR_SHAPE;
   const int group = Hq / Hkv, cols = attn::kv4_columns(group), tiles = (group + cols - 1) / cols;
   const int64_t rows = (int64_t)B * Hkv * tiles;
-  // The list of all tiles is counted in 32 bits.
+  // The list of all tiles is counted in 32 bits, and so is a page of all heads.
   if ((int64_t)B * Hq > kMaxInt || ((int64_t)max_pages << shift) > kMaxTokens ||
-      rows > kMaxInt / ((((int64_t)max_pages << shift) + 31) / 32 + 1))
+      (int64_t)(kv4_page_bytes(page, D) * Hkv) > kMaxInt || rows > kMaxInt / ((((int64_t)max_pages << shift) + 31) / 32 + 8))
     return ATTN_ERR_SHAPE;
   if (workspace_bytes < attn_decode_kv4_workspace_bytes(B, Hq, Hkv, D) || misaligned(workspace))
     return ATTN_ERR_WORKSPACE;
@@ -205,11 +206,12 @@ int attn_decode_kv4(const void* Q, const void* cache, const int* table, const in
   p.pages = pages; p.shift = shift; p.M = max_pages;
   p.window = window;
   p.head_tiles = tiles;
-  p.shares = attn::kv4_shares(group, attn::compute_units());
+  p.shares = attn::kv4_shares(D, group, attn::compute_units());
   const size_t parts = 2 * (size_t)p.shares * cols;
   p.ws_o = static_cast<float*>(workspace);
   p.ws_m = p.ws_o + parts * D;
   p.ws_l = p.ws_m + parts;
+  p.ws_rows = reinterpret_cast<int2*>(p.ws_l + parts);
   p.bf16 = dtype == ATTN_BF16;
   p.c = scale * kLog2e;
   p.cap_k2 = softcap > 0.f ? 2.f / softcap : 0.f;
