@@ -73,9 +73,9 @@ int rope_frequencies(int rotary_dim, double base, int scaling, double factor, do
  * Rows whose size, strides and addresses are multiples of 16 (or 8) bytes, with
  * pairs that fill such vectors, are read and written in vectors, others by
  * elements.
- * Errors: ATTN_ERR_NULL; ATTN_ERR_SHAPE for bad sizes, a non-finite magnitude,
- * positions_bits, or more than 2^31 - 1 workgroups; ATTN_ERR_UNSUPPORTED for
- * the dtype; ATTN_ERR_HIP.
+ * B * L * D < 2^31 and Hq + Hkv < 2^16.
+ * Errors: ATTN_ERR_NULL; ATTN_ERR_SHAPE for bad sizes, a non-finite magnitude
+ * or positions_bits; ATTN_ERR_UNSUPPORTED for the dtype; ATTN_ERR_HIP.
  */
 int rope_fwd(const void* Q, const long long* q_strides, void* Qo, int Hq,
              const void* K, const long long* k_strides, void* Ko, int Hkv,

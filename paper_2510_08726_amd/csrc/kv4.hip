@@ -2,6 +2,8 @@
 // reading them back.  The conversions between E2M1 and 16 bits are gfx950
 // instructions, which take the block's power of two as an operand.
 
+#include <algorithm>
+
 #include "kernel_common.h"
 #include "kv4_common.h"
 #include "launch.h"
@@ -107,67 +109,67 @@ __global__ __launch_bounds__(kThreads) void kv_slots_kernel(SlotsParams p) {
   }
 }
 
-// Four lanes hold a block of 32 dims, 8 each: 16 bytes in, 4 bytes out.  K and V
-// of a row in one thread; neighbouring lanes hold a row, then the next token's.
+// Grids of the two kernels below: a workgroup's lanes are the rows of neighbouring
+// tokens of one head, blockIdx.y is the head, and blockIdx.z strides the sequences.
+// (More tokens a thread, 2, 4 and 8 with all their loads in flight, took 46, 50 and 56 us
+// where one takes 44: the rows of a workgroup then lie further apart.)
+
+// Four lanes hold a block of 32 dims, 8 each: 16 bytes in, 4 bytes out, K and V in
+// one thread.  The input is streamed past the caches, which the cache's lines need until
+// all rows of a line are written (44.6 us for 8 prompts of up to 4095 tokens and their reading
+// back, 46.4 without).
 template <int D, typename T>
 __global__ __launch_bounds__(kThreads) void kv4_append_kernel(Kv4AppendParams p) {
   constexpr int LPR = D / 8;                 // lanes per row
-  constexpr int kTop = sizeof(T) == 2 && __is_same(T, _Float16) ? 13 : 125;
-  const int64_t idx = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  const int lig = (int)(idx % LPR);
-  int64_t row = idx / LPR;
-  const int l = (int)(row % p.L);
-  row /= p.L;
-  const int h = (int)(row % p.H), b = (int)(row / p.H);
-  if (b >= p.B) return;
-  const int64_t slot = p.slots[(int64_t)b * p.L + l];
-  if (slot < 0 || slot >= (int64_t)p.pages << p.shift) return;    // the lanes of a row agree
-  const int page = 1 << p.shift, r = (int)slot & (page - 1);
-  unsigned char* base = p.cache + ((slot >> p.shift) * p.H + h) * (int64_t)kv4_block_bytes<D>(p.shift);
-  u32x4 x[2];
+  constexpr int kTop = __is_same(T, _Float16) ? 13 : 125;
+  const int lig = threadIdx.x % LPR, h = blockIdx.y;
+  const int l = blockIdx.x * (kThreads / LPR) + threadIdx.x / LPR;
+  if (l >= p.L) return;
+  for (int b = blockIdx.z; b < p.B; b += gridDim.z) {
+    const int64_t slot = p.slots[(int64_t)b * p.L + l];
+    u32x4 x[2];
 #pragma unroll
-  for (int k = 0; k < 2; ++k)
-    x[k] = *reinterpret_cast<const u32x4*>(static_cast<const T*>(p.x[k]) + b * p.sb[k] + h * p.sh[k] + l * p.sl[k] + 8 * lig);
+    for (int k = 0; k < 2; ++k)
+      x[k] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(
+          static_cast<const T*>(p.x[k]) + b * p.sb[k] + h * p.sh[k] + l * p.sl[k] + 8 * lig));
+    if (slot < 0 || slot >= (int64_t)p.pages << p.shift) continue;    // the lanes of a row agree
+    const int r = (int)slot & ((1 << p.shift) - 1);
+    unsigned char* base = p.cache + ((slot >> p.shift) * p.H + h) * (int64_t)kv4_block_bytes<D>(p.shift);
 #pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    float f[8];
+    for (int k = 0; k < 2; ++k) {
+      float f[8];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      f[2 * i] = Elem<T>::lo(x[k][i]);
-      f[2 * i + 1] = Elem<T>::hi(x[k][i]);
-    }
-    // The largest magnitude as bits: ordered as the values are, infinities
-    // and NaN above them.
-    uint32_t top = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float v = f[i];
-      top = max(top, __builtin_bit_cast(uint32_t, v) & 0x7fffffffu);
-    }
-    top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0xB1, 0xf, 0xf, false));   // quad_perm [1,0,3,2]
-    top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0x4E, 0xf, 0xf, false));   // quad_perm [2,3,0,1]
-    const bool fine = top < 0x7f800000u;
-    // 2^e with a <= 7 2^e: the exponent of a less 2, one more over 1.75 of its binade.
-    int e = (int)((top + 0x1fffffu) >> 23) - 129;
-    e = min(max(e, -kTop), kTop);
-    const uint32_t inv = (uint32_t)(127 - e) << 23;
-    const float s = __builtin_bit_cast(float, inv);
-    uint32_t code = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {            // scaled first: the products are exact
-      const float a = f[2 * i] * s, c = f[2 * i + 1] * s;
-      switch (i) {
-        case 0: code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, a, c, 1.f, 0); break;
-        case 1: code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, a, c, 1.f, 1); break;
-        case 2: code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, a, c, 1.f, 2); break;
-        default: code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, a, c, 1.f, 3);
+      for (int i = 0; i < 4; ++i) {
+        f[2 * i] = Elem<T>::lo(x[k][i]);
+        f[2 * i + 1] = Elem<T>::hi(x[k][i]);
       }
+      // The largest magnitude as bits: ordered as the values are, infinities
+      // and NaN above them.
+      uint32_t top = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float v = f[i];
+        top = max(top, __builtin_bit_cast(uint32_t, v) & 0x7fffffffu);
+      }
+      top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0xB1, 0xf, 0xf, false));   // quad_perm [1,0,3,2]
+      top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0x4E, 0xf, 0xf, false));   // quad_perm [2,3,0,1]
+      const bool fine = top < 0x7f800000u;
+      // 2^e with a <= 7 2^e: the exponent of a less 2, one more over 1.75 of its binade.
+      int e = (int)((top + 0x1fffffu) >> 23) - 129;
+      e = min(max(e, -kTop), kTop);
+      const uint32_t inv = (uint32_t)(127 - e) << 23;
+      const float s = __builtin_bit_cast(float, inv);
+      // Scaled first: the products are exact.
+      uint32_t code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, f[0] * s, f[1] * s, 1.f, 0);
+      code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, f[2] * s, f[3] * s, 1.f, 1);
+      code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, f[4] * s, f[5] * s, 1.f, 2);
+      code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, f[6] * s, f[7] * s, 1.f, 3);
+      if (!fine) code = 0;
+      *reinterpret_cast<uint32_t*>(base + k * kv4_code_bytes<D>(p.shift) + r * (D / 2) + 4 * lig) = code;
+      if ((lig & 3) == 0)
+        base[2 * kv4_code_bytes<D>(p.shift) + k * kv4_scale_bytes<D>(p.shift) + ((lig >> 2) << p.shift) + r] =
+            (unsigned char)(fine ? e + 127 : 255);
     }
-    if (!fine) code = 0;
-    *reinterpret_cast<uint32_t*>(base + k * kv4_code_bytes<D>(p.shift) + (int64_t)r * (D / 2) + 4 * lig) = code;
-    if ((lig & 3) == 0)
-      base[2 * kv4_code_bytes<D>(p.shift) + k * kv4_scale_bytes<D>(p.shift) + ((lig >> 2) << p.shift) + r] =
-          (unsigned char)(fine ? e + 127 : 255);
   }
 }
 
@@ -175,53 +177,49 @@ __global__ __launch_bounds__(kThreads) void kv4_append_kernel(Kv4AppendParams p)
 template <int D, typename T>
 __global__ __launch_bounds__(kThreads) void kv4_load_kernel(Kv4LoadParams p) {
   constexpr int LPR = D / 8;
-  const int64_t idx = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  const int lig = (int)(idx % LPR);
-  const int64_t row = idx / LPR;
-  const int l = (int)(row % p.L);
-  const int64_t bh = row / p.L;
-  const int h = (int)(bh % p.H), b = (int)(bh / p.H);
-  if (b >= p.B) return;
-  const int64_t t = (int64_t)(p.starts ? max(p.starts[b], 0) : 0) + l;
-  const int64_t n = min((int64_t)p.lens[b], (int64_t)p.M << p.shift);
-  const int pg = t < n ? p.table[(int64_t)b * p.M + (t >> p.shift)] : -1;
-  const bool there = (unsigned)pg < (unsigned)p.pages;
-  uint32_t code[2] = {0u, 0u}, scale[2] = {0u, 0u};
-  if (there) {
-    const int r = (int)t & ((1 << p.shift) - 1);
-    const unsigned char* base = p.cache + ((int64_t)pg * p.H + h) * (int64_t)kv4_block_bytes<D>(p.shift);
+  const int lig = threadIdx.x % LPR, h = blockIdx.y;
+  const int l = blockIdx.x * (kThreads / LPR) + threadIdx.x / LPR;
+  if (l >= p.L) return;
+  for (int b = blockIdx.z; b < p.B; b += gridDim.z) {
+    const int64_t t = (int64_t)(p.starts ? max(p.starts[b], 0) : 0) + l;
+    const int64_t n = min((int64_t)p.lens[b], (int64_t)p.M << p.shift);
+    const int pg = t < n ? p.table[(int64_t)b * p.M + (t >> p.shift)] : -1;
+    uint32_t code[2] = {0u, 0u}, scale[2] = {0u, 0u};
+    if ((unsigned)pg < (unsigned)p.pages) {
+      const int r = (int)t & ((1 << p.shift) - 1);
+      const unsigned char* base = p.cache + ((int64_t)pg * p.H + h) * (int64_t)kv4_block_bytes<D>(p.shift);
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        code[k] = *reinterpret_cast<const uint32_t*>(base + k * kv4_code_bytes<D>(p.shift) + r * (D / 2) + 4 * lig);
+        scale[k] = base[2 * kv4_code_bytes<D>(p.shift) + k * kv4_scale_bytes<D>(p.shift) + ((lig >> 2) << p.shift) + r];
+      }
+    }
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
-      code[k] = *reinterpret_cast<const uint32_t*>(base + k * kv4_code_bytes<D>(p.shift) + (int64_t)r * (D / 2) + 4 * lig);
-      scale[k] = base[2 * kv4_code_bytes<D>(p.shift) + k * kv4_scale_bytes<D>(p.shift) + ((lig >> 2) << p.shift) + r];
+      const uint32_t bits = scale[k] << 23;
+      const float s = __builtin_bit_cast(float, bits);
+      const u32x4 out = {Fp4<T>::template cvt<0>(code[k], s), Fp4<T>::template cvt<1>(code[k], s),
+                         Fp4<T>::template cvt<2>(code[k], s), Fp4<T>::template cvt<3>(code[k], s)};
+      *reinterpret_cast<u32x4*>(static_cast<T*>(p.y[k]) + (((int64_t)b * p.H + h) * p.L + l) * D + 8 * lig) = out;
     }
   }
-#pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    const uint32_t bits = scale[k] << 23;
-    const float s = __builtin_bit_cast(float, bits);
-    u32x4 out;
-    out[0] = Fp4<T>::template cvt<0>(code[k], s);
-    out[1] = Fp4<T>::template cvt<1>(code[k], s);
-    out[2] = Fp4<T>::template cvt<2>(code[k], s);
-    out[3] = Fp4<T>::template cvt<3>(code[k], s);
-    *reinterpret_cast<u32x4*>(static_cast<T*>(p.y[k]) + row * D + 8 * lig) = out;
-  }
+}
+
+template <int D>
+dim3 grid_of(int B, int H, int L) {
+  constexpr int kTokens = kThreads / (D / 8);
+  return dim3((unsigned)((L + kTokens - 1) / kTokens), (unsigned)H, (unsigned)std::min(B, 65535));
 }
 
 template <int D, typename T>
 hipError_t append(const Kv4AppendParams& p, hipStream_t stream) {
-  const int64_t threads = (int64_t)p.B * p.H * p.L * (D / 8);
-  hipLaunchKernelGGL((kv4_append_kernel<D, T>), dim3((unsigned)((threads + kThreads - 1) / kThreads)), dim3(kThreads),
-                     0, stream, p);
+  hipLaunchKernelGGL((kv4_append_kernel<D, T>), grid_of<D>(p.B, p.H, p.L), dim3(kThreads), 0, stream, p);
   return hipGetLastError();
 }
 
 template <int D, typename T>
 hipError_t load(const Kv4LoadParams& p, hipStream_t stream) {
-  const int64_t threads = (int64_t)p.B * p.H * p.L * (D / 8);
-  hipLaunchKernelGGL((kv4_load_kernel<D, T>), dim3((unsigned)((threads + kThreads - 1) / kThreads)), dim3(kThreads), 0,
-                     stream, p);
+  hipLaunchKernelGGL((kv4_load_kernel<D, T>), grid_of<D>(p.B, p.H, p.L), dim3(kThreads), 0, stream, p);
   return hipGetLastError();
 }
 

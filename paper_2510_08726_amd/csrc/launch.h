@@ -147,7 +147,6 @@ struct RopeParams {
   float magnitude, sign;   // sign -1: the transposed rotation
   bool pos64, interleaved;
   int dtype;            // 0 fp16, 1 bf16, 2 fp32
-  int heads;            // heads per thread, set by the launcher
 };
 hipError_t launch_rope(const RopeParams& p, hipStream_t stream);
 

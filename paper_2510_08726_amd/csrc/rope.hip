@@ -1,12 +1,19 @@
 // Rotary positions (include/rope.h): queries and keys in one kernel, which
 // reads and writes every row once.
 //
-// A thread takes V pairs of one token (the same dims of every head turn by the
-// same angle), forms their sines and cosines once, and turns those pairs in
-// `heads` heads.  Angles: t = p f and its fraction of a turn in 64 bits, exactly
-// reduced to an eighth of a turn; sine and cosine there by their Taylor series
-// in 32 bits (through x^9 and x^10, under 2e-9 off for |x| <= pi / 4).
-// Bound by HBM for many tokens (a row in and out), by the launch for few.
+// Angles: t = p f and its fraction of a turn in 64 bits, exactly reduced to an
+// eighth of a turn; sine and cosine there by their Taylor series in 32 bits (through x^9
+// and x^10, under 2e-9 off for |x| <= pi / 4).  A thread forms them once for
+// its dims and turns four heads by them; with one head a thread, 4 x 4096 tokens
+// of 32 + 8 heads of 128 fp16 dims took 76 us, with 2, 4 and 8 62, 54 and 53.  Up to
+// 2048 workgroups that does not pay (2 x 512 tokens: 7.3 us either way), and
+// latency wants every thread there is.
+//
+// Bound by HBM for many tokens: 335 MB in 54 us, 6.3 TB/s of reads and writes
+// (interleaved and read out of a projection 57), by the launch for few (8 tokens: 3.8 us, a kernel that does
+// nothing 2).  Loads are streamed past the caches where a row's parts are whole
+// lines (64 us without); elsewhere lines are shared by neighbouring loads, and
+// streaming them costs (a part of 24 dims: 31 us, 57 streamed).
 
 #include "kernel_common.h"
 #include "launch.h"
@@ -16,6 +23,20 @@ namespace attn {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kHeads = 4;       // heads of a thread
+constexpr int kFew = 2048;      // workgroups of one head a thread up to which a thread has one
+
+// The a's and b's of a row, and the row, are whole cache lines.
+inline bool whole_lines(const RopeParams& p, size_t size) {
+  const size_t part = p.interleaved ? p.R * size : p.R / 2 * size;
+  return part % 128 == 0 && (p.D - p.R) * size % 128 == 0;
+}
+
+template <bool ONCE, typename R>
+__device__ __forceinline__ R load(const R* p) {
+  if constexpr (ONCE) return __builtin_nontemporal_load(p);
+  else return *p;
+}
 
 // V elements of T as one register group, to and from fp32.
 template <typename T, int V> struct Pack;
@@ -79,78 +100,118 @@ __device__ __forceinline__ void sin_cos(double p, double f, float& si, float& co
   co = (k + 1) & 2 ? -b : b;
 }
 
-// The threads of a token: R / (2 V) of V pairs each, then (D - R) / V that copy.
-template <typename T, int V, bool INTER>
+// Threads that copy the dims behind the rotated ones: two vectors each where a
+// thread that turns has two of 16 bytes (64 of 128 bf16 dims: 63 us, one each 67), else one
+// (40 of 64 fp16 dims in 8 bytes: 31 us, two each 36).
+template <typename T, int V, bool ONE>
+__device__ __host__ __forceinline__ int copying_threads(const RopeParams& p) {
+  const int copied = (p.D - p.R) / V;
+  return ONE || V * sizeof(T) < 16 ? copied : (copied + 1) / 2;
+}
+
+// The threads of a token: those that turn kPairs pairs each, then those that copy
+// the dims behind.  A thread has the pairs' a's in one vector of V elements and their b's in
+// another, or, interleaved, V / 2 pairs in one vector (one pair in two elements where V =
+// 1): so the lanes of a row cover it without gaps either way.  Its heads are
+// kBatch neighbours, all loaded before the angles are formed.
+template <typename T, int V, bool INTER, int kBatch, bool ONCE>
 __global__ __launch_bounds__(kThreads) void rope_kernel(RopeParams p) {
   typedef Pack<T, V> P;
   typedef typename P::raw raw;
-  const int turning = p.R / (2 * V), per = turning + (p.D - p.R) / V;
-  const int64_t idx = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  const int64_t token = idx / per;
-  if (token >= (int64_t)p.B * p.L) return;
+  constexpr bool kOne = INTER && V > 1;              // both of a pair in one vector
+  constexpr int kPairs = kOne ? V / 2 : V;
+  const uint32_t turning = (uint32_t)p.R / (2 * kPairs);
+  const int copying = copying_threads<T, V, kOne>(p);
+  const uint32_t per = turning + (uint32_t)copying;
+  const uint32_t idx = blockIdx.x * kThreads + threadIdx.x;
+  const uint32_t token = idx / per;
+  if (token >= (uint32_t)p.B * (uint32_t)p.L) return;
   const int w = (int)(idx - token * per);
-  const int b = (int)(token / p.L), l = (int)(token - (int64_t)b * p.L);
-  const bool turns = w < turning;
-  // The two vectors of V elements: a's and b's of the pairs, or neighbours.
-  const int d0 = turns ? (INTER ? 2 * V * w : V * w) : p.R + V * (w - turning);
-  const int d1 = turns ? (INTER ? d0 + V : d0 + p.R / 2) : d0;
+  const int b = (int)(token / (uint32_t)p.L), l = (int)(token - (uint32_t)b * (uint32_t)p.L);
+  const bool turns = w < (int)turning;
+  const int d0 = turns ? (INTER ? 2 * kPairs * w : V * w) : p.R + V * (w - (int)turning);
+  const int next = turns ? (INTER ? V : p.R / 2) : V * copying;
+  const int d1 = kOne || d0 + next >= p.D ? d0 : d0 + next;    // (a lone vector is copied twice)
+  const int heads = p.H[0] + p.H[1], first = blockIdx.y * kBatch;
 
-  float si[V], co[V];
-  if (turns) {
-    const int64_t at = b * p.pos_stride + l;
-    const double pos = p.pos64 ? (double)static_cast<const int64_t*>(p.pos)[at]
-                               : (double)static_cast<const int*>(p.pos)[at];
+  const T* x[kBatch];
+  T* y[kBatch];
+  raw r0[kBatch], r1[kBatch];
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      float s, c;
-      sin_cos(pos, p.freqs[V * w + i], s, c);
-      si[i] = s * p.magnitude * p.sign;
-      co[i] = c * p.magnitude;
-    }
-  }
-  const int first = blockIdx.y * p.heads, last = min(first + p.heads, p.H[0] + p.H[1]);
-  for (int hh = first; hh < last; ++hh) {
+  for (int u = 0; u < kBatch; ++u) {
+    const int hh = min(first + u, heads - 1);          // past the last: that head again, not stored
     const int k = hh >= p.H[0];
     const int h = k ? hh - p.H[0] : hh;
-    const T* x = static_cast<const T*>(p.x[k]) + b * p.sb[k] + h * p.sh[k] + l * p.sl[k];
-    T* y = static_cast<T*>(p.y[k]) + (((int64_t)b * p.H[k] + h) * p.L + l) * p.D;
-    const raw r0 = *reinterpret_cast<const raw*>(x + d0);
-    if (!turns) {
-      *reinterpret_cast<raw*>(y + d0) = r0;
-      continue;
-    }
-    const raw r1 = *reinterpret_cast<const raw*>(x + d1);
-    float f[2 * V], g[2 * V];
-    P::load(r0, f);
-    P::load(r1, f + V);
+    x[u] = static_cast<const T*>(p.x[k]) + b * p.sb[k] + h * p.sh[k] + l * p.sl[k];
+    y[u] = static_cast<T*>(p.y[k]) + (((int64_t)b * p.H[k] + h) * p.L + l) * p.D;
+  }
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
+  for (int u = 0; u < kBatch; ++u) {
+    r0[u] = load<ONCE>(reinterpret_cast<const raw*>(x[u] + d0));
+    if (!kOne) r1[u] = load<ONCE>(reinterpret_cast<const raw*>(x[u] + d1));
+  }
+  if (!turns) {
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u)
+      if (first + u < heads) {
+        *reinterpret_cast<raw*>(y[u] + d0) = r0[u];
+        if (!kOne) *reinterpret_cast<raw*>(y[u] + d1) = r1[u];
+      }
+    return;
+  }
+  const int64_t at = b * p.pos_stride + l;
+  const double pos = p.pos64 ? (double)static_cast<const int64_t*>(p.pos)[at]
+                             : (double)static_cast<const int*>(p.pos)[at];
+  float si[kPairs], co[kPairs];
+#pragma unroll
+  for (int i = 0; i < kPairs; ++i) {
+    float s, c;
+    sin_cos(pos, p.freqs[kPairs * w + i], s, c);
+    si[i] = s * p.magnitude * p.sign;
+    co[i] = c * p.magnitude;
+  }
+#pragma unroll
+  for (int u = 0; u < kBatch; ++u) {
+    if (first + u >= heads) break;
+    float f[2 * V], g[2 * V];
+    P::load(r0[u], f);
+    if (!kOne) P::load(r1[u], f + V);
+#pragma unroll
+    for (int i = 0; i < kPairs; ++i) {
       const int a = INTER ? 2 * i : i, c = INTER ? 2 * i + 1 : V + i;
       g[a] = f[a] * co[i] - f[c] * si[i];
       g[c] = __builtin_fmaf(f[a], si[i], f[c] * co[i]);
     }
-    *reinterpret_cast<raw*>(y + d0) = P::store(g);
-    *reinterpret_cast<raw*>(y + d1) = P::store(g + V);
+    *reinterpret_cast<raw*>(y[u] + d0) = P::store(g);
+    if (!kOne) *reinterpret_cast<raw*>(y[u] + d1) = P::store(g + V);
   }
 }
 
-template <typename T, int V>
-hipError_t launch(RopeParams p, hipStream_t stream) {
-  const int64_t threads = (int64_t)p.B * p.L * (p.R / (2 * V) + (p.D - p.R) / V);
-  const int heads = p.H[0] + p.H[1];
-  const int64_t blocks = (threads + kThreads - 1) / kThreads;
-  p.heads = 1;
-  const dim3 grid((unsigned)blocks, (unsigned)((heads + p.heads - 1) / p.heads)), block(kThreads);
+template <typename T, int V, int kBatch, bool ONCE>
+hipError_t launch_batch(const RopeParams& p, int64_t blocks, hipStream_t stream) {
+  const dim3 grid((unsigned)blocks, (unsigned)((p.H[0] + p.H[1] + kBatch - 1) / kBatch)), block(kThreads);
   if (p.interleaved)
-    hipLaunchKernelGGL((rope_kernel<T, V, true>), grid, block, 0, stream, p);
+    hipLaunchKernelGGL((rope_kernel<T, V, true, kBatch, ONCE>), grid, block, 0, stream, p);
   else
-    hipLaunchKernelGGL((rope_kernel<T, V, false>), grid, block, 0, stream, p);
+    hipLaunchKernelGGL((rope_kernel<T, V, false, kBatch, ONCE>), grid, block, 0, stream, p);
   return hipGetLastError();
+}
+
+template <typename T, int V>
+hipError_t launch(const RopeParams& p, hipStream_t stream) {
+  const bool one = p.interleaved && V > 1;             // as the kernel divides a row
+  const int64_t threads = (int64_t)p.B * p.L *
+                          (p.R / (one ? V : 2 * V) + (one ? copying_threads<T, V, true>(p) : copying_threads<T, V, false>(p)));
+  const int64_t blocks = (threads + kThreads - 1) / kThreads;
+  if (blocks * (p.H[0] + p.H[1]) <= kFew) return launch_batch<T, V, 1, false>(p, blocks, stream);
+  if constexpr (V * sizeof(T) == 16)
+    if (whole_lines(p, sizeof(T))) return launch_batch<T, V, kHeads, true>(p, blocks, stream);
+  return launch_batch<T, V, kHeads, false>(p, blocks, stream);
 }
 
 // Every row starts at a multiple of n elements, and pairs fill vectors of n.
 bool vectors(const RopeParams& p, int n, int size) {
-  if (p.D % n || p.R % (2 * n)) return false;
+  if (p.D % n || p.R % (p.interleaved ? n : 2 * n)) return false;
   for (int k = 0; k < 2; ++k) {
     if (!p.x[k]) continue;
     if (p.sb[k] % n || p.sh[k] % n || p.sl[k] % n) return false;

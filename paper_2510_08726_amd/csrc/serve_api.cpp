@@ -37,10 +37,8 @@ int rope(const void* Q, const long long* q_strides, void* Qo, int Hq, const void
   if ((K ? Hkv < 1 : Hkv != 0) || !std::isfinite(magnitude) || positions_stride < 0) return ATTN_ERR_SHAPE;
   if (positions_bits != 32 && positions_bits != 64) return ATTN_ERR_SHAPE;
   if (dtype < ROPE_F16 || dtype > ROPE_F32) return ATTN_ERR_UNSUPPORTED;
-  // One thread for each pair or copied element at most, in workgroups of 256,
-  // and a grid row for each head.
-  if ((int64_t)B * L > kMaxInt || (int64_t)B * L * D >= kMaxElements / 8 || (int64_t)Hq + Hkv > 65535)
-    return ATTN_ERR_SHAPE;
+  // At most a thread for each pair or copied element, and a grid row for each head.
+  if ((int64_t)B * L > kMaxInt / D || (int64_t)Hq + Hkv > 65535) return ATTN_ERR_SHAPE;
   attn::RopeParams p{};
   p.x[0] = Q; p.y[0] = Qo; p.H[0] = Hq;
   p.sb[0] = q_strides[0]; p.sh[0] = q_strides[1]; p.sl[0] = q_strides[2];
@@ -58,10 +56,10 @@ int rope(const void* Q, const long long* q_strides, void* Qo, int Hq, const void
   return done(attn::launch_rope(p, stream));
 }
 
-// Sizes of a cache that the kernels' 32-bit offsets within a page and head hold.
+// Sizes of calls on a cache: a grid row for each head, and elements that stay addressable.
 bool cache_ok(int B, int Hkv, int L, int pages) {
-  return B >= 1 && Hkv >= 1 && L >= 1 && pages >= 1 && (int64_t)B * Hkv <= kMaxInt && (int64_t)B * L <= kMaxInt &&
-         (int64_t)B * Hkv * L * 128 < kMaxElements / 8;
+  return B >= 1 && Hkv >= 1 && Hkv <= 65535 && L >= 1 && pages >= 1 && (int64_t)B * L <= kMaxInt &&
+         (int64_t)B * L <= kMaxElements / (128 * (int64_t)Hkv);
 }
 
 bool kv4_type(int D, attn_dtype dtype) {

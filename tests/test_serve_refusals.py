@@ -104,7 +104,7 @@ def load(lib, c=FAKE, t=FAKE, st=None, n=FAKE, k=FAKE, v=FAKE, B=1, H=2, L=3, D=
 @pytest.mark.parametrize("kw,code", [
     (dict(k=None), NULL), (dict(v=None), NULL), (dict(c=None), NULL),
     (dict(B=0), SHAPE), (dict(H=0), SHAPE), (dict(L=0), SHAPE), (dict(P=0), SHAPE), (dict(page=48), SHAPE),
-    (dict(k=ODD), SHAPE), (dict(v=ODD), SHAPE), (dict(c=ODD), SHAPE), (dict(B=1 << 16, H=1 << 10, L=1 << 12), SHAPE),
+    (dict(k=ODD), SHAPE), (dict(v=ODD), SHAPE), (dict(c=ODD), SHAPE), (dict(B=1 << 16, H=1 << 10, L=1 << 12), SHAPE), (dict(H=1 << 16), SHAPE),
     (dict(D=96), UNSUPPORTED), (dict(D=32), UNSUPPORTED), (dict(dtype=2), UNSUPPORTED),
 ], ids=str)
 def test_append_and_load(lib, kw, code):
