@@ -140,10 +140,11 @@ __global__ __launch_bounds__(kThreads, per_unit(D, 16 * NC)) void decode_kv4_ker
   // The waves' rings; at the end of a row their states, 16 columns at a time.
   constexpr int kRing = ring_tiles(D, COLS);
   constexpr int kLds = kWaves * kRing * TL::kBytes;
-  static_assert(kWaves * 16 * (D + 2) * 4 <= kLds, "the states fit into the rings");
+  constexpr int kPad = D + 4;         // floats of a state's row: 16 lanes write 16 bytes to 16 rows without conflicts
+  static_assert(kWaves * 16 * (kPad + 2) * 4 <= kLds, "the states fit into the rings");
   __shared__ __attribute__((aligned(1024))) char lds[kLds];
-  float (*sh_o)[16][D] = reinterpret_cast<float (*)[16][D]>(lds);
-  float (*sh_m)[16] = reinterpret_cast<float (*)[16]>(lds + kWaves * 16 * D * 4);
+  float (*sh_o)[16][kPad] = reinterpret_cast<float (*)[16][kPad]>(lds);
+  float (*sh_m)[16] = reinterpret_cast<float (*)[16]>(lds + kWaves * 16 * kPad * 4);
   float (*sh_l)[16] = sh_m + kWaves;
 
   const int lane = threadIdx.x & 63;
@@ -461,16 +462,18 @@ __global__ __launch_bounds__(kThreads, per_unit(D, 16 * NC)) void decode_kv4_ker
       l[c] += __shfl_xor(l[c], 16, 64);
       l[c] += __shfl_xor(l[c], 32, 64);
       __syncthreads();                 // every wave is done with its ring, or with the columns before
-      float* to = sh_o[wave][n];
+      if (16 * c + n < heads) {
+        float* to = sh_o[wave][n];
 #pragma unroll
-      for (int r = 0; r < 4; ++r)
+        for (int r = 0; r < 4; ++r)
 #pragma unroll
-        for (int j = 0; j < DL; j += 4)
-          *reinterpret_cast<f32x4*>(to + DL * (4 * g + r) + j) =
-              f32x4{o[c][j][r], o[c][j + 1][r], o[c][j + 2][r], o[c][j + 3][r]};
-      if (g == 0) {
-        sh_m[wave][n] = m[c];
-        sh_l[wave][n] = l[c];
+          for (int j = 0; j < DL; j += 4)
+            *reinterpret_cast<f32x4*>(to + DL * (4 * g + r) + j) =
+                f32x4{o[c][j][r], o[c][j + 1][r], o[c][j + 2][r], o[c][j + 3][r]};
+        if (g == 0) {
+          sh_m[wave][n] = m[c];
+          sh_l[wave][n] = l[c];
+        }
       }
       __syncthreads();
       for (int idx = threadIdx.x; idx < min(heads - 16 * c, 16) * (D / 4); idx += kThreads) {
