@@ -250,10 +250,13 @@ __global__ __launch_bounds__(kThreads, per_unit(D, 16 * NC)) void decode_kv4_ker
       for (int j = 0; j < DL; ++j) o[c][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
 
-    // What the table has for a tile's halves (past its end: the last entry again).
+    // What the table has for a tile's halves (past its end: the last entry again);
+    // in pages of 32 tokens or more both lie in one.
+    const bool paired = (1 << p.shift) >= kTile;
     auto pages = [&](int t, int (&pg)[2]) __attribute__((always_inline)) {
 #pragma unroll
-      for (int s = 0; s < 2; ++s) pg[s] = table[min((tok0 + t * kTile + 16 * s) >> p.shift, p.M - 1)];
+      for (int s = 0; s < 2; ++s)
+        pg[s] = s && paired ? pg[0] : table[min((tok0 + t * kTile + 16 * s) >> p.shift, p.M - 1)];
     };
     // Start the copies of a tile into a slot of the ring.  A half without a page
     // is read from page 0, and masked: returns bit s for it.
@@ -262,6 +265,12 @@ __global__ __launch_bounds__(kThreads, per_unit(D, 16 * NC)) void decode_kv4_ker
       uint32_t none = 0;
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
+        if (s && paired) {
+          none |= none << 1;
+          codes[1] = codes[0] + 16 * TL::kRow;
+          scales[1] = scales[0] + 16;
+          break;
+        }
         const int first = tok0 + t * kTile + 16 * s;
         const int r = first & ((1 << p.shift) - 1);
         const bool there = (unsigned)pg[s] < (unsigned)p.pages && (first >> p.shift) < p.M;
@@ -286,7 +295,7 @@ __global__ __launch_bounds__(kThreads, per_unit(D, 16 * NC)) void decode_kv4_ker
         }
       }
       const uint64_t at = (copy_word < 4 ? scales[0] : scales[1]) + copy_scales;
-      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" " nt"
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off"
                    : : "s"(to + (uint32_t)TL::kScales), "v"(at) : "memory", "m0");
       return none;
     };
@@ -355,7 +364,9 @@ __global__ __launch_bounds__(kThreads, per_unit(D, 16 * NC)) void decode_kv4_ker
 
       const int tok = tok0 + t * kTile;
       // Scores: element 4 s + r is token 16 s + 4 r + g of the tile.
-      float sc[NC][8], vscale[8];
+      float sc[NC][8], vscale[8], far_bias[NC];
+#pragma unroll
+      for (int c = 0; c < NC; ++c) far_bias[c] = ALIBI ? slope[c] * (float)(tok + g - (seen.hi - 1)) : 0.f;
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
         const float scale = as_float(ks[s] << 23);
@@ -376,10 +387,11 @@ __global__ __launch_bounds__(kThreads, per_unit(D, 16 * NC)) void decode_kv4_ker
           vscale[4 * s + r] = as_float(__builtin_amdgcn_alignbit(word, word, scale_turn));
 #pragma unroll
           for (int c = 0; c < NC; ++c) {
-            float v = acc[c][r] * p.c;
-            if (CAP) v = soft_cap(v, p.cap_k2, p.cap_cl);
-            if (ALIBI) v = __builtin_fmaf(slope[c], (float)(tok + 16 * s + 4 * r + g - (seen.hi - 1)), v);
-            sc[c][4 * s + r] = v;
+            // The bias from the tile's and the token's part of the distance, one
+            // rounding each.
+            const float bias = ALIBI ? __builtin_fmaf(slope[c], (float)(16 * s + 4 * r), far_bias[c]) : 0.f;
+            if (CAP) sc[c][4 * s + r] = soft_cap(acc[c][r] * p.c, p.cap_k2, p.cap_cl, p.cap_cl + bias);
+            else sc[c][4 * s + r] = ALIBI ? __builtin_fmaf(acc[c][r], p.c, bias) : acc[c][r] * p.c;
           }
         }
       }
