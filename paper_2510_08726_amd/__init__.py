@@ -579,9 +579,9 @@ def _allocate(shape, like, stream, dtype=None):
 
 
 def _overlaps(a, b):
-    """Whether two contiguous tensors share memory."""
-    return (a.data_ptr() < b.data_ptr() + b.numel() * b.element_size()
-            and b.data_ptr() < a.data_ptr() + a.numel() * a.element_size())
+    """Whether the memory that two tensors span has a common part."""
+    end = lambda t: t.data_ptr() + (1 + sum((n - 1) * s for n, s in zip(t.shape, t.stride()))) * t.element_size()  # noqa: E731
+    return bool(a.numel() and b.numel()) and a.data_ptr() < end(b) and b.data_ptr() < end(a)
 
 
 def _rope(bwd, q, k, positions, freqs, q_out, k_out, interleaved, magnitude, stream):
@@ -612,9 +612,14 @@ def _rope(bwd, q, k, positions, freqs, q_out, k_out, interleaved, magnitude, str
             _same_device(q, **{name + "_out": o})
             _require(o.shape == x.shape and o.dtype == x.dtype and o.is_contiguous(),
                      f"{name}_out must be a contiguous tensor shaped like {name}")
-            _require(o.data_ptr() != x.data_ptr() or x.is_contiguous(),
-                     f"{name}_out may be {name} itself only if that is contiguous")
         outs.append(o)
+    for name, x, o, others in (("q", q, outs[0], (k, outs[1])), ("k", k, outs[1], (q, outs[0]))):
+        if o is not None:
+            others = [t for t in others if t is not None]
+            if not (x.is_contiguous() and o.data_ptr() == x.data_ptr()):
+                others.append(x)
+            _require(not any(_overlaps(o, t) for t in others),
+                     f"{name}_out may share memory with nothing, but be {name} itself if that is contiguous")
     lib = load_library()
     fn = lib.rope_bwd if bwd else lib.rope_fwd
     with torch.cuda.device(q.device):

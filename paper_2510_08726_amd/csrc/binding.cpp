@@ -346,9 +346,15 @@ bool output(PyObject* obj, const at::Tensor& like, at::ScalarType type, at::IntA
   return t != nullptr;
 }
 
+// Whether the memory that two tensors span has a common part.
 bool overlap(const at::Tensor& a, const at::Tensor& b) {
-  const char *p = static_cast<const char*>(a.data_ptr()), *q = static_cast<const char*>(b.data_ptr());
-  return p < q + b.nbytes() && q < p + a.nbytes();
+  if (!a.numel() || !b.numel()) return false;
+  const auto end = [](const at::Tensor& t) {
+    int64_t n = 1;
+    for (int64_t i = 0; i < t.dim(); ++i) n += (t.size(i) - 1) * t.stride(i);
+    return static_cast<const char*>(t.data_ptr()) + n * t.element_size();
+  };
+  return a.data_ptr() < end(b) && b.data_ptr() < end(a);
 }
 
 // A tuple of outputs, or the error status.
@@ -396,8 +402,13 @@ PyObject* py_rope(PyObject*, PyObject* const* x, Py_ssize_t n) {
   if (freqs->size(0) > INT_MAX / 2) return none();
   at::Tensor qo, ko;
   if (!output(x[4], *q, type, q->sizes(), qo) || (k && !output(x[5], *q, type, k->sizes(), ko))) return none();
-  if (qo.data_ptr() == q->data_ptr() && !q->is_contiguous()) return none();
-  if (k && ko.data_ptr() == k->data_ptr() && !k->is_contiguous()) return none();
+  // An output that is given shares memory with nothing, or is its input.
+  const auto apart = [&](const at::Tensor& o, const at::Tensor& x, const at::Tensor* other, const at::Tensor& out) {
+    return ((o.data_ptr() == x.data_ptr() && x.is_contiguous()) || !overlap(o, x)) && (!other || !overlap(o, *other)) &&
+           (!out.defined() || !overlap(o, out));
+  };
+  if (x[4] != Py_None && !apart(qo, *q, k, ko)) return none();
+  if (x[5] != Py_None && !apart(ko, *k, q, qo)) return none();
   const void *qp = q->data_ptr(), *kp = k ? k->data_ptr() : nullptr, *pp = pos->data_ptr();
   void *qop = qo.data_ptr(), *kop = k ? ko.data_ptr() : nullptr;
   const double* fp = static_cast<const double*>(freqs->data_ptr());

@@ -37,7 +37,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
 constexpr int kTile = 32;          // tokens
-constexpr int kStart = 8;          // units of a row's start and end
+constexpr int kStart = kKv4RowStart;   // units of a row's start and end
 constexpr int kLeast = 8;          // units a share holds at least
 
 // How many workgroups share a compute unit, and the tiles that a wave has in LDS
@@ -541,7 +541,9 @@ __global__ __launch_bounds__(kThreads) void decode_kv4_combine_kernel(Kv4DecodeP
   const int cols = kv4_columns(p.group);
   const int hk = hq / p.group, in = hq - hk * p.group, ht = in / cols, h = in - ht * cols;
   const int ch = threadIdx.x % CH, g = threadIdx.x / CH;
-  const int2 span = p.ws_rows[(b * p.Hkv + hk) * p.head_tiles + ht];   // (of a row without tiles: not looked at)
+  int2 span = p.ws_rows[(b * p.Hkv + hk) * p.head_tiles + ht];   // (of a row without tiles: not looked at)
+  span.x = min(max(span.x, 0), p.shares - 1);                    // (and in bounds whatever it says)
+  span.y = min(max(span.y, 0), p.shares - 1);
   T* out = static_cast<T*>(p.o) + (int64_t)blockIdx.x * D + 4 * ch;
   if (p.lens[b] <= 0) {
     if (g == 0) *reinterpret_cast<uint2*>(out) = make_uint2(0u, 0u);
@@ -568,14 +570,13 @@ __global__ __launch_bounds__(kThreads) void decode_kv4_combine_kernel(Kv4DecodeP
     float mn = M;
 #pragma unroll
     for (int u = 0; u < kBatch; ++u) mn = fmaxf(mn, m[u]);
-    if (mn == kNegInf) continue;         // parts of missing pages only
     const float a = M == kNegInf ? 0.f : fast_exp2(M - mn);
     L *= a;
     acc *= a;
     M = mn;
 #pragma unroll
     for (int u = 0; u < kBatch; ++u) {
-      if (w0 + u * NG <= span.y) {
+      if (w0 + u * NG <= span.y) {       // (weight 0 where m is -inf: a NaN there stays one)
         const float e = m[u] == kNegInf ? 0.f : fast_exp2(m[u] - mn);
         L = __builtin_fmaf(e, l[u], L);
         acc += e * v[u];

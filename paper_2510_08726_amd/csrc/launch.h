@@ -206,6 +206,8 @@ struct Kv4DecodeParams {
   float c;              // scale * log2(e)
   float cap_k2, cap_cl; // as DecodeParams
 };
+// What a row of the list of tiles counts beside them.
+constexpr int kKv4RowStart = 8;
 // Query heads that one workgroup serves: 16 or 32 matrix columns.
 constexpr int kv4_columns(int group) { return group <= 16 ? 16 : 32; }
 // Workgroups of the split kernel on a device of `cus` compute units.

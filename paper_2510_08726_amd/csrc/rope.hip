@@ -83,8 +83,10 @@ template <> struct Pack<float, 4> {
   static __device__ __forceinline__ raw store(const float* f) { return raw{f[0], f[1], f[2], f[3]}; }
 };
 
-// Sine and cosine of p * f radians.
+// Sine and cosine of p * f radians.  (No products are contracted but those
+// written as such: every kernel then gives the same bits.)
 __device__ __forceinline__ void sin_cos(double p, double f, float& si, float& co) {
+#pragma clang fp contract(off)
   double t = p * f * 0.15915494309189535;      // turns: 1 / (2 pi)
   t = 4.0 * (t - __builtin_rint(t));           // quarters of a turn, -2 .. 2
   const double q = __builtin_rint(t);
@@ -179,7 +181,7 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeParams p) {
 #pragma unroll
     for (int i = 0; i < kPairs; ++i) {
       const int a = INTER ? 2 * i : i, c = INTER ? 2 * i + 1 : V + i;
-      g[a] = f[a] * co[i] - f[c] * si[i];
+      g[a] = __builtin_fmaf(f[a], co[i], -(f[c] * si[i]));
       g[c] = __builtin_fmaf(f[a], si[i], f[c] * co[i]);
     }
     *reinterpret_cast<raw*>(y[u] + d0) = P::store(g);

@@ -193,7 +193,7 @@ int attn_decode_kv4(const void* Q, const void* cache, const int* table, const in
   const int64_t rows = (int64_t)B * Hkv * tiles;
   // The list of all tiles is counted in 32 bits, and so is a page of all heads.
   if ((int64_t)B * Hq > kMaxInt || ((int64_t)max_pages << shift) > kMaxTokens ||
-      (int64_t)(kv4_page_bytes(page, D) * Hkv) > kMaxInt || rows > kMaxInt / ((((int64_t)max_pages << shift) + 31) / 32 + 8))
+      (int64_t)(kv4_page_bytes(page, D) * Hkv) > kMaxInt || rows > kMaxInt / ((((int64_t)max_pages << shift) + 31) / 32 + attn::kKv4RowStart))
     return ATTN_ERR_SHAPE;
   if (workspace_bytes < attn_decode_kv4_workspace_bytes(B, Hq, Hkv, D) || misaligned(workspace))
     return ATTN_ERR_WORKSPACE;

@@ -141,6 +141,19 @@ def test_nan_reaches_the_rows_that_see_it(dtype, D):
     assert not o.isnan().any()
 
 
+def test_a_share_of_nan_alone_is_not_left_out():
+    """All keys of 300 tokens in the middle are NaN: so whole shares have no maximum."""
+    lens, page, D = [3000], 64, 128
+    cache, table, _, _ = _cache(lens, 1, D, "bf16", page, 21)
+    q, = random_tensors([(1, 2, 1, D)], "bf16", 22, device="cuda")
+    x = torch.full((1, 1, 300, D), float("nan"), dtype=torch.bfloat16, device="cuda")
+    at = 1000 + np.arange(300)
+    pa.kv4_append(x, torch.zeros_like(x), cache, torch.tensor((table[0, at // page] * page + at % page)[None], device="cuda"))
+    assert pa.attn_decode_kv4(q, cache, _i32(table), _i32(lens)).isnan().all()
+    assert not pa.attn_decode_kv4(q, cache, _i32(table), _i32([1000])).isnan().any()
+    assert not pa.attn_decode_kv4(q, cache, _i32(table), _i32(lens), window=1700).isnan().any()
+
+
 def test_offsets_past_32_bits():
     """Pages behind the first 4 GB of a cache."""
     page, D, Hkv = 256, 128, 8

@@ -72,6 +72,25 @@ def test_rope(dtype, interleaved, D, R, layout):
                 _check(o, t, pos, freqs, interleaved, np.float32(1.1), bwd, (dtype, D, R, layout, B, L, bwd))
 
 
+@pytest.mark.parametrize("D,R", [(128, 128), (128, 64), (64, 24), (40, 20)])
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("interleaved", [False, True], ids=["half", "interleaved"])
+def test_many_tokens_are_turned_like_few(dtype, interleaved, D, R):
+    """Enough rows that a thread takes several heads (a number that its four do not divide,
+    keys behind queries): the same bits as call by call on a few tokens."""
+    L, f = 2050, pa.rope_frequencies(R, device="cuda")
+    q, k = (_views(2, H, L, D, DT[dtype], 40 + H, "projection") for H in (25, 6))
+    pos = torch.randint(0, 100000, (2, L), dtype=torch.int32, device="cuda")
+    whole = pa.rope_fwd(q, k, pos, f, interleaved=interleaved)
+    for lo in range(0, L, 410):
+        some = pa.rope_fwd(q[:, :, lo:lo + 410], k[:, :, lo:lo + 410], pos[:, lo:lo + 410].contiguous(), f,
+                           interleaved=interleaved)
+        one = pa.rope_fwd(q[:, :1, lo:lo + 3], None, pos[:, lo:lo + 3].contiguous(), f, interleaved=interleaved)[0]
+        for a, b in zip(whole, some):
+            assert torch.equal(a[:, :, lo:lo + 410], b)
+        assert torch.equal(whole[0][:, :1, lo:lo + 3], one)
+
+
 def test_far_positions_and_their_types():
     freqs = serve.frequencies(128, 10000.0)
     f = torch.tensor(freqs, device="cuda")
@@ -149,6 +168,7 @@ def test_refusals():
     q, k = random_tensors([(2, 4, 3, 64), (2, 2, 3, 64)], "f16", 7, device="cuda")
     f, pos = pa.rope_frequencies(64, device="cuda"), torch.zeros(2, 3, dtype=torch.int32, device="cuda")
     t = q.transpose(1, 2).contiguous().transpose(1, 2)
+    x = torch.zeros(q.numel() + 1, dtype=q.dtype, device="cuda")
     bad = [lambda: pa.rope_fwd(q.cpu(), k, pos, f), lambda: pa.rope_fwd(q.double(), None, pos, f),
            lambda: pa.rope_fwd(q, k.float(), pos, f), lambda: pa.rope_fwd(q, k[:1], pos, f),
            lambda: pa.rope_fwd(q, k[:, :, :2], pos, f), lambda: pa.rope_fwd(q, k, pos.float(), f),
@@ -158,6 +178,9 @@ def test_refusals():
            lambda: pa.rope_fwd(q[0], None, pos, f), lambda: pa.rope_fwd(q.transpose(2, 3), None, pos, f),
            lambda: pa.rope_fwd(q, None, pos, f, k_out=k), lambda: pa.rope_fwd(q, k, pos, f, q[:1]),
            lambda: pa.rope_fwd(q, k, pos, f, q.float()), lambda: pa.rope_fwd(t, None, pos, f, t),
+           lambda: pa.rope_fwd(x[:-1].view_as(q), None, pos, f, x[1:].view_as(q)),
+           lambda: pa.rope_fwd(q, k, pos, f, x[:q.numel()].view_as(q), x[:k.numel()].view_as(k)),
+           lambda: pa.rope_fwd(q, q, pos, f, q), lambda: pa.rope_fwd(q, k, pos, f, k_out=q[:, :2].contiguous()[:, :1]),
            lambda: pa.rope_fwd(q, k, pos, f, magnitude=float("inf")),
            lambda: pa.rope_fwd(q, k, pos, torch.cat((f, f)).contiguous()),
            lambda: pa.rope_fwd(q[:, :, :0], None, pos[:, :0].contiguous(), f)]
