@@ -177,7 +177,7 @@ def build(verbose=False):
     link([HIPCC, "-shared", "-fPIC", f"--offload-arch={ARCH}", *objs], LIB)
     import torch
     link(["g++", "-shared", os.path.join(OBJDIR, "binding.o"), "-L", PKG, "-lattn",
-          "-L", os.path.join(os.path.dirname(torch.__file__), "lib"), "-lc10", "-lc10_hip", "-ltorch_cpu",
+          "-L", os.path.join(os.path.dirname(torch.__file__), "lib"), "-lc10", "-lc10_hip", "-ltorch_cpu", "-ltorch_hip",
           "-ltorch_python", "-Wl,-rpath,$ORIGIN"], BINDING)
     return LIB
 

@@ -20,6 +20,7 @@
 #include <utility>
 
 #include <ATen/ATen.h>
+#include <ATen/hip/EmptyTensor.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
@@ -335,10 +336,16 @@ const at::Tensor* rows(PyObject* obj, long long (&strides)[3]) {
   return t;
 }
 
+// A new contiguous tensor on the current device, from PyTorch's allocator: what
+// at::empty makes, without its dispatch (0.5 us each against 0.75).
+at::Tensor fresh(at::IntArrayRef shape, at::ScalarType type, const at::Tensor& like) {
+  return at::detail::empty_cuda(shape, type, like.device(), std::nullopt);
+}
+
 // The given output of that type and shape, or a new one; false if the given one is not plain.
 bool output(PyObject* obj, const at::Tensor& like, at::ScalarType type, at::IntArrayRef shape, at::Tensor& out) {
   if (obj == Py_None) {
-    out = at::empty(shape, like.options().dtype(type));
+    out = fresh(shape, type, like);
     return true;
   }
   const at::Tensor* t = here(obj, type, shape);
@@ -551,7 +558,7 @@ PyObject* py_attn_decode_kv4(PyObject*, PyObject* const* x, Py_ssize_t n) {
     ws = *t;
   } else {
     const size_t need = attn_decode_kv4_workspace_bytes((int)B, Hq, (int)cache->size(1), D);
-    ws = at::empty({(int64_t)std::max<size_t>(need, 16)}, q->options().dtype(at::kByte));
+    ws = fresh({(int64_t)std::max<size_t>(need, 16)}, at::kByte, *q);
   }
   const void *qp = q->data_ptr(), *cp = cache->data_ptr();
   const int *tp = static_cast<const int*>(table->data_ptr()), *lp = static_cast<const int*>(lens->data_ptr());

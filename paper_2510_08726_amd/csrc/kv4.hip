@@ -57,8 +57,8 @@ __device__ __forceinline__ Need need_of(const SlotsParams& p, int b) {
 // the scan of its own), and writes each item's slot; the item in a new page's
 // first row writes the page into the table.  No workgroup waits for another: each reads the
 // lengths before its own, which the caches hold.  Latency bound: three dependent
-// reads (lengths, page, and the table's or the list's) and two barriers, 2.8 us for 64 requests of one token;
-// 256 requests of up to 2048 tokens write 6.3 MB in 4.9.
+// reads (lengths, page, and the table's or the list's) and two barriers, 2.2 us for 64 requests of one token;
+// 256 requests of up to 2048 tokens write 6.3 MB in 4.9 us.
 constexpr int kItems = 512;
 
 __global__ __launch_bounds__(kThreads) void kv_slots_kernel(SlotsParams p) {
