@@ -179,7 +179,9 @@ __global__ __launch_bounds__(kThreads) void kv4_append_kernel(Kv4AppendParams p)
   }
 }
 
-// 8 dims a lane: 4 bytes of codes and a scale byte in, 16 bytes out.
+// 8 dims a lane: 4 bytes of codes and a scale byte in, 16 bytes out.  The stores are
+// ordinary ones, since attention reads K and V next: 30000 tokens, 36 us, and a piece of 64
+// queries take 81 us together, 92 with streamed stores (the load alone 35).
 template <int D, typename T>
 __global__ __launch_bounds__(kThreads) void kv4_load_kernel(Kv4LoadParams p) {
   constexpr int LPR = D / 8;

@@ -4,16 +4,17 @@
 // Angles: t = p f and its fraction of a turn in 64 bits, exactly reduced to an
 // eighth of a turn; sine and cosine there by their Taylor series in 32 bits (through x^9
 // and x^10, under 2e-9 off for |x| <= pi / 4).  A thread forms them once for
-// its dims and turns four heads by them; with one head a thread, 4 x 4096 tokens
-// of 32 + 8 heads of 128 fp16 dims took 76 us, with 2, 4 and 8 62, 54 and 53.  Up to
-// 2048 workgroups that does not pay (2 x 512 tokens: 7.3 us either way), and
-// latency wants every thread there is.
+// its dims and turns four heads by them: 4 x 4096 tokens of 32 + 8 heads of 128 bf16 dims
+// take 76 us with one head a thread, 61 with 2, 56 with 4 and 57 with 8.  Up to 2048
+// workgroups that does not pay (2 x 512 tokens: 7.5 us either way), and latency wants
+// every thread there is.
 //
-// Bound by HBM for many tokens: 335 MB in 54 us, 6.3 TB/s of reads and writes
-// (interleaved and read out of a projection 57), by the launch for few (8 tokens: 3.8 us, a kernel that does
-// nothing 2).  Loads are streamed past the caches where a row's parts are whole
-// lines (64 us without); elsewhere lines are shared by neighbouring loads, and
-// streaming them costs (a part of 24 dims: 31 us, 57 streamed).
+// Bound by HBM for many tokens: 335 MB in and out in 56 us, 6.0 TB/s (interleaved
+// pairs out of a projection's [B, L, H, D] 61), by the launch for few (8 tokens: 3.8 us, a
+// kernel that does nothing 2).  Calls with 64 MB of outputs or more, which leave the
+// caches before anybody reads them, are streamed past them: 60 us without, and
+// fp32 74 against 66 (at 67 MB the same, 26.5).  Not where neighbouring loads share
+// lines, which then are fetched again (nearly twice the time for a part of 24 dims).
 
 #include "kernel_common.h"
 #include "launch.h"
@@ -26,16 +27,24 @@ constexpr int kThreads = 256;
 constexpr int kHeads = 4;       // heads of a thread
 constexpr int kFew = 2048;      // workgroups of one head a thread up to which a thread has one
 
-// The a's and b's of a row, and the row, are whole cache lines.
-inline bool whole_lines(const RopeParams& p, size_t size) {
-  const size_t part = p.interleaved ? p.R * size : p.R / 2 * size;
-  return part % 128 == 0 && (p.D - p.R) * size % 128 == 0;
+constexpr int64_t kStream = int64_t(64) << 20;   // bytes of outputs from which a call is streamed
+
+// Whether a call is read and written past the caches: one whose outputs
+// leave them before they are read again, and whose rows' parts are whole lines.
+inline bool streamed(const RopeParams& p, int64_t size) {
+  const int64_t part = p.interleaved ? p.R * size : p.R / 2 * size;
+  return part % 128 == 0 && (p.D - p.R) * size % 128 == 0 && (int64_t)p.B * p.L * (p.H[0] + p.H[1]) * p.D * size >= kStream;
 }
 
 template <bool ONCE, typename R>
 __device__ __forceinline__ R load(const R* p) {
   if constexpr (ONCE) return __builtin_nontemporal_load(p);
   else return *p;
+}
+template <bool ONCE, typename R>
+__device__ __forceinline__ void store(R* p, const R& v) {
+  if constexpr (ONCE) __builtin_nontemporal_store(v, p);
+  else *p = v;
 }
 
 // V elements of T as one register group, to and from fp32.
@@ -102,13 +111,12 @@ __device__ __forceinline__ void sin_cos(double p, double f, float& si, float& co
   co = (k + 1) & 2 ? -b : b;
 }
 
-// Threads that copy the dims behind the rotated ones: two vectors each where a
-// thread that turns has two of 16 bytes (64 of 128 bf16 dims: 63 us, one each 67), else one
-// (40 of 64 fp16 dims in 8 bytes: 31 us, two each 36).
-template <typename T, int V, bool ONE>
+// Threads that copy the dims behind the rotated ones: as many vectors each as a
+// thread that turns has, one or two.
+template <int V, bool ONE>
 __device__ __host__ __forceinline__ int copying_threads(const RopeParams& p) {
   const int copied = (p.D - p.R) / V;
-  return ONE || V * sizeof(T) < 16 ? copied : (copied + 1) / 2;
+  return ONE ? copied : (copied + 1) / 2;
 }
 
 // The threads of a token: those that turn kPairs pairs each, then those that copy
@@ -123,7 +131,7 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeParams p) {
   constexpr bool kOne = INTER && V > 1;              // both of a pair in one vector
   constexpr int kPairs = kOne ? V / 2 : V;
   const uint32_t turning = (uint32_t)p.R / (2 * kPairs);
-  const int copying = copying_threads<T, V, kOne>(p);
+  const int copying = copying_threads<V, kOne>(p);
   const uint32_t per = turning + (uint32_t)copying;
   const uint32_t idx = blockIdx.x * kThreads + threadIdx.x;
   const uint32_t token = idx / per;
@@ -156,8 +164,8 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeParams p) {
 #pragma unroll
     for (int u = 0; u < kBatch; ++u)
       if (first + u < heads) {
-        *reinterpret_cast<raw*>(y[u] + d0) = r0[u];
-        if (!kOne) *reinterpret_cast<raw*>(y[u] + d1) = r1[u];
+        store<ONCE>(reinterpret_cast<raw*>(y[u] + d0), r0[u]);
+        if (!kOne) store<ONCE>(reinterpret_cast<raw*>(y[u] + d1), r1[u]);
       }
     return;
   }
@@ -184,8 +192,8 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeParams p) {
       g[a] = __builtin_fmaf(f[a], co[i], -(f[c] * si[i]));
       g[c] = __builtin_fmaf(f[a], si[i], f[c] * co[i]);
     }
-    *reinterpret_cast<raw*>(y[u] + d0) = P::store(g);
-    if (!kOne) *reinterpret_cast<raw*>(y[u] + d1) = P::store(g + V);
+    store<ONCE>(reinterpret_cast<raw*>(y[u] + d0), P::store(g));
+    if (!kOne) store<ONCE>(reinterpret_cast<raw*>(y[u] + d1), P::store(g + V));
   }
 }
 
@@ -203,11 +211,11 @@ template <typename T, int V>
 hipError_t launch(const RopeParams& p, hipStream_t stream) {
   const bool one = p.interleaved && V > 1;             // as the kernel divides a row
   const int64_t threads = (int64_t)p.B * p.L *
-                          (p.R / (one ? V : 2 * V) + (one ? copying_threads<T, V, true>(p) : copying_threads<T, V, false>(p)));
+                          (p.R / (one ? V : 2 * V) + (one ? copying_threads<V, true>(p) : copying_threads<V, false>(p)));
   const int64_t blocks = (threads + kThreads - 1) / kThreads;
   if (blocks * (p.H[0] + p.H[1]) <= kFew) return launch_batch<T, V, 1, false>(p, blocks, stream);
   if constexpr (V * sizeof(T) == 16)
-    if (whole_lines(p, sizeof(T))) return launch_batch<T, V, kHeads, true>(p, blocks, stream);
+    if (streamed(p, sizeof(T))) return launch_batch<T, V, kHeads, true>(p, blocks, stream);
   return launch_batch<T, V, kHeads, false>(p, blocks, stream);
 }
 

@@ -78,7 +78,7 @@ def test_rope(dtype, interleaved, D, R, layout):
 def test_many_tokens_are_turned_like_few(dtype, interleaved, D, R):
     """Enough rows that a thread takes several heads (a number that its four do not divide,
     keys behind queries): the same bits as call by call on a few tokens."""
-    L, f = 2050, pa.rope_frequencies(R, device="cuda")
+    L, f = 4300, pa.rope_frequencies(R, device="cuda")      # 68 MB of 16-bit outputs at D = 128: streamed
     q, k = (_views(2, H, L, D, DT[dtype], 40 + H, "projection") for H in (25, 6))
     pos = torch.randint(0, 100000, (2, L), dtype=torch.int32, device="cuda")
     whole = pa.rope_fwd(q, k, pos, f, interleaved=interleaved)
