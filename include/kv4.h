@@ -10,7 +10,8 @@
  * itself is held as 6), limited to -13 .. 13 for fp16 and -125 .. 125 for bf16, so
  * that every value held is a normal number of the type, or zero; each element is held
  * as the nearest code (ties to the even code, magnitudes over 6 as 6).  A block
- * with an infinity or NaN is held as 32 NaN.
+ * with an infinity or NaN is held as 32 NaN.  (Read in fp16, a block that was
+ * written from larger or smaller bf16 values gives infinities or zeros.)
  *
  * Layout.  cache is [pages, Hkv, kv4_page_bytes(page, D)] bytes, contiguous,
  * 16-byte aligned.  `page` is the tokens of a page, a power of two from 16 to

@@ -49,6 +49,8 @@ DEVICE = ["-x", "hip", f"--offload-arch={ARCH}", "-Xclang", "-target-feature", "
 # values produced by inline assembly compiles to a plain v_max instead of
 # canonicalising both inputs first.  The prefill device assembly is kept
 # (-save-temps) for the ISA hazard check in the tests.
+# The 4-bit decode's accumulators stay in VGPRs (-amdgpu-mfma-vgpr-form): the
+# softmax repairs them there.
 UNITS = [(f"prefill{k}", "prefill.hip", ["-fno-honor-nans", f"-DATTN_PREFILL_SHARD={k}", "-save-temps"])
          for k in range(4)] + [("decode", "decode.hip", ["-save-temps"]), ("peaks", "peaks.hip", ["-save-temps"]),
             ("norms", "norms.hip", ["-save-temps"]),
