@@ -110,8 +110,8 @@ const char* attn_status_string(int status) {
   switch (status) {
     case ATTN_OK: return "ATTN_OK: success";
     case ATTN_ERR_NULL: return "ATTN_ERR_NULL: a required pointer is NULL";
-    case ATTN_ERR_SHAPE: return "ATTN_ERR_SHAPE: invalid sizes (need B,Hq,Hkv,Lq,Lk >= 1, Hq % Hkv == 0, num_splits >= 0, window >= 0, finite scale, finite softcap >= 0)";
-    case ATTN_ERR_UNSUPPORTED: return "ATTN_ERR_UNSUPPORTED: head dim must be 64 or 128 and dtype ATTN_F16 or ATTN_BF16; softcap and window need the causal mask, softcap excludes ALiBi";
+    case ATTN_ERR_SHAPE: return "ATTN_ERR_SHAPE: invalid sizes (need B,Hq,Hkv,Lq,Lk >= 1, Hq % Hkv == 0, num_splits >= 0, window >= 0, finite scale, finite softcap >= 0; rope.h and kv4.h say what their calls need)";
+    case ATTN_ERR_UNSUPPORTED: return "ATTN_ERR_UNSUPPORTED: head dim must be 64 or 128 and dtype ATTN_F16 or ATTN_BF16; softcap and window need the causal mask, softcap excludes ALiBi (rope.h: dtype ROPE_F16, ROPE_BF16 or ROPE_F32)";
     case ATTN_ERR_WORKSPACE: return "ATTN_ERR_WORKSPACE: workspace too small or not 16-byte aligned (attn_decode_noalloc: the split count needs more than its 16 MiB static workspace)";
     case ATTN_ERR_HIP: return "ATTN_ERR_HIP: a HIP launch failed (see attn_last_hip_error)";
     default: return "unknown attn_status";

@@ -209,12 +209,28 @@ __global__ __launch_bounds__(kThreads, per_unit(D, 16 * NC)) void decode_kv4_ker
   int row = (at - before * rows_b) / max(units_of(seen), 1);    // of the sequence
   int u0 = (at - before * rows_b) - row * units_of(seen);
 
-  // (The lengths are read again for further sequences; were they changed meanwhile,
+  // From unit u1 of this row to the next row of the share; false at its end.  (The
+  // lengths are read again for further sequences; were they changed meanwhile,
   // the conditions on row and b still keep every access in bounds.)
+  auto next_row = [&](int u1) __attribute__((always_inline)) {
+    at += u1 - u0;
+    u0 = 0;
+    if (at >= end) return false;
+    if (++row < rows_b) return true;
+    row = 0;
+    do {
+      if (++b == p.B) return false;
+      seen = seen_of(p, scalar(p.lens)[b]);
+    } while (seen.tiles == 0);
+    return true;
+  };
   for (bool wrote = false; row < rows_b;) {
     const int u1 = min(units_of(seen), u0 + (end - at));
     const int t0 = max(u0 - kStart, 0), t1 = max(u1 - kStart, 0);
-    if (t0 < t1) {
+    if (t0 >= t1) {                    // the start of a row, and none of its tiles
+      if (!next_row(u1)) return;
+      continue;
+    }
     if (wrote) __syncthreads();        // the states of the row before have been read
     wrote = true;
     const int hk = row / p.head_tiles, ht = row - hk * p.head_tiles;
@@ -286,11 +302,11 @@ __global__ __launch_bounds__(kThreads, per_unit(D, 16 * NC)) void decode_kv4_ker
         if constexpr (D == 128) {
 #pragma unroll
           for (int s = 0; s < 2; ++s)
-            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" " nt"
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt"
                          : : "s"(to + (uint32_t)(kv * TL::kCodes + s * 1024)), "v"(off), "s"(codes[s]) : "memory", "m0");
         } else {
           const uint64_t at = (lane < 32 ? codes[0] : codes[1]) + off;
-          asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" " nt"
+          asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off nt"
                        : : "s"(to + (uint32_t)(kv * TL::kCodes)), "v"(at) : "memory", "m0");
         }
       }
@@ -516,17 +532,7 @@ __global__ __launch_bounds__(kThreads, per_unit(D, 16 * NC)) void decode_kv4_ker
         }
       }
     }
-    }
-    at += u1 - u0;
-    if (at >= end) break;
-    u0 = 0;
-    if (++row == rows_b) {
-      row = 0;
-      do {
-        if (++b == p.B) return;
-        seen = seen_of(p, scalar(p.lens)[b]);
-      } while (seen.tiles == 0);
-    }
+    if (!next_row(u1)) return;
   }
 }
 
