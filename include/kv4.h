@@ -100,9 +100,11 @@ int kv4_load(const void* cache, const int* table, const int* starts, const int* 
  *
  *   workspace  at least attn_decode_kv4_workspace_bytes(B, Hq, Hkv, D) bytes,
  *              16-byte aligned, used until the call's kernels end.  The size depends on
- *              the device's compute units, not on the lengths.
+ *              B, the heads and the current device's compute units, not on the
+ *              lengths.
  *
- * The 32-token tiles of all sequences and KV heads are one list, of which every
+ * lens and table are read while the kernels run, and must not change before
+ * they end.  The 32-token tiles of all sequences and KV heads are one list, of which every
  * workgroup takes an equal share, so uneven lengths balance; rows that
  * lie in several shares are joined by a second kernel.
  * K . Q and P . V run on the matrix unit in the type of Q with fp32
