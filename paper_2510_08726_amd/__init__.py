@@ -680,6 +680,8 @@ def kv_slots(lens, counts, table, free_pages, page, L, *, slots=None, positions=
     _ints("table", table, torch.int32, (B, M))
     _ints("free_pages", free_pages, torch.int32, (free_pages.shape[0],))
     _require(L >= 1, "L must be at least 1")
+    _require(not any(_overlaps(table, x) for x in (lens, counts, free_pages)),
+             "table, which is written, must not share memory with the other tensors")
     stream = _on_device(lens, stream)
     outs = []
     for name, t, dtype, shape in (("slots", slots, torch.int64, (B, L)), ("positions", positions, torch.int32, (B, L)),
@@ -689,8 +691,8 @@ def kv_slots(lens, counts, table, free_pages, page, L, *, slots=None, positions=
         else:
             _same_device(lens, **{name: t})
             _ints(name, t, dtype, shape)
-            _require(not any(_overlaps(t, x) for x in (lens, counts, table, free_pages)),
-                     f"{name} must not share memory with what is read")
+            _require(not any(_overlaps(t, x) for x in (lens, counts, table, free_pages, *outs)),
+                     f"{name} must not share memory with the other tensors")
         outs.append(t)
     with torch.cuda.device(lens.device):
         _check(load_library().kv_slots(_ptr(lens), _ptr(counts), _ptr(table), _ptr(free_pages), free_pages.shape[0], B,

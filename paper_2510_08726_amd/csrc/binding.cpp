@@ -445,10 +445,15 @@ PyObject* py_kv_slots(PyObject*, PyObject* const* x, Py_ssize_t n) {
   if (!output(x[6], *lens, at::kLong, {B, L}, out[0]) || !output(x[7], *lens, at::kInt, {B, L}, out[1]) ||
       !output(x[8], *lens, at::kInt, {B}, out[2]) || !output(x[9], *lens, at::kInt, {1}, out[3]))
     return none();
+  for (const at::Tensor* t : {lens, counts, pages})
+    if (overlap(*table, *t)) return none();
   for (int i = 0; i < 4; ++i)
-    if (x[6 + i] != Py_None)
+    if (x[6 + i] != Py_None) {
       for (const at::Tensor* t : {lens, counts, table, pages})
         if (overlap(out[i], *t)) return none();
+      for (int j = 0; j < i; ++j)
+        if (overlap(out[i], out[j])) return none();
+    }
   const int* pt[3] = {static_cast<const int*>(lens->data_ptr()), static_cast<const int*>(counts->data_ptr()),
                       static_cast<const int*>(pages->data_ptr())};
   int* tp = static_cast<int*>(table->data_ptr());

@@ -66,7 +66,9 @@ def test_slots_given_outputs_and_refusals():
            lambda: pa.kv_slots(lens.long(), counts, table, free, 16, 3), lambda: pa.kv_slots(lens[:1], counts, table, free, 16, 3),
            lambda: pa.kv_slots(lens, counts, table.t(), free, 16, 3), lambda: pa.kv_slots(lens, counts, table[0], free, 16, 3),
            lambda: pa.kv_slots(lens, counts.cpu(), table, free, 16, 3),
-           lambda: pa.kv_slots(lens, counts, table, free, 16, 3, slots=out[1])]
+           lambda: pa.kv_slots(lens, counts, table, free, 16, 3, slots=out[1]),
+           lambda: pa.kv_slots(lens, counts, table, free, 16, 3, new_lens=out[2], taken=out[2][:1]),
+           lambda: pa.kv_slots(table[0], counts, table, free, 16, 3), lambda: pa.kv_slots(lens, counts, table, table[1, 1:], 16, 3)]
     for i, call in enumerate(bad):
         with pytest.raises((ValueError, pa.AttnError)):
             call()
