@@ -5,7 +5,7 @@
 // eighth of a turn; sine and cosine there by their Taylor series in 32 bits (through x^9
 // and x^10, under 2e-9 off for |x| <= pi / 4).  A thread forms them once for
 // its dims and turns four heads by them: 4 x 4096 tokens of 32 + 8 heads of 128 bf16 dims
-// take 76 us with one head a thread, 61 with 2, 56 with 4 and 57 with 8.  Up to 2048
+// take 61 us with two heads a thread, 56 with 4 and 57 with 8.  Up to 2048
 // workgroups that does not pay (2 x 512 tokens: 7.5 us either way), and latency wants
 // every thread there is.
 //
