@@ -5,15 +5,16 @@
 // eighth of a turn; sine and cosine there by their Taylor series in 32 bits (through x^9
 // and x^10, under 2e-9 off for |x| <= pi / 4).  A thread forms them once for
 // its dims and turns four heads by them: 4 x 4096 tokens of 32 + 8 heads of 128 bf16 dims
-// take 61 us with two heads a thread, 56 with 4 and 57 with 8.  Up to 2048
-// workgroups that does not pay (2 x 512 tokens: 7.5 us either way), and latency wants
-// every thread there is.
+// take 67 us with one head a thread, 61 with two, 56 with 4 and 56.5 with 8.  Up to 512
+// workgroups latency wants every thread there is: on the GPU 8 tokens take 3.4 us
+// with one head a thread and 4.1 with four, 256 tokens 4.3 and 4.6, but 512 tokens 5.1 and
+// 4.8, 3 x 512 11.0 and 9.0.
 //
 // Bound by HBM for many tokens: 335 MB in and out in 56 us, 6.0 TB/s (interleaved
-// pairs out of a projection's [B, L, H, D] 61), by the launch for few (8 tokens: 3.8 us, a
+// pairs out of a projection's [B, L, H, D] 61), by the launch for few (8 tokens: 3.4 us, a
 // kernel that does nothing 2).  Calls with 64 MB of outputs or more, which leave the
-// caches before anybody reads them, are streamed past them: 60 us without, and
-// fp32 74 against 66 (at 67 MB the same, 26.5).  Not where neighbouring loads share
+// caches before anybody reads them, are streamed past them: 63 us without, and
+// fp32 70 against 66 (at 67 MB the same, 26.5).  Not where neighbouring loads share
 // lines, which then are fetched again (nearly twice the time for a part of 24 dims).
 
 #include "kernel_common.h"
@@ -25,7 +26,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kHeads = 4;       // heads of a thread
-constexpr int kFew = 2048;      // workgroups of one head a thread up to which a thread has one
+constexpr int kFew = 512;       // workgroups of one head a thread up to which a thread has one
 
 constexpr int64_t kStream = int64_t(64) << 20;   // bytes of outputs from which a call is streamed
 
