@@ -38,17 +38,17 @@ constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
 constexpr int kTile = 32;          // tokens
 constexpr int kStart = kKv4RowStart;   // units of a row's start and end
-// Units that a share holds at least: two tiles a wave, where one pays its start and the
-// combine for less (one request of 3001 tokens 9.5 us; 12 with 16 units, 13.4 with 24,
-// 15.5 with 40; 64 requests of up to 200 tokens 13.7, 16.2, 16.7 and 22; one of 32768 tokens
-// would rather have longer shares, 19.1 against 18.4, 17.0 and 16.5).
+// Units that a share holds at least, one row's start or two tiles a wave: one request
+// of 3001 tokens takes 9 us, 10.8 with 16 units, 12.1 with 24, 14.4 with 40, and 64 requests of up
+// to 200 tokens 11.4, 13.5, 14.7 and 19.2 (one of 32768 tokens would rather have longer
+// shares: 17.0 against 16.2, 15.9 and 15.0).
 constexpr int kLeast = 8;
 
 // How many workgroups share a compute unit, and the tiles that a wave has in LDS: as
 // many waves as the registers allow, then the tiles that 160 KB hold.  16 x 32768
-// tokens of 8 KV heads at D = 128 take 98.6 us with 4 workgroups of 2 tiles a wave, 101 with
-// 3 of 3 and 100.6 with 2 of 4; at D = 64 4 of 4 and 5 of 3 are alike (8 x 16 heads of
-// 16384 tokens with ALiBi 37.7 and 36.8 us, 16 x 32 / 4 of 32768 35.9 and 38.1).
+// tokens of 8 KV heads at D = 128 take 94.4 us with 4 workgroups of 2 tiles a wave, 95.5 with
+// 3 of 3 and 96.7 with 2 of 4.  At D = 64 a fifth workgroup takes 8 x 16 heads of 16384
+// tokens with ALiBi from 37.6 to 36.4, but spills registers in the kernels without it.
 constexpr int per_unit(int D, int cols) { return cols == 16 ? 4 : D == 64 ? 3 : 2; }
 constexpr int ring_tiles(int D, int cols) { return D == 128 && cols == 16 ? 2 : 4; }
 constexpr float kLazy = 8.f;       // log2 units that a score may exceed its reference by

@@ -207,11 +207,11 @@ struct Kv4DecodeParams {
   float cap_k2, cap_cl; // as DecodeParams
 };
 // What a row of the list of tiles counts beside them: 32 uneven requests of 16
-// KV heads took 73 us with 0, 31 with 4, 27.4 with 8, 27.0 with 12, 27.8 with 16 and 29.5 with 24.
+// KV heads take 62 us with 0, 27.3 with 4, 24.5 with 8, 24.7 with 12, 25.4 with 16 and 27.2 with 24.
 constexpr int kKv4RowStart = 8;
 // Query heads that one workgroup serves: 16 or 32 matrix columns.  More than 16
-// in two workgroups of 16 read K and V twice: 16 x 40 / 2 heads of 32768 tokens 52 us
-// against 40, 16 x 256 / 8 190 against 125 (but 8 x 40 / 2 of 1500 9.4 against 11.4).
+// in two workgroups of 16 read K and V twice: 16 x 40 / 2 heads of 32768 tokens 50 us
+// against 39, 16 x 256 / 8 188 against 117 (but 8 x 40 / 2 of 1500 10.4 against 12.0).
 constexpr int kv4_columns(int group) { return group <= 16 ? 16 : 32; }
 // Workgroups of the split kernel on a device of `cus` compute units.
 int kv4_shares(int D, int group, int cus);
