@@ -108,7 +108,7 @@ int kv4_load(const void* cache, const int* table, const int* starts, const int* 
  * workgroup takes an equal share, so uneven lengths balance; rows that
  * lie in several shares are joined by a second kernel.
  * K . Q and P . V run on the matrix unit in the type of Q with fp32
- * accumulation; P is rounded to that type.
+ * accumulation; a weight of P is the sum of two values of that type.
  * Errors: ATTN_ERR_NULL, ATTN_ERR_SHAPE, ATTN_ERR_UNSUPPORTED, ATTN_ERR_WORKSPACE, ATTN_ERR_HIP.
  */
 size_t attn_decode_kv4_workspace_bytes(int B, int Hq, int Hkv, int D);

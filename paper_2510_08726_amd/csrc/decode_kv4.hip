@@ -432,8 +432,12 @@ __global__ __launch_bounds__(kThreads, per_unit(D, 16 * NC)) void decode_kv4_ker
             }
           }
       }
-      // Lazy repair: the reference moves when a score exceeds it by more than kLazy.
-      vec8 pb[NC];
+      // Lazy repair: the reference moves when a score exceeds it by more than kLazy.  A
+      // weight goes to the matrix unit as two values of T, itself rounded and what that
+      // leaves, so that P . V has the 32 bits of its sum and of its division: one value
+      // alone, half a step of bf16 off, was most of the output's error (16 x 32768 tokens
+      // then took 95.1 us, 97.1 with both).
+      vec8 pb[NC], pr[NC];
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
         float top = sc[c][0];
@@ -456,9 +460,14 @@ __global__ __launch_bounds__(kThreads, per_unit(D, 16 * NC)) void decode_kv4_ker
           e[i] = fast_exp2(sc[c][i] - ref);
           l[c] += e[i];
         }
-        const u32x4 pw = {Elem<T>::pack2(e[0], e[1]), Elem<T>::pack2(e[2], e[3]), Elem<T>::pack2(e[4], e[5]),
-                          Elem<T>::pack2(e[6], e[7])};
+        u32x4 pw, rw;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          pw[i] = Elem<T>::pack2(e[2 * i], e[2 * i + 1]);
+          rw[i] = Elem<T>::pack2(e[2 * i] - Elem<T>::lo(pw[i]), e[2 * i + 1] - Elem<T>::hi(pw[i]));
+        }
         pb[c] = __builtin_bit_cast(vec8, pw);
+        pr[c] = __builtin_bit_cast(vec8, rw);
       }
       // O^T: byte h of a lane's dims of tokens 2 i and 2 i + 1 gives word i of
       // the operands of dims 2 h and 2 h + 1.
@@ -476,6 +485,8 @@ __global__ __launch_bounds__(kThreads, per_unit(D, 16 * NC)) void decode_kv4_ker
         for (int c = 0; c < NC; ++c) {
           o[c][2 * h] = Mfma16<T>::mul(__builtin_bit_cast(vec8, a0), pb[c], o[c][2 * h]);
           o[c][2 * h + 1] = Mfma16<T>::mul(__builtin_bit_cast(vec8, a1), pb[c], o[c][2 * h + 1]);
+          o[c][2 * h] = Mfma16<T>::mul(__builtin_bit_cast(vec8, a0), pr[c], o[c][2 * h]);
+          o[c][2 * h + 1] = Mfma16<T>::mul(__builtin_bit_cast(vec8, a1), pr[c], o[c][2 * h + 1]);
         }
       };
       block(std::integral_constant<int, 0>{});
