@@ -94,9 +94,9 @@ int kv4_load(const void* cache, const int* table, const int* starts, const int* 
  *   Q [B, Hq, 1, D], O [B, Hq, 1, D]; the query of sequence b is its token
  *   lens[b] - 1 and sees tokens max(0, lens[b] - window) .. lens[b] - 1
  *   (window 0: all).  scale, alibi_slopes (i = lens[b] - 1) and softcap as
- *   attn_decode_mod.  A sequence that sees nothing gives 0.  For several query
- *   tokens of one sequence, pass the sequence's table row once for each, with its
- *   own length.
+ *   attn_decode_mod; a cap of any size keeps a score to its 32-bit rounding.  A
+ *   sequence that sees nothing gives 0.  For several query tokens of one sequence,
+ *   pass the sequence's table row once for each, with its own length.
  *
  *   workspace  at least attn_decode_kv4_workspace_bytes(B, Hq, Hkv, D) bytes,
  *              16-byte aligned, used until the call's kernels end.  The size depends on

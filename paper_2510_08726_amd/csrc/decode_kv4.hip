@@ -135,6 +135,20 @@ __device__ __forceinline__ ScalarInts scalar(const int* p) {
   return (ScalarInts)reinterpret_cast<uintptr_t>(p);
 }
 
+// soft_cap of a cap above kKv4HighCap.  There 1 - 2 / (1 + e^2t) loses the score in
+// the cap: it is off by 2^-22 of the cap.  Up to half the cap: the series of tanh t /
+// t, t = x / cl, to t^12 (the next term is under 1e-7 there); beyond, the loss is under 3e-7 of the score.
+__device__ __forceinline__ float high_cap(float x, const Kv4DecodeParams& p) {
+  const float t = x * p.cap_inv, z = t * t;
+  float s = 3.5921280e-3f;                       // 21844 / 6081075
+  s = __builtin_fmaf(s, z, -8.8632355e-3f);      // -1382 / 155925
+  s = __builtin_fmaf(s, z, 2.1869489e-2f);       // 62 / 2835
+  s = __builtin_fmaf(s, z, -5.3968254e-2f);      // -17 / 315
+  s = __builtin_fmaf(s, z, 1.3333333e-1f);       // 2 / 15
+  s = __builtin_fmaf(s, z, -3.3333333e-1f);      // -1 / 3
+  return fabsf(t) < 0.5f ? __builtin_fmaf(x * z, s, x) : soft_cap(x, p.cap_k2, p.cap_cl);
+}
+
 __device__ __forceinline__ float as_float(uint32_t bits) { return __builtin_bit_cast(float, bits); }
 
 template <int D, typename T, int NC, bool ALIBI, bool CAP>
@@ -413,10 +427,23 @@ __global__ __launch_bounds__(kThreads, per_unit(D, 16 * NC)) void decode_kv4_ker
             // The bias from the tile's and the token's part of the distance, one
             // rounding each.
             const float bias = ALIBI ? __builtin_fmaf(slope[c], (float)(16 * s + 4 * r), far_bias[c]) : 0.f;
-            if (CAP) sc[c][4 * s + r] = soft_cap(acc[c][r] * p.c, p.cap_k2, p.cap_cl, p.cap_cl + bias);
+            if (CAP) sc[c][4 * s + r] = acc[c][r] * p.c;
             else sc[c][4 * s + r] = ALIBI ? __builtin_fmaf(acc[c][r], p.c, bias) : acc[c][r] * p.c;
           }
         }
+      }
+      if (CAP) {
+        auto capped = [&](auto cap) __attribute__((always_inline)) {
+#pragma unroll
+          for (int c = 0; c < NC; ++c)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const float bias = ALIBI ? __builtin_fmaf(slope[c], (float)(16 * (i >> 2) + 4 * (i & 3)), far_bias[c]) : 0.f;
+              sc[c][i] = cap(sc[c][i], bias);
+            }
+        };
+        if (p.cap_inv != 0.f) capped([&](float x, float bias) { return high_cap(x, p) + bias; });
+        else capped([&](float x, float bias) { return soft_cap(x, p.cap_k2, p.cap_cl, p.cap_cl + bias); });
       }
       if (tok < seen.lo || tok + kTile > seen.hi || lost) {
         // What is not seen: no weight, and no NaN from what its bytes hold.
@@ -522,7 +549,11 @@ __global__ __launch_bounds__(kThreads, per_unit(D, 16 * NC)) void decode_kv4_ker
         }
       }
       __syncthreads();
-      for (int idx = threadIdx.x; idx < min(heads - 16 * c, 16) * (D / 4); idx += kThreads) {
+      // (Not known to be the same at every row: its addresses would be held in
+      // registers through the tile loops, which have none to spare.)
+      int tid = threadIdx.x;
+      asm volatile("" : "+v"(tid));
+      for (int idx = tid; idx < min(heads - 16 * c, 16) * (D / 4); idx += kThreads) {
         const int in = idx / (D / 4), d = idx % (D / 4) * 4, h = 16 * c + in;
         float M = kNegInf;
 #pragma unroll
