@@ -715,7 +715,7 @@ def kv4_append(k, v, cache, slots, *, stream=None):
     """Round k and v [B, Hkv, L, D] (float16 or bfloat16, rows contiguous) to 4
     bits and write them into ``cache`` (uint8 [pages, Hkv, kv4_page_bytes(page,
     D)]) at ``slots`` (int64 [B, L], distinct; others than 0 .. pages * page - 1
-    are skipped).  Returns ``cache``."""
+    are skipped).  The cache shares memory with no other operand.  Returns ``cache``."""
     r = (_BINDING or _load_binding()).kv4_append(k, v, cache, slots, stream)
     if r is not None:
         return _result(r)
@@ -747,7 +747,8 @@ def kv4_load(cache, table, lens, L, D, dtype, k=None, v=None, *, starts=None, st
     """k and v [B, Hkv, L, D] of tokens starts[b] .. starts[b] + L - 1 (default:
     from token 0) of each sequence of a 4-bit cache, as held; zeros from
     token lens[b] on.  ``table`` int32 [B, max_pages], ``lens`` and
-    ``starts`` int32 [B].  Returns (k, v), which attn_fwd takes."""
+    ``starts`` int32 [B]; k and v, if given, share memory with nothing.  Returns
+    (k, v), which attn_fwd takes."""
     r = (_BINDING or _load_binding()).kv4_load(cache, table, lens, L, D, dtype, k, v, starts, stream)
     if r is not None:
         return _result(r)
@@ -790,8 +791,9 @@ def attn_decode_kv4(q, cache, table, lens, o=None, *, scale=None, alibi_slopes=N
     ``cache`` uint8 [pages, Hkv, kv4_page_bytes(page, D)], ``table`` int32 [B,
     max_pages], ``lens`` int32 [B].  ``scale`` defaults to 1/sqrt(D);
     ``alibi_slopes`` and ``softcap`` as for attn_decode.  ``workspace`` (uint8
-    GPU tensor of attn_decode_kv4_workspace_bytes) is allocated when not given.
-    Returns ``o`` [B, Hq, 1, D], 0 for a sequence that sees nothing.
+    GPU tensor of attn_decode_kv4_workspace_bytes) is allocated when not given;
+    neither it nor ``o`` may share memory with another operand.  Returns ``o``
+    [B, Hq, 1, D], 0 for a sequence that sees nothing.
     """
     r = (_BINDING or _load_binding()).attn_decode_kv4(q, cache, table, lens, o, scale, alibi_slopes, softcap, window,
                                                       workspace, stream)

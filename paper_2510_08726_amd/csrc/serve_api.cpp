@@ -4,6 +4,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
+#include <initializer_list>
 #include <limits>
 
 #include "../../include/attn.h"
@@ -64,6 +65,40 @@ bool cache_ok(int B, int Hkv, int L, int pages) {
 
 bool kv4_type(int D, attn_dtype dtype) {
   return (D == 64 || D == 128) && (dtype == ATTN_F16 || dtype == ATTN_BF16);
+}
+
+// The bytes that an operand spans.
+struct Span {
+  uintptr_t begin, end;
+};
+
+Span span(const void* p, int64_t bytes) {
+  const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+  return {at, p ? at + (uintptr_t)bytes : at};
+}
+
+// Those of rows of D 16-bit elements, with strides of batches, heads and tokens of either sign.
+Span span(const void* p, const long long* strides, int B, int H, int L, int D) {
+  const int n[3] = {B, H, L};
+  __int128 low = 0, high = D;
+  for (int i = 0; i < 3; ++i) {
+    const __int128 reach = (__int128)(n[i] - 1) * strides[i];
+    (reach < 0 ? low : high) += reach;
+  }
+  const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+  return {at + (uintptr_t)(2 * low), at + (uintptr_t)(2 * high)};
+}
+
+// Whether `out`, which a call writes, lies apart from all the others.
+bool apart(Span out, std::initializer_list<Span> others) {
+  for (const Span& x : others)
+    if (x.begin < out.end && out.begin < x.end) return false;
+  return true;
+}
+
+// (More than 2^62 bytes are no cache.)
+int64_t cache_bytes(int pages, int Hkv, int page, int D) {
+  return (int64_t)std::min((__int128)kv4_page_bytes(page, D) * Hkv * pages, (__int128)1 << 62);
 }
 
 }  // namespace
@@ -142,6 +177,9 @@ int kv4_append(const void* K, const long long* k_strides, const void* V, const l
   if (misaligned(K) || misaligned(V) || misaligned(cache)) return ATTN_ERR_SHAPE;
   for (int i = 0; i < 3; ++i)
     if (k_strides[i] % 8 || v_strides[i] % 8) return ATTN_ERR_SHAPE;
+  if (!apart(span(cache, cache_bytes(pages, Hkv, page, D)),
+             {span(K, k_strides, B, Hkv, L, D), span(V, v_strides, B, Hkv, L, D), span(slots, 8LL * B * L)}))
+    return ATTN_ERR_SHAPE;
   attn::Kv4AppendParams p{};
   p.x[0] = K; p.x[1] = V;
   p.sb[0] = k_strides[0]; p.sh[0] = k_strides[1]; p.sl[0] = k_strides[2];
@@ -161,6 +199,12 @@ int kv4_load(const void* cache, const int* table, const int* starts, const int* 
     return ATTN_ERR_SHAPE;
   if (!kv4_type(D, dtype)) return ATTN_ERR_UNSUPPORTED;
   if (misaligned(K) || misaligned(V) || misaligned(cache)) return ATTN_ERR_SHAPE;
+  const int64_t rows = 2LL * B * Hkv * L * D;
+  const Span in[] = {span(cache, cache_bytes(pages, Hkv, page, D)), span(table, 4LL * B * max_pages),
+                     span(starts, 4LL * B), span(lens, 4LL * B)};
+  if (!apart(span(K, rows), {span(V, rows), in[0], in[1], in[2], in[3]}) ||
+      !apart(span(V, rows), {in[0], in[1], in[2], in[3]}))
+    return ATTN_ERR_SHAPE;
   attn::Kv4LoadParams p{};
   p.cache = static_cast<const unsigned char*>(cache);
   p.table = table; p.starts = starts; p.lens = lens;
@@ -195,8 +239,14 @@ int attn_decode_kv4(const void* Q, const void* cache, const int* table, const in
   if ((int64_t)B * Hq > kMaxInt || ((int64_t)max_pages << shift) > kMaxTokens ||
       (int64_t)(kv4_page_bytes(page, D) * Hkv) > kMaxInt || rows > kMaxInt / ((((int64_t)max_pages << shift) + 31) / 32 + attn::kKv4RowStart))
     return ATTN_ERR_SHAPE;
-  if (workspace_bytes < attn_decode_kv4_workspace_bytes(B, Hq, Hkv, D) || misaligned(workspace))
-    return ATTN_ERR_WORKSPACE;
+  const size_t need = attn_decode_kv4_workspace_bytes(B, Hq, Hkv, D);
+  if (workspace_bytes < need || misaligned(workspace)) return ATTN_ERR_WORKSPACE;
+  const int64_t heads = 2LL * B * Hq * D;
+  const Span ws = span(workspace, (int64_t)need);
+  const Span in[] = {span(Q, heads), span(cache, cache_bytes(pages, Hkv, page, D)), span(table, 4LL * B * max_pages),
+                     span(lens, 4LL * B), span(alibi_slopes, 4LL * Hq)};
+  if (!apart(span(O, heads), {ws, in[0], in[1], in[2], in[3], in[4]}) || !apart(ws, {in[0], in[1], in[2], in[3], in[4]}))
+    return ATTN_ERR_SHAPE;
   attn::Kv4DecodeParams p{};
   p.q = Q; p.cache = static_cast<const unsigned char*>(cache); p.table = table; p.lens = lens; p.o = O;
   p.slopes = alibi_slopes;
