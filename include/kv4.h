@@ -74,7 +74,8 @@ int kv_slots(const int* lens, const int* counts, int* table, const int* free_pag
  *           are contiguous).  Pointers 16-byte aligned, strides multiples of 8.
  *   slots   device long long [B, L], distinct; a slot outside 0 .. pages * page - 1
  *           is skipped (padding).  Slots given twice keep a mixture.
- *   D 64 or 128, dtype fp16 or bf16.
+ *   D 64 or 128, dtype fp16 or bf16.  L < 2^28 - 15 (D = 128) or 2^29 - 31, B * L < 2^31,
+ *   Hkv < 2^16.
  * Errors: ATTN_ERR_NULL, ATTN_ERR_SHAPE (sizes, page, alignment), ATTN_ERR_UNSUPPORTED.
  */
 int kv4_append(const void* K, const long long* k_strides, const void* V, const long long* v_strides, void* cache,
@@ -110,6 +111,10 @@ int kv4_load(const void* cache, const int* table, const int* starts, const int* 
  * they end.  The 32-token tiles of all sequences and KV heads are one list, of which every
  * workgroup takes an equal share, so uneven lengths balance; rows that
  * lie in several shares are joined by a second kernel.
+ * B * Hq < 2^24.  The list is counted in 32 bits, with 8 more for each row, for the
+ * longest contexts that the table holds whatever lens says: B * Hkv * T *
+ * (max_pages * page / 32 + 8) < 2^31, where T is the workgroups of up to 32 query heads
+ * that a KV head takes.
  * K . Q and P . V run on the matrix unit in the type of Q with fp32
  * accumulation; a weight of P is the sum of two values of that type.
  * Errors: ATTN_ERR_NULL, ATTN_ERR_SHAPE, ATTN_ERR_UNSUPPORTED, ATTN_ERR_WORKSPACE, ATTN_ERR_HIP.

@@ -19,6 +19,8 @@ constexpr int64_t kMaxInt = std::numeric_limits<int32_t>::max();
 constexpr int64_t kMaxElements = int64_t(1) << 40;
 constexpr int64_t kMaxTokens = int64_t(1) << 30;   // that a sequence's table row may hold
 
+constexpr int64_t kMaxGroups = (int64_t(1) << 24) - 1;   // workgroups of 256 threads in a row of a grid: under 2^32 threads
+
 bool misaligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) != 0; }
 
 // log2 of a page size, or -1.
@@ -62,6 +64,9 @@ bool cache_ok(int B, int Hkv, int L, int pages) {
   return B >= 1 && Hkv >= 1 && Hkv <= 65535 && L >= 1 && pages >= 1 && (int64_t)B * L <= kMaxInt &&
          (int64_t)B * L <= kMaxElements / (128 * (int64_t)Hkv);
 }
+
+// A thread for every 8 dims of L tokens in a row of the grid of kv4_append and kv4_load.
+bool tokens_ok(int L, int D) { return L <= kMaxGroups * (2048 / D); }
 
 bool kv4_type(int D, attn_dtype dtype) {
   return (D == 64 || D == 128) && (dtype == ATTN_F16 || dtype == ATTN_BF16);
@@ -174,7 +179,7 @@ int kv4_append(const void* K, const long long* k_strides, const void* V, const l
   const int shift = page_shift(page);
   if (!cache_ok(B, Hkv, L, pages) || shift < 0) return ATTN_ERR_SHAPE;
   if (!kv4_type(D, dtype)) return ATTN_ERR_UNSUPPORTED;
-  if (misaligned(K) || misaligned(V) || misaligned(cache)) return ATTN_ERR_SHAPE;
+  if (!tokens_ok(L, D) || misaligned(K) || misaligned(V) || misaligned(cache)) return ATTN_ERR_SHAPE;
   for (int i = 0; i < 3; ++i)
     if (k_strides[i] % 8 || v_strides[i] % 8) return ATTN_ERR_SHAPE;
   if (!apart(span(cache, cache_bytes(pages, Hkv, page, D)),
@@ -198,7 +203,7 @@ int kv4_load(const void* cache, const int* table, const int* starts, const int* 
   if (!cache_ok(B, Hkv, L, pages) || shift < 0 || max_pages < 1 || ((int64_t)max_pages << shift) > kMaxTokens)
     return ATTN_ERR_SHAPE;
   if (!kv4_type(D, dtype)) return ATTN_ERR_UNSUPPORTED;
-  if (misaligned(K) || misaligned(V) || misaligned(cache)) return ATTN_ERR_SHAPE;
+  if (!tokens_ok(L, D) || misaligned(K) || misaligned(V) || misaligned(cache)) return ATTN_ERR_SHAPE;
   const int64_t rows = 2LL * B * Hkv * L * D;
   const Span in[] = {span(cache, cache_bytes(pages, Hkv, page, D)), span(table, 4LL * B * max_pages),
                      span(starts, 4LL * B), span(lens, 4LL * B)};
@@ -236,7 +241,7 @@ int attn_decode_kv4(const void* Q, const void* cache, const int* table, const in
   const int group = Hq / Hkv, cols = attn::kv4_columns(group), tiles = (group + cols - 1) / cols;
   const int64_t rows = (int64_t)B * Hkv * tiles;
   // The list of all tiles is counted in 32 bits, and so is a page of all heads.
-  if ((int64_t)B * Hq > kMaxInt || ((int64_t)max_pages << shift) > kMaxTokens ||
+  if ((int64_t)B * Hq > kMaxGroups || ((int64_t)max_pages << shift) > kMaxTokens ||
       (int64_t)(kv4_page_bytes(page, D) * Hkv) > kMaxInt || rows > kMaxInt / ((((int64_t)max_pages << shift) + 31) / 32 + attn::kKv4RowStart))
     return ATTN_ERR_SHAPE;
   const size_t need = attn_decode_kv4_workspace_bytes(B, Hq, Hkv, D);
