@@ -60,7 +60,7 @@ size_t kv4_page_bytes(int page, int D);
  *   taken      [1] int: pages taken off free_pages
  *
  * lens[b] is clamped to 0 .. max_pages * page.  nfree >= 0; B * max_pages
- * and B * L < 2^31.  One kernel.
+ * and B * L < 2^31, max_pages * page + L <= 2^31.  One kernel.
  * Errors: ATTN_ERR_NULL (free_pages may be NULL where nfree is 0), ATTN_ERR_SHAPE (sizes, new_lens == lens).
  */
 int kv_slots(const int* lens, const int* counts, int* table, const int* free_pages, int nfree, int B, int max_pages,

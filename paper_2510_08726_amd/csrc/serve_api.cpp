@@ -163,6 +163,7 @@ int kv_slots(const int* lens, const int* counts, int* table, const int* free_pag
   if (B < 1 || L < 1 || max_pages < 1 || nfree < 0 || shift < 0 || new_lens == lens) return ATTN_ERR_SHAPE;
   if ((int64_t)B * L > kMaxInt || (int64_t)B * max_pages > kMaxInt || ((int64_t)max_pages << shift) > kMaxTokens)
     return ATTN_ERR_SHAPE;
+  if (((int64_t)max_pages << shift) + L > kMaxInt + 1) return ATTN_ERR_SHAPE;    // positions are int
   attn::SlotsParams p{};
   p.lens = lens; p.counts = counts; p.table = table; p.free_pages = free_pages; p.nfree = nfree;
   p.B = B; p.M = max_pages; p.L = L; p.shift = shift;

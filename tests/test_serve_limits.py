@@ -34,3 +34,8 @@ def test_append_and_load_have_a_thread_for_each_vector_of_a_head(lib, D, L):
     """2^32 threads, which hold 8 dims each, of L tokens."""
     assert lib.kv4_append(AT[0], ZERO, AT[1], ZERO, AT[2], AT[3], 1, 1, L, D, 4, 16, 0, None) == SHAPE
     assert lib.kv4_load(*AT[:4], AT[4], AT[5], 1, 1, L, D, 4, 16, 1 << 20, 0, None) == SHAPE
+
+
+@pytest.mark.parametrize("M,page,L", [(1 << 15, 1 << 15, (1 << 30) + 1), (1, 16, (1 << 31) - 15), (1 << 26, 16, (1 << 31) - 1)])
+def test_positions_fit_32_bits(lib, M, page, L):
+    assert lib.kv_slots(*AT[:4], 4, 1, M, page, L, *AT[4:8], None) == SHAPE
