@@ -817,8 +817,9 @@ def attn_decode_kv4(q, cache, table, lens, o=None, *, scale=None, alibi_slopes=N
              "o must be a contiguous GPU tensor shaped like q")
     if workspace is None:
         _require(isinstance(stream, torch.cuda.Stream), "a stream of this kind needs a workspace of the caller's")
-        workspace = _allocate((max(attn_decode_kv4_workspace_bytes(B, Hq, cache.shape[1], D), 16),), q, stream,
-                              torch.uint8)
+        with torch.cuda.device(q.device):            # whose compute units the size counts
+            size = attn_decode_kv4_workspace_bytes(B, Hq, cache.shape[1], D)
+        workspace = _allocate((max(size, 16),), q, stream, torch.uint8)
     _same_device(q, workspace=workspace)
     _require(workspace.is_contiguous(), "workspace must be contiguous")
     sc = 1.0 / math.sqrt(D) if scale is None else float(scale)
