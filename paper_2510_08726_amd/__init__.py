@@ -533,10 +533,19 @@ def rope_frequencies(rotary_dim, base=10000.0, *, scaling=None, factor=1.0, orig
     """
     _require(scaling in _ROPE_SCALING, "scaling must be None, 'linear', 'base' or 'parts'")
     n = int(rotary_dim)
+    _require(_fits(n), "rotary_dim must fit 32 bits")
     f = torch.empty(max(n // 2, 1), dtype=torch.float64)
     _check(load_library().rope_frequencies(n, float(base), _ROPE_SCALING[scaling], float(factor),
                                            float(original_length), float(slow), float(fast), _ptr(f)))
     return f if device is None else f.to(device)
+
+
+_INT_MAX = (1 << 31) - 1
+
+
+def _fits(*sizes):
+    """Whether the C entry points' ints hold them (ctypes would cut them to 32 bits)."""
+    return all(0 <= n <= _INT_MAX for n in sizes)
 
 
 def _on_device(t, stream):
@@ -550,8 +559,10 @@ def _on_device(t, stream):
 
 def _same_device(first, **tensors):
     _require(first.is_cuda, "tensors must be on the GPU")
+    _require(_fits(*first.shape), "sizes must fit 32 bits")
     for name, t in tensors.items():
         _require(t.device == first.device, f"{name} must be on the same GPU as the other tensors")
+        _require(_fits(*t.shape), f"{name}'s sizes must fit 32 bits")
 
 
 def _ints(name, t, dtype, shape):
@@ -599,7 +610,7 @@ def _rope(bwd, q, k, positions, freqs, q_out, k_out, interleaved, magnitude, str
         _same_device(q, k=k)
         _require(k.dtype == q.dtype and (k.shape[0], *k.shape[2:]) == (B, L, D),
                  "k must have q's dtype, batch, length and head dim")
-    _require(freqs.dtype == torch.float64 and freqs.dim() == 1 and freqs.is_contiguous(),
+    _require(freqs.dtype == torch.float64 and freqs.dim() == 1 and freqs.is_contiguous() and _fits(2 * freqs.numel()),
              "freqs must be a contiguous float64 tensor [rotary_dim / 2]")
     _require(positions.dtype in (torch.int32, torch.int64) and tuple(positions.shape) in ((B, L), (L,))
              and positions.is_contiguous(), "positions must be a contiguous int32 or int64 tensor [B, L] or [L]")
@@ -652,7 +663,7 @@ def rope_bwd(dq, dk, positions, freqs, q_out=None, k_out=None, *, interleaved=Fa
 
 def kv4_page_bytes(page, D):
     """Bytes of a page of `page` tokens of one head in the 4-bit cache (0 if not supported)."""
-    return load_library().kv4_page_bytes(page, D)
+    return load_library().kv4_page_bytes(page, D) if _fits(page, D) else 0
 
 
 def kv_slots(lens, counts, table, free_pages, page, L, *, slots=None, positions=None, new_lens=None, taken=None,
@@ -679,7 +690,7 @@ def kv_slots(lens, counts, table, free_pages, page, L, *, slots=None, positions=
     _ints("counts", counts, torch.int32, (B,))
     _ints("table", table, torch.int32, (B, M))
     _ints("free_pages", free_pages, torch.int32, (free_pages.shape[0],))
-    _require(L >= 1, "L must be at least 1")
+    _require(L >= 1 and _fits(page, L), "page and L must be at least 1 and fit 32 bits")
     _require(not any(_overlaps(table, x) for x in (lens, counts, free_pages)),
              "table, which is written, must not share memory with the other tensors")
     stream = _on_device(lens, stream)
@@ -756,7 +767,7 @@ def kv4_load(cache, table, lens, L, D, dtype, k=None, v=None, *, starts=None, st
     _require(dtype in _DTYPE_CODE, "dtype must be float16 or bfloat16")
     page = _cache_page(cache, D)
     B, M = _paged(cache, table, lens)
-    _require(L >= 1, "L must be at least 1")
+    _require(L >= 1 and _fits(L), "L must be at least 1 and fit 32 bits")
     if starts is not None:
         _same_device(cache, starts=starts)
         _ints("starts", starts, torch.int32, (B,))
@@ -779,7 +790,7 @@ def kv4_load(cache, table, lens, L, D, dtype, k=None, v=None, *, starts=None, st
 
 
 def attn_decode_kv4_workspace_bytes(B, Hq, Hkv, D):
-    return load_library().attn_decode_kv4_workspace_bytes(B, Hq, Hkv, D)
+    return load_library().attn_decode_kv4_workspace_bytes(B, Hq, Hkv, D) if _fits(B, Hq, Hkv, D) else 0
 
 
 def attn_decode_kv4(q, cache, table, lens, o=None, *, scale=None, alibi_slopes=None, softcap=None, window=None,
@@ -823,10 +834,12 @@ def attn_decode_kv4(q, cache, table, lens, o=None, *, scale=None, alibi_slopes=N
     _same_device(q, workspace=workspace)
     _require(workspace.is_contiguous(), "workspace must be contiguous")
     sc = 1.0 / math.sqrt(D) if scale is None else float(scale)
+    win = min(int(window or 0), _INT_MAX)            # (that many see every token)
+    _require(win >= 0, "window must be at least 1")
     with torch.cuda.device(q.device):
         _check(load_library().attn_decode_kv4(_ptr(q), _ptr(cache), _ptr(table), _ptr(lens), _ptr(o), B, Hq,
                                               cache.shape[1], D, cache.shape[0], page, table.shape[1], sc,
-                                              _ptr(alibi_slopes), float(softcap or 0.0), int(window or 0),
+                                              _ptr(alibi_slopes), float(softcap or 0.0), win,
                                               _ptr(workspace), workspace.numel() * workspace.element_size(),
                                               _DTYPE_CODE[q.dtype], _stream(stream)))
     return o
