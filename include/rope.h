@@ -51,7 +51,8 @@ typedef enum {
  * program uploads them once).  rotary_dim even, >= 2 (ROPE_BASE: >= 4); base
  * > 0; factor > 0 except ROPE_PLAIN; ROPE_PARTS: original_length > 0 and 0 <=
  * slow < fast.  Errors: ATTN_ERR_NULL, ATTN_ERR_SHAPE for the sizes and
- * non-finite values, ATTN_ERR_UNSUPPORTED for another scaling.
+ * non-finite values (a base or frequency that 64 bits do not hold among them),
+ * ATTN_ERR_UNSUPPORTED for another scaling.
  */
 int rope_frequencies(int rotary_dim, double base, int scaling, double factor, double original_length, double slow,
                      double fast, double* freqs);

@@ -121,6 +121,7 @@ int rope_frequencies(int rotary_dim, double base, int scaling, double factor, do
                                 !std::isfinite(fast) || slow < 0 || fast <= slow))
     return ATTN_ERR_SHAPE;
   if (scaling == ROPE_BASE) base *= std::pow(factor, (double)rotary_dim / (rotary_dim - 2));
+  if (!std::isfinite(base)) return ATTN_ERR_SHAPE;
   for (int i = 0; i < rotary_dim / 2; ++i) {
     double f = std::pow(base, -2.0 * i / rotary_dim);
     if (scaling == ROPE_LINEAR) f /= factor;
@@ -129,6 +130,7 @@ int rope_frequencies(int rotary_dim, double base, int scaling, double factor, do
       const double w = std::min(std::max((turns - slow) / (fast - slow), 0.0), 1.0);
       f = f * w + f / factor * (1.0 - w);
     }
+    if (!std::isfinite(f)) return ATTN_ERR_SHAPE;
     freqs[i] = f;
   }
   return ATTN_OK;
