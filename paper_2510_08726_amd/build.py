@@ -76,6 +76,18 @@ def serve_asm_files():
     return [os.path.join(unit_dir(u), f"{u}-hip-amdgcn-amd-amdhsa-{ARCH}.s") for u in ("rope", "kv4", "decode_kv4")]
 
 
+SERVE_SOURCES = ["rope.hip", "kv4.hip", "decode_kv4.hip", "kv4_common.h", "kernel_common.h", "launch.h"]
+
+
+def serve_asm_stale():
+    """Whether any of serve_asm_files() is missing, or older than a source or this file."""
+    files = serve_asm_files()
+    if not all(os.path.exists(f) for f in files):
+        return True
+    newest = max(os.path.getmtime(f) for f in [os.path.join(CSRC, n) for n in SERVE_SOURCES] + [__file__])
+    return min(os.path.getmtime(f) for f in files) < newest
+
+
 def prefill_asm_files():
     """Device assembly of the prefill shards written by the last build()."""
     return [os.path.join(unit_dir(f"prefill{k}"), f"prefill-hip-amdgcn-amd-amdhsa-{ARCH}.s") for k in range(4)]
