@@ -270,8 +270,9 @@ int attn_decode_kv4(const void* Q, const void* cache, const int* table, const in
   p.ws_rows = reinterpret_cast<int2*>(p.ws_l + parts);
   p.bf16 = dtype == ATTN_BF16;
   p.c = scale * kLog2e;
-  // Finite for every cap: an infinity times a score of 0 would be NaN.
-  constexpr float kTop = std::numeric_limits<float>::max();
+  // Finite for every cap, and twice as well: an infinity times 0 (a score, or what is left of
+  // one at infinity) would be NaN.
+  constexpr float kTop = std::numeric_limits<float>::max() / 2;
   p.cap_k2 = softcap > 0.f ? std::min(2.f / softcap, kTop) : 0.f;
   p.cap_cl = softcap > 0.f ? std::min(softcap * kLog2e, kTop) : 0.f;
   p.cap_inv = softcap > attn::kKv4HighCap ? 1.f / p.cap_cl : 0.f;

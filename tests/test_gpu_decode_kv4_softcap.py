@@ -62,3 +62,19 @@ def test_scores_of_zero(cap):
     q = torch.zeros(1, 1, 1, D, dtype=torch.float16, device="cuda")
     o = pa.attn_decode_kv4(q, cache, _i32([[0]]), _i32([n]), softcap=cap)
     assert torch.equal(o[0, 0, 0], v[0, 0, 0])
+
+
+@pytest.mark.parametrize("cap", [30.0, 1e5, 3.4e38])
+def test_infinite_scores_reach_the_cap(cap):
+    """Half of the scores are inf, half -inf: capped, the first weigh the same and the others nothing
+    (e^-2 cap of a weight)."""
+    D, n = 64, 32
+    k, v = torch.zeros(2, 1, 1, n, D, dtype=torch.float16, device="cuda")
+    k[..., 0::2, 0], k[..., 1::2, 0] = 1.0, -1.0
+    v[..., 0::2, :], v[..., 1::2, :] = 2.0, 6.0
+    cache = torch.zeros(1, 1, pa.kv4_page_bytes(32, D), dtype=torch.uint8, device="cuda")
+    pa.kv4_append(k, v, cache, torch.arange(n, device="cuda")[None])
+    q = torch.zeros(1, 1, 1, D, dtype=torch.float16, device="cuda")
+    q[..., 0] = float("inf")
+    o = pa.attn_decode_kv4(q, cache, _i32([[0]]), _i32([n]), softcap=cap)
+    assert (o == 2.0).all()
