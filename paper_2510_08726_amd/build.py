@@ -49,14 +49,12 @@ DEVICE = ["-x", "hip", f"--offload-arch={ARCH}", "-Xclang", "-target-feature", "
 # values produced by inline assembly compiles to a plain v_max instead of
 # canonicalising both inputs first.  The prefill device assembly is kept
 # (-save-temps) for the ISA hazard check in the tests.
-# The 4-bit decode's accumulators stay in VGPRs (-amdgpu-mfma-vgpr-form): the
-# softmax repairs them there.
 UNITS = [(f"prefill{k}", "prefill.hip", ["-fno-honor-nans", f"-DATTN_PREFILL_SHARD={k}", "-save-temps"])
          for k in range(4)] + [("decode", "decode.hip", ["-save-temps"]), ("peaks", "peaks.hip", ["-save-temps"]),
             ("norms", "norms.hip", ["-save-temps"]),
             ("prefill_split", "prefill_split.hip", ["-fno-honor-nans", "-save-temps"]),
             ("rope", "rope.hip", ["-save-temps"]), ("kv4", "kv4.hip", ["-save-temps"]),
-            ("decode_kv4", "decode_kv4.hip", ["-mllvm", "-amdgpu-mfma-vgpr-form=1", "-save-temps"]),
+            ("decode_kv4", "decode_kv4.hip", ["-save-temps"]),
             ("attn_api", "attn_api.cpp", []), ("serve_api", "serve_api.cpp", [])]
 
 
