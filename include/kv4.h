@@ -53,7 +53,8 @@ size_t kv4_page_bytes(int page, int D);
  * get no new page stay as they are.  Where the free pages or the table's row
  * run out, the tokens that fit are kept.
  *
- *   slots      [B, L] long long: the slot of token l < stored[b], -1 behind
+ *   slots      [B, L] long long: the slot of token l < stored[b], -1 behind (and
+ *              for a token whose page in the table or the list is negative)
  *   positions  [B, L] int: lens[b] + l, for every l
  *   new_lens   [B] int: lens[b] + stored[b]; not lens itself, which other
  *              workgroups still read (refused)
@@ -86,7 +87,8 @@ int kv4_append(const void* K, const long long* k_strides, const void* V, const l
  * K and V [B, Hkv, L, D] (contiguous) of tokens starts[b] .. starts[b] + L - 1 of
  * each sequence, exactly as held; zeros for tokens at or past lens[b], or in
  * a page that does not exist.  starts NULL: from token 0 (negative: as 0).
- * What attn_fwd takes for the next piece of a prompt.
+ * What attn_fwd takes for the next piece of a prompt: one request (or requests of
+ * one length) a call, since it has one Lk and sees every key up to it, zeros too.
  * Errors as kv4_append.
  */
 int kv4_load(const void* cache, const int* table, const int* starts, const int* lens, void* K, void* V, int B,

@@ -650,7 +650,8 @@ def rope_fwd(q, k, positions, freqs, q_out=None, k_out=None, *, interleaved=Fals
     (rope_frequencies); the first rotary_dim dims are rotated in pairs
     (i, i + rotary_dim / 2), or (2 i, 2 i + 1) if ``interleaved``, and the
     rest copied.  ``magnitude`` scales the rotated dims.  Outputs are contiguous;
-    q_out may be q itself, and k_out k.  Returns (q_out, k_out).
+    q_out may be q itself, and k_out k.  Nothing is recorded for autograd: a program
+    that trains calls rope_bwd.  Returns (q_out, k_out).
     """
     return _rope(False, q, k, positions, freqs, q_out, k_out, interleaved, magnitude, stream)
 
@@ -759,7 +760,7 @@ def kv4_load(cache, table, lens, L, D, dtype, k=None, v=None, *, starts=None, st
     from token 0) of each sequence of a 4-bit cache, as held; zeros from
     token lens[b] on.  ``table`` int32 [B, max_pages], ``lens`` and
     ``starts`` int32 [B]; k and v, if given, share memory with nothing.  Returns
-    (k, v), which attn_fwd takes."""
+    (k, v), which attn_fwd takes: for requests of one length, as it sees every key."""
     r = (_BINDING or _load_binding()).kv4_load(cache, table, lens, L, D, dtype, k, v, starts, stream)
     if r is not None:
         return _result(r)

@@ -39,16 +39,16 @@ constexpr int kWaves = kThreads / 64;
 constexpr int kTile = 32;          // tokens
 constexpr int kStart = kKv4RowStart;   // units of a row's start and end
 // Units that a share holds at least, one row's start or two tiles a wave: one request
-// of 3001 tokens takes 9 us, 10.8 with 16 units, 12.1 with 24, 14.4 with 40, and 64 requests of up
-// to 200 tokens 11.4, 13.5, 14.7 and 19.2 (one of 32768 tokens would rather have longer
-// shares: 17.0 against 16.2, 15.9 and 15.0).
+// of 3001 tokens takes 9 us, 10.7 with 16 units, 12.6 with 24, 15.4 with 40, and 64 requests of up
+// to 200 tokens 11.6, 13.5, 15.1 and 20.0 (one of 32768 tokens would rather have longer
+// shares: 17.4 against 16.9, 16.6 and 15.9).
 constexpr int kLeast = 8;
 
 // How many workgroups share a compute unit, and the tiles that a wave has in LDS: as
 // many waves as the registers allow, then the tiles that 160 KB hold.  16 x 32768
-// tokens of 8 KV heads at D = 128 take 94.4 us with 4 workgroups of 2 tiles a wave, 95.5 with
-// 3 of 3 and 96.7 with 2 of 4.  At D = 64 a fifth workgroup takes 8 x 16 heads of 16384
-// tokens with ALiBi from 37.6 to 36.4, but spills registers in the kernels without it.
+// tokens of 8 KV heads at D = 128 take 96.9 us with 4 workgroups of 2 tiles a wave, 100.5 with
+// 3 of 3 and with 2 of 4.  At D = 64 a fifth workgroup takes 8 x 16 heads of 16384
+// tokens with ALiBi from 40.7 to 40.0, but spills registers in five of eight kernels.
 constexpr int per_unit(int D, int cols) { return cols == 16 ? 4 : D == 64 ? 3 : 2; }
 constexpr int ring_tiles(int D, int cols) { return D == 128 && cols == 16 ? 2 : 4; }
 constexpr float kLazy = 8.f;       // log2 units that a score may exceed its reference by
@@ -345,7 +345,8 @@ __global__ __launch_bounds__(kThreads, per_unit(D, 16 * NC)) void decode_kv4_ker
 #pragma unroll
     for (int k = 0; k < kRing; ++k) pages(t0 + wave + k * kWaves, near[k]);
     pages(t0 + wave + kRing * kWaves, far);
-    // The loop's waits count copies alone: what was loaded above is here first.
+    // The loop's waits count copies: were what was loaded above still on its way, or a
+    // spill among them, they would wait for more than their tile (never for less: in order).
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
 #pragma unroll
@@ -462,8 +463,8 @@ __global__ __launch_bounds__(kThreads, per_unit(D, 16 * NC)) void decode_kv4_ker
       // Lazy repair: the reference moves when a score exceeds it by more than kLazy.  A
       // weight goes to the matrix unit as two values of T, itself rounded and what that
       // leaves, so that P . V has the 32 bits of its sum and of its division: one value
-      // alone, half a step of bf16 off, was most of the output's error (16 x 32768 tokens
-      // then took 95.1 us, 97.1 with both).
+      // alone, half a step of bf16 off, is most of the output's error (16 x 32768 tokens then
+      // take 94.7 us, 96.9 with both; with 32 heads a KV head 122 and 143).
       vec8 pb[NC], pr[NC];
 #pragma unroll
       for (int c = 0; c < NC; ++c) {

@@ -57,8 +57,9 @@ __device__ __forceinline__ Need need_of(const SlotsParams& p, int b) {
 // the scan of its own), and writes each item's slot; the item in a new page's
 // first row writes the page into the table.  No workgroup waits for another: each reads the
 // lengths before its own, which the caches hold.  Latency bound: three dependent
-// reads (lengths, page, and the table's or the list's) and two barriers, 2.2 us for 64 requests of one token;
-// 256 requests of up to 2048 tokens write 6.3 MB in 4.9 us.
+// reads (lengths, page, and the table's or the list's) and three barriers (two more for each further
+// 256 sequences, and two for those before), 2.1 us for 64 requests of one token;
+// 256 requests of up to 2048 tokens write 6.3 MB in 4.8 us.
 constexpr int kItems = 512;
 
 __global__ __launch_bounds__(kThreads) void kv_slots_kernel(SlotsParams p) {
@@ -117,13 +118,15 @@ __global__ __launch_bounds__(kThreads) void kv_slots_kernel(SlotsParams p) {
 
 // Grids of the two kernels below: a workgroup's lanes are the rows of neighbouring
 // tokens of one head, blockIdx.y is the head, and blockIdx.z strides the sequences.
-// (More tokens a thread, 2, 4 and 8 with all their loads in flight, took 46, 50 and 56 us
-// where one takes 44: the rows of a workgroup then lie further apart.)
+// (More tokens a thread, 2, 4 and 8 with all their loads in flight, took 4, 13 and 27 % longer
+// than one: the rows of a workgroup then lie further apart.)
 
 // Four lanes hold a block of 32 dims, 8 each: 16 bytes in, 4 bytes out, K and V in
 // one thread.  The input is streamed past the caches, which the cache's lines need until
-// all rows of a line are written (44.6 us for 8 prompts of up to 4095 tokens and their reading
-// back, 46.4 without).
+// all rows of a line are written (47.1 us for 8 prompts of up to 4095 tokens and their reading
+// back, 51.9 without).  The slot decides whether a row is read at all, so that padding is
+// not: two round trips in a row, where kv4_load's codes have one (88 MB in 21.6 us, 4.1
+// TB/s; kv4_load 6.6).
 template <int D, typename T>
 __global__ __launch_bounds__(kThreads) void kv4_append_kernel(Kv4AppendParams p) {
   constexpr int LPR = D / 8;                 // lanes per row
@@ -133,12 +136,12 @@ __global__ __launch_bounds__(kThreads) void kv4_append_kernel(Kv4AppendParams p)
   if (l >= p.L) return;
   for (int b = blockIdx.z; b < p.B; b += gridDim.z) {
     const int64_t slot = p.slots[(int64_t)b * p.L + l];
+    if (slot < 0 || slot >= (int64_t)p.pages << p.shift) continue;    // the lanes of a row agree
     u32x4 x[2];
 #pragma unroll
     for (int k = 0; k < 2; ++k)
       x[k] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(
           static_cast<const T*>(p.x[k]) + b * p.sb[k] + h * p.sh[k] + l * p.sl[k] + 8 * lig));
-    if (slot < 0 || slot >= (int64_t)p.pages << p.shift) continue;    // the lanes of a row agree
     const int r = (int)slot & ((1 << p.shift) - 1);
     unsigned char* base = p.cache + ((slot >> p.shift) * p.H + h) * (int64_t)kv4_block_bytes<D>(p.shift);
 #pragma unroll

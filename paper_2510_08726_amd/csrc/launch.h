@@ -208,7 +208,7 @@ struct Kv4DecodeParams {
   float cap_inv;        // 1 / cap_cl for a cap above kKv4HighCap, else 0
 };
 // What a row of the list of tiles counts beside them: 32 uneven requests of 16
-// KV heads take 62 us with 0, 27.3 with 4, 24.5 with 8, 24.7 with 12, 25.4 with 16 and 27.2 with 24.
+// KV heads take 66.6 us with 0, 28.5 with 4, 25.7 with 8, 26.3 with 12, 27.4 with 16 and 29.3 with 24.
 constexpr int kKv4RowStart = 8;
 // SoftCap caps up to which cap tanh(s / cap) is formed as 1 - 2 / (1 + e^2t), which is off
 // by 2^-22 of the cap: 1.5e-5 at 64, as a score of 60 in 32 bits is, but 0.01 at 1e5.
@@ -216,8 +216,8 @@ constexpr int kKv4RowStart = 8;
 // instead of 33.3.
 constexpr float kKv4HighCap = 64.f;
 // Query heads that one workgroup serves: 16 or 32 matrix columns.  More than 16
-// in two workgroups of 16 read K and V twice: 16 x 40 / 2 heads of 32768 tokens 50 us
-// against 39, 16 x 256 / 8 188 against 117 (but 8 x 40 / 2 of 1500 10.4 against 12.0).
+// in two workgroups of 16 read K and V twice: 16 x 40 / 2 heads of 32768 tokens 53.7 us
+// against 43.5, 16 x 256 / 8 196 against 143 (but 8 x 40 / 2 of 1500 10.3 against 12.0).
 constexpr int kv4_columns(int group) { return group <= 16 ? 16 : 32; }
 // Workgroups of the split kernel on a device of `cus` compute units.
 int kv4_shares(int D, int group, int cus);

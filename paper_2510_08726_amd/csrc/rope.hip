@@ -1,21 +1,22 @@
 // Rotary positions (include/rope.h): queries and keys in one kernel, which
 // reads and writes every row once.
 //
-// Angles: t = p f and its fraction of a turn in 64 bits, exactly reduced to an
-// eighth of a turn; sine and cosine there by their Taylor series in 32 bits (through x^9
-// and x^10, under 2e-9 off for |x| <= pi / 4).  A thread forms them once for
+// Angles: t = p f and its fraction of a turn in 64 bits (three roundings: 3.3e-16 of t),
+// exactly reduced to an eighth of a turn; sine and cosine there by their Taylor series in 32
+// bits (through x^9 and x^10, under 2e-9 off for |x| <= pi / 4).  A thread forms them once for
 // its dims and turns four heads by them: 4 x 4096 tokens of 32 + 8 heads of 128 bf16 dims
-// take 67 us with one head a thread, 61 with two, 56 with 4 and 56.5 with 8.  Up to 512
-// workgroups latency wants every thread there is: on the GPU 8 tokens take 3.4 us
-// with one head a thread and 4.1 with four, 256 tokens 4.3 and 4.6, but 512 tokens 5.1 and
-// 4.8, 3 x 512 11.0 and 9.0.
+// take 68 us with one head a thread, 61 with two, 56 with 4 and 57 with 8.  Up to 512
+// workgroups latency wants every thread there is: the kernel takes 3.4 us for 8 tokens
+// with one head a thread and 4.0 with four, 4.4 and 4.6 for 256, but 5.0 and 4.9 for
+// 512, 10.8 and 8.5 for 3 x 512 (medians of a profiled run; calls in a row 10.0 and 8.4).
 //
 // Bound by HBM for many tokens: 335 MB in and out in 56 us, 6.0 TB/s (interleaved
 // pairs out of a projection's [B, L, H, D] 61), by the launch for few (8 tokens: 3.4 us, a
 // kernel that does nothing 2).  Calls with 64 MB of outputs or more, which leave the
-// caches before anybody reads them, are streamed past them: 63 us without, and
-// fp32 70 against 66 (at 67 MB the same, 26.5).  Not where neighbouring loads share
-// lines, which then are fetched again (nearly twice the time for a part of 24 dims).
+// caches before anybody reads them, are streamed past them: 63 us without, 8192 tokens
+// 34.1 against 29.3, 2 x 4096 of fp32 70.8 against 65.9 (but 4096 tokens, 42 MB, 14.2 and 16.1
+// streamed).  Not where neighbouring loads share lines, which then are fetched again: 4 x
+// 4096 tokens of 32 heads of 64, in halves of 64 bytes, 26.4 and 32.0 streamed.
 
 #include "kernel_common.h"
 #include "launch.h"
