@@ -28,8 +28,8 @@
  * the host: lengths are clamped to what the table can hold, a page outside the
  * cache is never read or written, and its tokens count as masked.  What a call
  * on the cache writes (kv4_append: the cache; kv4_load: K and V; attn_decode_kv4:
- * O and the workspace) shares memory with nothing else that it is given:
- * ATTN_ERR_SHAPE.
+ * O and the workspace) shares memory with nothing else that it is given, but that O
+ * may be Q itself: ATTN_ERR_SHAPE.
  */
 #ifndef KV4_H
 #define KV4_H

@@ -804,8 +804,8 @@ def attn_decode_kv4(q, cache, table, lens, o=None, *, scale=None, alibi_slopes=N
     max_pages], ``lens`` int32 [B].  ``scale`` defaults to 1/sqrt(D);
     ``alibi_slopes`` and ``softcap`` as for attn_decode.  ``workspace`` (uint8
     GPU tensor of attn_decode_kv4_workspace_bytes) is allocated when not given;
-    neither it nor ``o`` may share memory with another operand.  Returns ``o``
-    [B, Hq, 1, D], 0 for a sequence that sees nothing.
+    neither it nor ``o`` may share memory with another operand, but ``o`` may be
+    q itself.  Returns ``o`` [B, Hq, 1, D], 0 for a sequence that sees nothing.
     """
     r = (_BINDING or _load_binding()).attn_decode_kv4(q, cache, table, lens, o, scale, alibi_slopes, softcap, window,
                                                       workspace, stream)

@@ -253,7 +253,9 @@ int attn_decode_kv4(const void* Q, const void* cache, const int* table, const in
   const Span ws = span(workspace, (int64_t)need);
   const Span in[] = {span(Q, heads), span(cache, cache_bytes(pages, Hkv, page, D)), span(table, 4LL * B * max_pages),
                      span(lens, 4LL * B), span(alibi_slopes, 4LL * Hq)};
-  if (!apart(span(O, heads), {ws, in[0], in[1], in[2], in[3], in[4]}) || !apart(ws, {in[0], in[1], in[2], in[3], in[4]}))
+  // In place: a query head's output is written when all that read its query are done.
+  if ((O != Q && !apart(span(O, heads), {in[0]})) || !apart(span(O, heads), {ws, in[1], in[2], in[3], in[4]}) ||
+      !apart(ws, {in[0], in[1], in[2], in[3], in[4]}))
     return ATTN_ERR_SHAPE;
   attn::Kv4DecodeParams p{};
   p.q = Q; p.cache = static_cast<const unsigned char*>(cache); p.table = table; p.lens = lens; p.o = O;

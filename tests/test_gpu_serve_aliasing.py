@@ -10,6 +10,11 @@ from paper_2510_08726_amd.workloads import random_tensors
 pytestmark = pytest.mark.gpu
 
 
+def _shifted(q):
+    """A tensor of one sequence that begins eight elements into q."""
+    return q.view(-1)[8:8 + q[:1].numel()].view(q[:1].shape)
+
+
 @pytest.mark.parametrize("path", ["marshalled", "checked"])
 def test_neighbours_and_common_memory(monkeypatch, path):
     if path == "checked":
@@ -31,12 +36,31 @@ def test_neighbours_and_common_memory(monkeypatch, path):
     assert torch.equal(both[0], a) and torch.equal(both[1], b)
     pair = torch.stack((q, torch.zeros_like(q)))
     assert torch.equal(pa.attn_decode_kv4(pair[0], cache, table, lens, pair[1]), o)
+    mine = q.clone()
+    assert pa.attn_decode_kv4(mine, cache, table, lens, mine) is mine and torch.equal(mine, o)     # in place
 
     far = torch.zeros(3 * cache.numel(), dtype=torch.uint8, device="cuda")
     shared, rows = far[:cache.numel()].view(cache.shape), far[:2 * a.numel()].view(torch.float16).view(a.shape)
     for call in (lambda: pa.kv4_load(cache, table, lens, L, D, torch.float16, a, a),
                  lambda: pa.kv4_load(shared, table, lens, L, D, torch.float16, rows, b),
-                 lambda: pa.kv4_append(rows, v, shared, slots), lambda: pa.attn_decode_kv4(q, cache, table, lens, q)):
+                 lambda: pa.kv4_append(rows, v, shared, slots),
+                 lambda: pa.attn_decode_kv4(q[:1], cache, table[:1], lens[:1], _shifted(q))):
         with pytest.raises(pa.AttnError) as e:
             call()
         assert e.value.status == pa.ATTN_ERR_SHAPE
+
+
+@pytest.mark.parametrize("Hq,Hkv,lens", [(8, 2, [5000, 0, 33, 1, 900]), (40, 1, [4000, 4000]), (64, 64, [17] * 40)])
+def test_decode_in_place(Hq, Hkv, lens):
+    """Rows in one share, in many, and without tokens."""
+    D, page, B, M = 128, 64, len(lens), 80
+    cache = torch.randint(0, 120, (B * M, Hkv, pa.kv4_page_bytes(page, D)), dtype=torch.uint8,
+                          generator=torch.Generator().manual_seed(3)).cuda()
+    table = torch.arange(B * M, dtype=torch.int32, device="cuda").view(B, M)
+    n = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    q, = random_tensors([(B, Hq, 1, D)], "bf16", 4, device="cuda")
+    o = pa.attn_decode_kv4(q, cache, table, n)
+    for _ in range(10):
+        mine = q.clone()
+        pa.attn_decode_kv4(mine, cache, table, n, mine)
+        assert torch.equal(mine, o)

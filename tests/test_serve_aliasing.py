@@ -84,7 +84,7 @@ def decode(lib, **at):
 
 
 @pytest.mark.parametrize("at", [
-    dict(o=("q", 0)), dict(o=("q", QO - 16)), dict(q=("o", QO - 16)), dict(o=("cache", CACHE - 16)), dict(o=("table", 0)),
+    dict(o=("q", 16)), dict(o=("q", QO - 16)), dict(q=("o", QO - 16)), dict(o=("cache", CACHE - 16)), dict(o=("table", 0)),
     dict(lens=("o", QO - 4)), dict(slopes=("o", 4)), dict(o=("ws", 0)), dict(ws=("o", QO - 16)), dict(ws=("cache", 16)),
     dict(q=("ws", 4096)), dict(table=("ws", 64)), dict(lens=("ws", 4)), dict(slopes=("ws", 8)),
 ], ids=str)
