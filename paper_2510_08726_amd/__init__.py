@@ -26,6 +26,7 @@ __all__ = [
     "attn_decode_kernels",
     "rope_frequencies", "rope_fwd", "rope_bwd", "kv4_page_bytes", "kv_slots", "kv4_append", "kv4_load",
     "attn_decode_kv4", "attn_decode_kv4_workspace_bytes",
+    "attn_fwd_lse", "attn_bwd", "attn_bwd_workspace_bytes",
     "attn_status_string", "attn_last_hip_error", "library_path", "load_library", "AttnError",
     "ATTN_OK", "ATTN_ERR_NULL", "ATTN_ERR_SHAPE", "ATTN_ERR_UNSUPPORTED", "ATTN_ERR_WORKSPACE",
     "ATTN_ERR_HIP",
@@ -135,6 +136,12 @@ def load_library():
     lib.attn_decode_kv4_workspace_bytes.restype = cs
     lib.attn_decode_kv4.argtypes = [vp, vp, vp, vp, vp, ci, ci, ci, ci, ci, ci, ci, cf, vp, cf, ci, vp, cs, ci, vp]
     lib.attn_decode_kv4.restype = ci
+    lib.attn_fwd_lse.argtypes = [vp, vp, vp, vp, vp, ci, ci, ci, ci, ci, ci, ci, cf, vp, cf, ci, ci, vp]
+    lib.attn_fwd_lse.restype = ci
+    lib.attn_bwd_workspace_bytes.argtypes = [ci] * 8
+    lib.attn_bwd_workspace_bytes.restype = cs
+    lib.attn_bwd.argtypes = [vp] * 10 + [ci] * 7 + [cf, vp, cf, ci, vp, cs, ci, vp]
+    lib.attn_bwd.restype = ci
     lib.attn_status_string.argtypes = [ci]
     lib.attn_status_string.restype = ctypes.c_char_p
     lib.attn_last_hip_error.argtypes = []
@@ -153,6 +160,7 @@ class _NotBuilt:
 
     attn_fwd = attn_decode = attn_decode_noalloc = norm_l2 = rmsnorm_rowmax = _none
     rope = kv_slots = kv4_append = kv4_load = attn_decode_kv4 = _none
+    attn_fwd_lse = attn_bwd = _none
 
 
 def _load_binding():
@@ -844,6 +852,112 @@ def attn_decode_kv4(q, cache, table, lens, o=None, *, scale=None, alibi_slopes=N
                                               _ptr(workspace), workspace.numel() * workspace.element_size(),
                                               _DTYPE_CODE[q.dtype], _stream(stream)))
     return o
+
+
+# Attention in training: the forward pass with its rows' log-sum-exp, and the backward pass.
+
+def _train_args(q, k, v, alibi_slopes):
+    for name, t in (("q", q), ("k", k), ("v", v)):
+        _require(t.dim() == 4 and t.is_contiguous(), f"{name} must be contiguous [B, H, L, D]")
+    _same_device(q, k=k, v=v)
+    _require(q.dtype == k.dtype == v.dtype and q.dtype in _DTYPE_CODE, "q, k, v must share one dtype, float16 or bfloat16")
+    B, Hq, Lq, D = q.shape
+    _require(k.shape == v.shape and k.shape[0] == B and k.shape[3] == D,
+             "k and v must have the same shape, and q's batch and head dim")
+    if alibi_slopes is not None:
+        _same_device(q, alibi_slopes=alibi_slopes)
+        _require(alibi_slopes.dtype == torch.float32 and alibi_slopes.is_contiguous() and alibi_slopes.numel() == Hq,
+                 "alibi_slopes must be a contiguous float32 tensor with one value per query head")
+    return B, Hq, k.shape[1], Lq, k.shape[2], D
+
+
+def _train_mod(D, scale, softcap, window):
+    win = min(int(window or 0), _INT_MAX)            # (that many see every key)
+    _require(win >= 0, "window must be at least 1")
+    return 1.0 / math.sqrt(D) if scale is None else float(scale), float(softcap or 0.0), win
+
+
+def _given(name, t, like, stream, shape=None, dtype=None):
+    """An output: allocated, or the one that the caller gave, which has to be laid out like it."""
+    shape, dtype = tuple(like.shape) if shape is None else tuple(shape), dtype or like.dtype
+    if t is None:
+        return _allocate(shape, like, stream, dtype)
+    _same_device(like, **{name: t})
+    _require(tuple(t.shape) == shape and t.dtype == dtype and t.is_contiguous(),
+             f"{name} must be a contiguous {str(dtype)[6:]} tensor of shape {list(shape)}")
+    return t
+
+
+def attn_fwd_lse(q, k, v, o=None, lse=None, *, causal=False, scale=None, alibi_slopes=None, softcap=None, window=None,
+                 stream=None):
+    """attn_fwd that also gives each row's log-sum-exp, for attn_bwd.
+
+    q [B, Hq, Lq, D], k and v [B, Hkv, Lk, D] and the other arguments as for
+    attn_fwd; ``softcap`` at most 1024.  ``lse`` [B, Hq, Lq] float32: log sum_j
+    exp(s_ij) of the row's scores (scaled, capped, with the bias), -inf for a row
+    that sees no key.  Neither output may share memory with another operand.
+    Nothing is recorded for autograd: a program that trains calls attn_bwd.
+    Returns (o, lse).
+    """
+    r = (_BINDING or _load_binding()).attn_fwd_lse(q, k, v, o, lse, causal, scale, alibi_slopes, softcap, window, stream)
+    if r is not None:
+        return _result(r)
+    B, Hq, Hkv, Lq, Lk, D = _train_args(q, k, v, alibi_slopes)
+    sc, cap, win = _train_mod(D, scale, softcap, window)
+    stream = _on_device(q, stream)
+    o = _given("o", o, q, stream)
+    lse = _given("lse", lse, q, stream, (B, Hq, Lq), torch.float32)
+    with torch.cuda.device(q.device):
+        _check(load_library().attn_fwd_lse(_ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse), B, Hq, Hkv, Lq, Lk, D,
+                                           int(bool(causal)), sc, _ptr(alibi_slopes), cap, win, _DTYPE_CODE[q.dtype],
+                                           _stream(stream)))
+    return o, lse
+
+
+def attn_bwd_workspace_bytes(B, Hq, Hkv, Lq, Lk, D, causal=False, window=None):
+    sizes = (B, Hq, Hkv, Lq, Lk, D, min(int(window or 0), _INT_MAX))
+    return load_library().attn_bwd_workspace_bytes(*sizes[:6], int(bool(causal)), sizes[6]) if _fits(*sizes) else 0
+
+
+def attn_bwd(do, q, k, v, o, lse, dq=None, dk=None, dv=None, *, causal=False, scale=None, alibi_slopes=None,
+             softcap=None, window=None, workspace=None, stream=None):
+    """Gradients of attention's q, k and v from ``do``, that of its output.
+
+    ``o`` and ``lse`` are attn_fwd_lse's of the same q, k, v and arguments; the
+    probabilities are recomputed.  ``do`` [B, Hq, Lq, D] may be a strided view
+    with contiguous rows (a [B, Lq, Hq, D] transposed), strides multiples of 8.
+    dk and dv [B, Hkv, Lk, D] are summed over the query heads of each KV head; alibi_slopes get
+    no gradient.  ``workspace`` (uint8 GPU tensor of attn_bwd_workspace_bytes) is
+    allocated when not given; neither it nor an output may share memory with
+    another operand.  Returns (dq, dk, dv).
+    """
+    r = (_BINDING or _load_binding()).attn_bwd(do, q, k, v, o, lse, dq, dk, dv, causal, scale, alibi_slopes, softcap, window,
+                                               workspace, stream)
+    if r is not None:
+        return _result(r)
+    B, Hq, Hkv, Lq, Lk, D = _train_args(q, k, v, alibi_slopes)
+    sc, cap, win = _train_mod(D, scale, softcap, window)
+    _same_device(q, do=do, o=o, lse=lse)
+    _rows("do", do, q.shape)
+    _require(do.dtype == q.dtype, "do must have q's dtype")
+    _require(o.shape == q.shape and o.dtype == q.dtype and o.is_contiguous(), "o must be a contiguous tensor like q")
+    _ints("lse", lse, torch.float32, (B, Hq, Lq))
+    stream = _on_device(q, stream)
+    dq, dk, dv = _given("dq", dq, q, stream), _given("dk", dk, k, stream), _given("dv", dv, v, stream)
+    if workspace is None:
+        _require(isinstance(stream, torch.cuda.Stream), "a stream of this kind needs a workspace of the caller's")
+        with torch.cuda.device(q.device):            # whose compute units the size counts
+            size = attn_bwd_workspace_bytes(B, Hq, Hkv, Lq, Lk, D, causal, win)
+        workspace = _allocate((max(size, 16),), q, stream, torch.uint8)
+    _same_device(q, workspace=workspace)
+    _require(workspace.is_contiguous(), "workspace must be contiguous")
+    with torch.cuda.device(q.device):
+        _check(load_library().attn_bwd(_ptr(do), _strides(do), _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse), _ptr(dq),
+                                       _ptr(dk), _ptr(dv), B, Hq, Hkv, Lq, Lk, D, int(bool(causal)), sc,
+                                       _ptr(alibi_slopes), cap, win, _ptr(workspace),
+                                       workspace.numel() * workspace.element_size(), _DTYPE_CODE[q.dtype],
+                                       _stream(stream)))
+    return dq, dk, dv
 
 
 def norm_partials(workspace, N, chunks):

@@ -37,8 +37,9 @@ HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 LLVM_DIS = "/opt/rocm/llvm/bin/llvm-dis"
 # AGPRs reserved for the prefill kernels' fixed operands, in the allocation
 # granularity of 4, per shard: D = 128 (shards 0, 1) uses a0..a101, D = 64
-# (shards 2, 3) a0..a53.
-PREFILL_AGPRS = {0: 104, 1: 104, 2: 56, 3: 56}
+# (shards 2, 3) a0..a53; shards 4 to 7, the same kernels with the rows'
+# log-sum-exp, a0..a95 and a0..a47.
+PREFILL_AGPRS = {0: 104, 1: 104, 2: 56, 3: 56, 4: 96, 5: 96, 6: 48, 7: 48}
 ARCH = "gfx950"
 COMMON = ["-O3", "-std=c++20", "-fPIC", "-I", INCLUDE, "-I", CSRC]
 DEVICE = ["-x", "hip", f"--offload-arch={ARCH}", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
@@ -50,12 +51,14 @@ DEVICE = ["-x", "hip", f"--offload-arch={ARCH}", "-Xclang", "-target-feature", "
 # canonicalising both inputs first.  The prefill device assembly is kept
 # (-save-temps) for the ISA hazard check in the tests.
 UNITS = [(f"prefill{k}", "prefill.hip", ["-fno-honor-nans", f"-DATTN_PREFILL_SHARD={k}", "-save-temps"])
-         for k in range(4)] + [("decode", "decode.hip", ["-save-temps"]), ("peaks", "peaks.hip", ["-save-temps"]),
+         for k in range(8)] + [("decode", "decode.hip", ["-save-temps"]), ("peaks", "peaks.hip", ["-save-temps"]),
             ("norms", "norms.hip", ["-save-temps"]),
             ("prefill_split", "prefill_split.hip", ["-fno-honor-nans", "-save-temps"]),
             ("rope", "rope.hip", ["-save-temps"]), ("kv4", "kv4.hip", ["-save-temps"]),
             ("decode_kv4", "decode_kv4.hip", ["-save-temps"]),
-            ("attn_api", "attn_api.cpp", []), ("serve_api", "serve_api.cpp", [])]
+            ("attn_bwd", "attn_bwd.hip", ["-save-temps"]),
+            ("attn_api", "attn_api.cpp", []), ("serve_api", "serve_api.cpp", []),
+            ("train_api", "train_api.cpp", [])]
 
 
 def unit_dir(name):

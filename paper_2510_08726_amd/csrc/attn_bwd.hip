@@ -1,0 +1,699 @@
+// Attention's backward pass for gfx950 (include/attn_bwd.h).  With the scores
+// s = mod(scale q k^T) + bias and each row's log-sum-exp from the forward pass,
+//
+//   P = exp(s - lse)                  recomputed, never in memory
+//   dV = P^T dO
+//   dS = P (dO V^T - delta) mod'(s) scale,   delta_i = dO_i . O_i
+//   dQ = dS K,  dK = dS^T Q           dK and dV summed over the query heads of a KV head
+//
+// Three kernels, without atomics, so that a call's bits do not depend on timing:
+//   bwd_rows_kernel  what a row brings into its scores: (delta, lse), once
+//   bwd_dkv_kernel   a workgroup owns 128 keys and streams the tiles of 32 queries that see them
+//   bwd_dq_kernel    a workgroup owns 128 query rows and streams the tiles of 32 keys
+// The last two each form S and dP, seven products in the place of five.  (One loop for
+// both would need the partial dQ of every key block in memory, 1 KB a row and block of 256 keys
+// against 131 kflop saved: no less time at this card's rates, and a sum over blocks.)
+//
+// A wave owns 32 keys (or rows) for the whole loop, 32x32x16 MFMAs with fp32
+// accumulators in registers; Q and dO (or K and V) tiles pass through LDS, swizzled
+// as prefill.hip's, filled by buffer loads that write LDS directly.  The products
+// are arranged so that the lane is the wave's own index (key or row): S and dP come out in the
+// layout in which P and dS go into the second products, in registers alone.
+//
+// Rounding.  P and dS go to the matrix unit in the type of Q: 2^-9 (bf16) or 2^-12 (fp16) relative to
+// each, as much as the outputs' own rounding.  Sums are in fp32.  fp16 holds 5
+// exponent bits, and both get small in long rows (dS also with the loss's scale), so there P is
+// held times 2^15 and dS times a power of two from a bound on |dO| |V| of its KV head
+// (bwd_scale), taken out of the fp32 sums at the end.
+
+#include <algorithm>
+#include <type_traits>
+
+#include "kernel_common.h"
+#include "launch.h"
+
+namespace attn {
+
+namespace {
+
+constexpr int kWaves = 4;
+constexpr int kThreads = 64 * kWaves;
+constexpr int TN = 32;                  // rows of a streamed tile, and of a wave's own block
+constexpr int BLK = TN * kWaves;        // keys (rows) that a workgroup owns
+constexpr int kXcds = 8;
+constexpr int kRowsBlock = 64;          // rows of a workgroup of bwd_rows_kernel
+constexpr int kShift = 15;              // fp16: P is held times 2^kShift
+
+template <typename T> constexpr bool is_half = std::is_same_v<T, _Float16>;
+
+// A tile of 32 rows of D 16-bit values in LDS, 16-byte chunks swizzled (swz).
+template <int D, typename T>
+struct Tile {
+  typedef typename Elem<T>::vec8 vec8;
+  static constexpr int BYTES = TN * D * 2;
+  static constexpr int NBLK = BYTES / 1024;     // 1 KB copies
+  static constexpr int CPR = D / 8;             // 16-byte chunks of a row
+  static constexpr int KX = D / 16;             // MFMA steps over D
+  static constexpr int DB = D / 32;             // 32-dim blocks
+  // Operand with the rows along M (or N) and the dims along K, step kx: lane (n, hh)
+  // reads row n, dims 16 kx + 8 hh ..: the lane's offset for step 0; step kx is at its xor with 32 kx.
+  static __device__ __forceinline__ int row_offset(int lane) {
+    const int n = lane & 31, hh = lane >> 5;
+    return 2 * n * D + 16 * (hh ^ swz<D>(n));
+  }
+  static __device__ __forceinline__ vec8 rows(const char* tile, int off, int kx) {
+    return __builtin_bit_cast(vec8, *reinterpret_cast<const u32x4*>(tile + (off ^ (32 * kx))));
+  }
+  // Operand with the dims along M and the rows along K: block db, rows 16 c16 ..:
+  // lane (m, hh) receives rows 16 c16 + 4 hh + 0..3 and 16 c16 + 8 + 4 hh + 0..3 of dim 32 db + m, the
+  // order in which an accumulator of 32 rows by 32 holds them.
+  static __device__ __forceinline__ int dim_offset(int lane) {
+    const int G = lane >> 4, i = lane & 15;
+    const int d = 16 * (G & 1) + 4 * (i & 3), k = 4 * (G >> 1) + (i >> 2);
+    return 2 * k * D + 16 * ((d >> 3) ^ swz<D>(k)) + 2 * (d & 7);
+  }
+  static __device__ __forceinline__ vec8 dims(const char* tile, int off, int c16, int db) {
+    const char* at = tile + c16 * 32 * D;
+    const uint2 lo = lds_read_tr(at + (off ^ (64 * db)));
+    const uint2 hi = lds_read_tr(at + 16 * D + (off ^ (64 * db) ^ 32));
+    return __builtin_bit_cast(vec8, make_uint4(lo.x, lo.y, hi.x, hi.y));
+  }
+};
+
+// Rows of an accumulator: register r of lane (n, hh) is row kconst(r) + 4 hh of column n.
+constexpr __host__ __device__ int kconst(int r) { return 8 * (r / 4) + r % 4; }
+
+__device__ __forceinline__ u32x4 resource(const void* base, unsigned bytes) {
+  const uint64_t a = reinterpret_cast<uint64_t>(base);
+  return u32x4{(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)a),
+               (uint32_t)__builtin_amdgcn_readfirstlane((int)((uint32_t)(a >> 32) & 0xffffu)),
+               (uint32_t)__builtin_amdgcn_readfirstlane((int)bytes), 0x00020000u};
+}
+
+// 16 (or 4) bytes a lane from `off` of a resource to LDS address dst + 16 (4) lane;
+// past the resource's end zeros.
+__device__ __forceinline__ void copy16(const u32x4& rs, uint32_t dst, int off) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+               : : "s"(dst), "v"(off), "s"(rs) : "memory", "m0");
+}
+__device__ __forceinline__ void copy4(const u32x4& rs, uint32_t dst, int off) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds"
+               : : "s"(dst), "v"(off), "s"(rs) : "memory", "m0");
+}
+
+template <typename T>
+__device__ __forceinline__ typename Elem<T>::vec8 load8(const T* at, unsigned sign = 0) {
+  u32x4 w = *reinterpret_cast<const u32x4*>(at);
+  w ^= sign;
+  return __builtin_bit_cast(typename Elem<T>::vec8, w);
+}
+
+// 32 x 32 weights of a wave as two operands of 16 rows.
+template <typename T>
+struct Weights {
+  uint32_t w[2][4];
+  __device__ __forceinline__ void set(int r, float a, float b) { w[r / 8][(r % 8) / 2] = Elem<T>::pack2(a, b); }
+  __device__ __forceinline__ typename Elem<T>::vec8 operand(int c16) const {
+    return __builtin_bit_cast(typename Elem<T>::vec8, make_uint4(w[c16][0], w[c16][1], w[c16][2], w[c16][3]));
+  }
+};
+
+// SoftCap of a score x: the exponent of its weight, cap tanh(s / cap) log2 e + add,
+// and the derivative of the cap, 1 - tanh^2 = 4 r (1 - r) with r = 1 / (1 + e^2t).
+__device__ __forceinline__ float capped(float x, const BwdParams& p, float add, float& slope) {
+  const float r = __builtin_amdgcn_rcpf(1.f + fast_exp2(x * p.cap_k2));
+  slope = 4.f * r * (1.f - r);
+  return __builtin_fmaf(-2.f * p.cap_cl, r, p.cap_cl + add);
+}
+
+// What item of `n` a workgroup takes: an XCD a contiguous share (workgroup g runs on XCD g mod
+// 8), so that those that read the same rows share its L2; -1 for none.
+__device__ __forceinline__ int item_of(int n, bool shares) {
+  const int g = blockIdx.x;
+  if (!shares) return g < n ? g : -1;
+  const int x = g % kXcds;
+  const int s0 = (int)((long long)n * x / kXcds), s1 = (int)((long long)n * (x + 1) / kXcds);
+  const int i = s0 + g / kXcds;
+  return i < s1 ? i : -1;
+}
+
+// fp16: the power of two that dS is held times, as an exponent: |dS| <= 2 |dO| |V| of the
+// largest rows of the KV head stays below 2^15.  The workgroup's threads each look at a part of the rows'
+// largest squares.
+template <typename T>
+__device__ __forceinline__ int bwd_scale(const BwdParams& p, int unit, float* shared) {
+  if constexpr (!is_half<T>) return 0;
+  const int nq = p.group * p.row_blocks, nk = p.key_blocks;
+  const float* a = p.peaks + (size_t)unit * nq;
+  const float* b = p.peaks + (size_t)p.B * p.Hq * p.row_blocks + (size_t)unit * nk;
+  float x = 0.f, y = 0.f;
+  for (int i = threadIdx.x; i < nq; i += kThreads) x = fmaxf(x, a[i]);
+  for (int i = threadIdx.x; i < nk; i += kThreads) y = fmaxf(y, b[i]);
+#pragma unroll
+  for (int m = 32; m > 0; m >>= 1) {
+    x = fmaxf(x, __shfl_xor(x, m, 64));
+    y = fmaxf(y, __shfl_xor(y, m, 64));
+  }
+  if ((threadIdx.x & 63) == 0) {
+    shared[threadIdx.x / 64] = x;
+    shared[kWaves + threadIdx.x / 64] = y;
+  }
+  __syncthreads();
+  for (int w = 0; w < kWaves; ++w) {
+    x = fmaxf(x, shared[w]);
+    y = fmaxf(y, shared[kWaves + w]);
+  }
+  __syncthreads();
+  const float bound = 2.02f * __builtin_sqrtf(x) * __builtin_sqrtf(y);
+  if (!(bound > 0.f && bound < 3e38f)) return 0;
+  return __builtin_amdgcn_readfirstlane(min(max(14 - __builtin_amdgcn_frexp_expf(bound), -100), 100));
+}
+
+// A row's part of its scores and of dP, in tiles of 32 rows: [B Hq, tiles, 64] floats,
+// first what is added to a score before its exponential, (2^15's exponent - lse log2 e - the ALiBi bias of
+// the row within its tile) over the scale, so that it starts the accumulator of Q K^T (with
+// SoftCap: not over the scale); then -delta, which starts that of dO V^T.  fp16: the largest square sums of
+// the rows of dO and V in each block of 64.  Rows that see no key (the first Lq - Lk with the causal mask)
+// take no part: their dQ is zero.  One pass over dO and O: bound by memory.
+template <int D, typename T>
+__global__ __launch_bounds__(kThreads) void bwd_rows_kernel(BwdParams p) {
+  constexpr int LANES = D / 8, RPP = kThreads / LANES;     // lanes of a row, rows of a pass
+  __shared__ float top[kWaves];
+  const int lane = threadIdx.x % LANES, sub = threadIdx.x / LANES;
+  const int nheads = p.B * p.Hq, nkv = p.B * p.Hkv;
+  int blk = blockIdx.x;
+  float peak = 0.f;
+  float* peak_at = nullptr;
+  if (blk < nheads * p.row_blocks) {
+    const int head = blk / p.row_blocks, b = head / p.Hq, h = head - b * p.Hq;
+    const int i0 = (blk - head * p.row_blocks) * kRowsBlock;
+    peak_at = p.peaks + blk;
+    const float sl2 = p.slopes ? p.slopes[h] * kLog2e : 0.f;
+    const T* og = reinterpret_cast<const T*>(p.o) + ((size_t)head * p.Lq + p.row0) * D + 8 * lane;
+    const T* dg = reinterpret_cast<const T*>(p.d_o) + b * p.do_sb + h * p.do_sh + p.row0 * p.do_sl + 8 * lane;
+#pragma unroll
+    for (int u = 0; u < kRowsBlock / RPP; ++u) {
+      const int i = i0 + u * RPP + sub, row = min(i, p.rows - 1);
+      const u32x4 x = *reinterpret_cast<const u32x4*>(og + (size_t)row * D);
+      const u32x4 y = *reinterpret_cast<const u32x4*>(dg + (int64_t)row * p.do_sl);
+      float dot = 0.f, sq = 0.f;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const unsigned xw = x[k], yw = y[k];
+        const float ylo = Elem<T>::lo(yw), yhi = Elem<T>::hi(yw);
+        dot = __builtin_fmaf(ylo, Elem<T>::lo(xw), dot);
+        dot = __builtin_fmaf(yhi, Elem<T>::hi(xw), dot);
+        if (is_half<T>) sq = __builtin_fmaf(ylo, ylo, __builtin_fmaf(yhi, yhi, sq));
+      }
+#pragma unroll
+      for (int m = LANES / 2; m > 0; m >>= 1) {
+        dot += __shfl_xor(dot, m, 64);
+        if (is_half<T>) sq += __shfl_xor(sq, m, 64);
+      }
+      peak = fmaxf(peak, sq);
+      if (lane == 0 && i < p.row_tiles * TN) {
+        float start = kNegInf, nd = 0.f;
+        if (i < p.rows) {
+          const float lse = p.lse[(size_t)head * p.Lq + p.row0 + i];
+          float e = (is_half<T> ? (float)kShift : 0.f) - lse * kLog2e;
+          if (p.cap_cl == 0.f) e = (e - sl2 * (float)(i % TN)) / p.c;
+          start = lse == kNegInf ? kNegInf : e;
+          nd = -dot;
+        }
+        float* at = p.stats + ((size_t)head * p.row_tiles + i / TN) * (2 * TN) + i % TN;
+        at[0] = start;
+        at[TN] = nd;
+      }
+    }
+  } else if (is_half<T> && (blk -= nheads * p.row_blocks) < nkv * p.key_blocks) {
+    const int unit = blk / p.key_blocks, j0 = (blk - unit * p.key_blocks) * kRowsBlock;
+    peak_at = p.peaks + (size_t)nheads * p.row_blocks + blk;
+    const T* vg = reinterpret_cast<const T*>(p.v) + (size_t)unit * p.Lk * D + 8 * lane;
+#pragma unroll
+    for (int u = 0; u < kRowsBlock / RPP; ++u) {
+      const u32x4 y = *reinterpret_cast<const u32x4*>(vg + (size_t)min(j0 + u * RPP + sub, p.Lk - 1) * D);
+      float sq = 0.f;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const unsigned yw = y[k];
+        const float ylo = Elem<T>::lo(yw), yhi = Elem<T>::hi(yw);
+        sq = __builtin_fmaf(ylo, ylo, __builtin_fmaf(yhi, yhi, sq));
+      }
+#pragma unroll
+      for (int m = LANES / 2; m > 0; m >>= 1) sq += __shfl_xor(sq, m, 64);
+      peak = fmaxf(peak, sq);
+    }
+  } else {
+    if (is_half<T>) blk -= nkv * p.key_blocks;
+    else blk -= nheads * p.row_blocks;
+    const int per = (p.row0 + kRowsBlock - 1) / kRowsBlock;
+    const int head = blk / per, i0 = (blk - head * per) * kRowsBlock;
+    T* at = reinterpret_cast<T*>(p.dq) + (size_t)head * p.Lq * D + 8 * lane;
+    for (int i = i0 + sub; i < min(i0 + kRowsBlock, p.row0); i += RPP)
+      *reinterpret_cast<u32x4*>(at + (size_t)i * D) = u32x4{0u, 0u, 0u, 0u};
+    return;
+  }
+  if constexpr (is_half<T>) {
+#pragma unroll
+    for (int m = 32; m > 0; m >>= 1) peak = fmaxf(peak, __shfl_xor(peak, m, 64));
+    if ((threadIdx.x & 63) == 0) top[threadIdx.x / 64] = peak;
+    __syncthreads();
+    if (threadIdx.x == 0) *peak_at = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+  }
+}
+
+// Store a wave's transposed accumulators (register r of block db, lane (n, hh): dim
+// 32 db + kconst(r) + 4 hh of row n), times f: rounded, or as a partial in fp32.
+template <int D, typename T>
+__device__ __forceinline__ void store(const f32x16 (&acc)[D / 32], float f, T* out, float* part, int hh) {
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const int d = 32 * db + 8 * g + 4 * hh;
+      const f32x4 v = {acc[db][4 * g] * f, acc[db][4 * g + 1] * f, acc[db][4 * g + 2] * f, acc[db][4 * g + 3] * f};
+      if (part) *reinterpret_cast<f32x4*>(part + d) = v;
+      else *reinterpret_cast<uint2*>(out + d) = make_uint2(Elem<T>::pack2(v[0], v[1]), Elem<T>::pack2(v[2], v[3]));
+    }
+}
+
+// Stages of a workgroup's ring (a tile pair and 64 floats each): two workgroups
+// share a compute unit's 160 KB.
+constexpr int kStages = 4;
+
+// dK and dV of 128 keys of a KV head: the tiles of 32 queries that see them, of all query heads of
+// the group, or the share `part` of them (partials in fp32, summed by bwd_sum_kernel).
+template <int D, typename T, bool CAUSAL, bool ALIBI, bool CAP>
+__global__ __launch_bounds__(kThreads, 2) void bwd_dkv_kernel(BwdParams p) {
+  typedef Elem<T> E;
+  typedef Tile<D, T> TL;
+  typedef typename E::vec8 vec8;
+  constexpr int TB = TL::BYTES, STAGE = 2 * TB + 256, CPR = TL::CPR;
+  constexpr int CB = TL::NBLK / kWaves;            // 1 KB copies of a tile that a wave makes
+  constexpr int CPW = 2 * CB + 1;                  // copies in flight of a stage
+  static_assert(CB >= 1, "a tile's copies divide over the waves");
+  __shared__ __attribute__((aligned(1024))) char lds[kStages * STAGE];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int n = lane & 31, hh = lane >> 5;
+
+  const int units = p.B * p.Hkv, nkb = (p.Lk + BLK - 1) / BLK, S = p.dkv_parts;
+  const int item = item_of(units * nkb * S, p.shares);
+  if (item < 0) return;
+  // Key blocks in order: the first ones see the most queries.
+  int unit, kb, part;
+  if (p.shares) {
+    unit = item / (nkb * S);
+    kb = item / S - unit * nkb;
+    part = item % S;
+  } else {
+    kb = item / (units * S);
+    unit = item / S - kb * units;
+    part = item % S;
+  }
+  const int b = unit / p.Hkv, h0 = (unit - b * p.Hkv) * p.group;   // batch and first query head
+  const int rows = p.rows, off = p.Lk - rows, W = p.window;
+  const int j0 = kb * BLK, jw = j0 + TN * wave;
+  // The queries that see keys [j0, j0 + 128): tiles [ta, ta + nt) of each head.
+  int ilo = 0, ihi = rows;
+  if (CAUSAL) {
+    ilo = max(0, j0 - off);
+    if (W > 0) ihi = min(rows, min(j0 + BLK, p.Lk) - off + W - 1);
+  }
+  const int ta = ilo / TN, nt = ihi > ilo ? (ihi + TN - 1) / TN - ta : 0;
+  const int total = nt * p.group;
+  const int u0 = (int)((long long)total * part / S), u1 = (int)((long long)total * (part + 1) / S);
+
+  const int key = jw + n, krow = min(key, p.Lk - 1);
+  int scale_exp = 0;
+  if (is_half<T>) scale_exp = bwd_scale<T>(p, unit, reinterpret_cast<float*>(lds));
+
+  // K and V of the wave's keys: lane (n, hh) holds key n, dims 16 kx + 8 hh ...  (A negative scale: K
+  // negated, which only the scores see.)
+  vec8 kf[TL::KX], vf[TL::KX];
+  {
+    const T* kg = reinterpret_cast<const T*>(p.k) + ((size_t)unit * p.Lk + krow) * D + 8 * hh;
+    const T* vg = reinterpret_cast<const T*>(p.v) + ((size_t)unit * p.Lk + krow) * D + 8 * hh;
+#pragma unroll
+    for (int kx = 0; kx < TL::KX; ++kx) {
+      kf[kx] = load8(kg + 16 * kx, p.sign);
+      vf[kx] = load8(vg + 16 * kx);
+    }
+  }
+
+  // Copies: this wave's blocks of the Q and dO tiles and, every wave alike, the tile's 64 floats.
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_void*)lds;
+  int qoff[CB], goff[CB];
+#pragma unroll
+  for (int u = 0; u < CB; ++u) {
+    const int r = (wave * CB + u) * (1024 / (2 * D)) + lane / CPR;
+    const int c = 8 * ((lane % CPR) ^ swz<D>(r));
+    qoff[u] = (r * D + c) * 2;
+    goff[u] = (int)(r * p.do_sl + c) * 2;
+  }
+  const int gstep = (int)(TN * p.do_sl) * 2;
+  int cu = u0, cg = nt ? u0 / nt : 0, ct = ta + (nt ? u0 % nt : 0);    // the next tile to copy
+  auto copy_next = [&]() __attribute__((always_inline)) {
+    if (cu >= u1) return;
+    const uint32_t dst = lds0 + (uint32_t)((cu - u0) % kStages * STAGE);
+    const size_t head = (size_t)b * p.Hq + h0 + cg;
+    const u32x4 rq = resource(reinterpret_cast<const T*>(p.q) + (head * p.Lq + p.row0) * D, (unsigned)rows * D * 2);
+    const u32x4 rg = resource(reinterpret_cast<const T*>(p.d_o) + b * p.do_sb + (h0 + cg) * p.do_sh + p.row0 * p.do_sl,
+                              (unsigned)((rows - 1) * p.do_sl + D) * 2);
+    const u32x4 rx = resource(p.stats + (head * p.row_tiles + ct) * (2 * TN), 8 * TN);
+#pragma unroll
+    for (int u = 0; u < CB; ++u) {
+      copy16(rq, dst + (uint32_t)((wave * CB + u) * 1024), qoff[u] + ct * TB);
+      copy16(rg, dst + (uint32_t)(TB + (wave * CB + u) * 1024), goff[u] + ct * gstep);
+    }
+    copy4(rx, dst + 2 * TB, 4 * lane);
+    ++cu;
+    if (++ct == ta + nt) {
+      ct = ta;
+      ++cg;
+    }
+  };
+
+  const int roff = TL::row_offset(lane), doff = TL::dim_offset(lane);
+  f32x16 dk[TL::DB], dv[TL::DB];
+#pragma unroll
+  for (int db = 0; db < TL::DB; ++db) dk[db] = dv[db] = f32x16{};
+  const float c = p.c;
+  const float held = __builtin_ldexpf(1.f, scale_exp - (is_half<T> ? kShift : 0));
+
+  // One tile: queries i0 .. i0 + 31 of a head against the wave's keys.
+  auto tile = [&](auto masked, const char* st, int i0, float sl2) __attribute__((always_inline)) {
+    constexpr bool MASKED = decltype(masked)::value;
+    const char* gt = st + TB;
+    const char* sx = st + 2 * TB + 16 * hh;
+    f32x16 s = f32x16{};
+    if constexpr (!CAP) {
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const f32x4 a = *reinterpret_cast<const f32x4*>(sx + 32 * g);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[4 * g + i] = a[i];
+      }
+    }
+#pragma unroll
+    for (int kx = 0; kx < TL::KX; ++kx) s = E::mfma(TL::rows(st, roff, kx), kf[kx], s);
+    // Query i sees this lane's key: lo <= i - i0 - 4 hh < hi.
+    const int lo = key - off - i0 - 4 * hh, hi = W > 0 ? lo + W : 1 << 30;
+    const float bias = ALIBI ? sl2 * (float)(key - off - i0) : 0.f;
+    Weights<T> w;
+#pragma unroll
+    for (int r = 0; r < 16; r += 2) {
+      float x[2], f[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        if constexpr (CAP) {
+          const float a = *reinterpret_cast<const float*>(sx + 4 * kconst(r + i));
+          x[i] = fast_exp2(capped(s[r + i], p, a, f[i]));
+        } else {
+          x[i] = fast_exp2(ALIBI ? __builtin_fmaf(s[r + i], c, bias) : s[r + i] * c);
+        }
+        if (MASKED && (kconst(r + i) < lo || kconst(r + i) >= hi)) x[i] = 0.f;
+        s[r + i] = CAP ? x[i] * f[i] : x[i];
+      }
+      w.set(r, x[0], x[1]);
+    }
+#pragma unroll
+    for (int c16 = 0; c16 < 2; ++c16)
+#pragma unroll
+      for (int db = 0; db < TL::DB; ++db) dv[db] = E::mfma(TL::dims(gt, doff, c16, db), w.operand(c16), dv[db]);
+    f32x16 x;
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const f32x4 a = *reinterpret_cast<const f32x4*>(sx + 4 * TN + 32 * g);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[4 * g + i] = a[i];
+    }
+#pragma unroll
+    for (int kx = 0; kx < TL::KX; ++kx) x = E::mfma(TL::rows(gt, roff, kx), vf[kx], x);
+#pragma unroll
+    for (int r = 0; r < 16; r += 2) {
+      float y[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        y[i] = s[r + i] * x[r + i];
+        if (is_half<T>) y[i] *= held;
+        if (MASKED && (kconst(r + i) < lo || kconst(r + i) >= hi)) y[i] = 0.f;   // (0 times an infinity is NaN)
+      }
+      w.set(r, y[0], y[1]);
+    }
+#pragma unroll
+    for (int c16 = 0; c16 < 2; ++c16)
+#pragma unroll
+      for (int db = 0; db < TL::DB; ++db) dk[db] = E::mfma(TL::dims(st, doff, c16, db), w.operand(c16), dk[db]);
+  };
+
+  for (int u = 0; u < kStages - 1; ++u) copy_next();
+  int g = nt ? u0 / nt : 0, t = ta + (nt ? u0 % nt : 0);
+  for (int u = u0; u < u1; ++u) {
+    // The tile is in LDS when every wave has waited for its own copies; the stage of tile u - 1
+    // is free behind the same barrier.
+    if (u + kStages - 2 < u1) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"((kStages - 2) * CPW) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    copy_next();
+    const char* st = lds + (u - u0) % kStages * STAGE;
+    const int i0 = t * TN;
+    const float sl2 = ALIBI ? p.slopes[h0 + g] * kLog2e : 0.f;
+    if (!CAUSAL) {
+      tile(std::false_type{}, st, i0, sl2);
+    } else if (i0 + TN - 1 + off >= jw && (W == 0 || i0 + off - W < jw + TN - 1)) {
+      if (i0 + off >= jw + TN - 1 && (W == 0 || i0 + TN - 1 + off - W < jw)) tile(std::false_type{}, st, i0, sl2);
+      else tile(std::true_type{}, st, i0, sl2);
+    }
+    if (++t == ta + nt) {
+      t = ta;
+      ++g;
+    }
+  }
+
+  if (key < p.Lk) {
+    const size_t at = ((size_t)unit * p.Lk + key) * D, all = (size_t)units * p.Lk * D;
+    float* pk = S > 1 ? p.ws_dkv + 2 * part * all + at : nullptr;
+    store<D, T>(dk, __builtin_ldexpf(p.scale, -scale_exp), reinterpret_cast<T*>(p.dk) + at, pk, hh);
+    store<D, T>(dv, is_half<T> ? __builtin_ldexpf(1.f, -kShift) : 1.f, reinterpret_cast<T*>(p.dv) + at,
+                pk ? pk + all : nullptr, hh);
+  }
+}
+
+// dQ of 128 query rows (of p.hg heads that share a KV head, 128 / hg rows each): the tiles of 32
+// keys that they see, or the share `part` of them.
+template <int D, typename T, bool CAUSAL, bool ALIBI, bool CAP>
+__global__ __launch_bounds__(kThreads, 2) void bwd_dq_kernel(BwdParams p) {
+  typedef Elem<T> E;
+  typedef Tile<D, T> TL;
+  typedef typename E::vec8 vec8;
+  constexpr int TB = TL::BYTES, STAGE = 2 * TB, CPR = TL::CPR;
+  constexpr int CB = TL::NBLK / kWaves, CPW = 2 * CB;
+  __shared__ __attribute__((aligned(1024))) char lds[kStages * STAGE];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int n = lane & 31, hh = lane >> 5;
+
+  const int hg = p.hg, bm = TN * (kWaves / hg), ngrp = p.group / hg;
+  const int rows = p.rows, off = p.Lk - rows, W = p.window, S = p.dq_parts;
+  const int units = p.B * p.Hkv, nqb = (rows + bm - 1) / bm;
+  const int item = item_of(units * ngrp * nqb * S, p.shares);
+  if (item < 0) return;
+  // Row blocks from the last, which sees the most keys.
+  int unit, rb, grp, part = item % S;
+  if (p.shares) {
+    unit = item / (nqb * ngrp * S);
+    const int rest = item / S - unit * nqb * ngrp;
+    rb = nqb - 1 - rest / ngrp;
+    grp = rest % ngrp;
+  } else {
+    const int rest = item / S, per = units * ngrp;
+    rb = nqb - 1 - rest / per;
+    unit = rest % per / ngrp;
+    grp = rest % ngrp;
+  }
+  const int b = unit / p.Hkv, hq = (unit - b * p.Hkv) * p.group + grp * hg + wave % hg;
+  const size_t head = (size_t)b * p.Hq + hq;
+  const int i0 = rb * bm, iw = i0 + TN * (wave / hg), wlast = min(iw + TN, rows) - 1;
+  int jlo = 0, jhi = p.Lk;
+  if (CAUSAL) {
+    jhi = min(p.Lk, min(i0 + bm, rows) + off);
+    if (W > 0) jlo = max(0, i0 + off + 1 - W);
+  }
+  const int ta = jlo / TN, nt = (jhi + TN - 1) / TN - ta;
+  const int t0 = ta + (int)((long long)nt * part / S), t1 = ta + (int)((long long)nt * (part + 1) / S);
+
+  int scale_exp = 0;
+  if (is_half<T>) scale_exp = bwd_scale<T>(p, unit, reinterpret_cast<float*>(lds));
+
+  const int row = min(iw + n, rows - 1);
+  vec8 qf[TL::KX], gf[TL::KX];
+  {
+    const T* qg = reinterpret_cast<const T*>(p.q) + (head * p.Lq + p.row0 + row) * D + 8 * hh;
+    const T* gg = reinterpret_cast<const T*>(p.d_o) + b * p.do_sb + hq * p.do_sh + (p.row0 + row) * p.do_sl + 8 * hh;
+#pragma unroll
+    for (int kx = 0; kx < TL::KX; ++kx) {
+      qf[kx] = load8(qg + 16 * kx, p.sign);
+      gf[kx] = load8(gg + 16 * kx);
+    }
+  }
+  const float* sx = p.stats + (head * p.row_tiles + row / TN) * (2 * TN) + row % TN;
+  const float start = sx[0], nd = sx[TN];
+  const float sl2 = ALIBI ? p.slopes[hq] * kLog2e : 0.f;
+  const float c = p.c, add = CAP ? start : start * c;
+
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_void*)lds;
+  int coff[CB];
+#pragma unroll
+  for (int u = 0; u < CB; ++u) {
+    const int r = (wave * CB + u) * (1024 / (2 * D)) + lane / CPR;
+    coff[u] = (r * D + 8 * ((lane % CPR) ^ swz<D>(r))) * 2;
+  }
+  const u32x4 rk = resource(reinterpret_cast<const T*>(p.k) + (size_t)unit * p.Lk * D, (unsigned)p.Lk * D * 2);
+  const u32x4 rv = resource(reinterpret_cast<const T*>(p.v) + (size_t)unit * p.Lk * D, (unsigned)p.Lk * D * 2);
+  auto copy_tile = [&](int t) __attribute__((always_inline)) {
+    if (t >= t1) return;
+    const uint32_t dst = lds0 + (uint32_t)((t - t0) % kStages * STAGE);
+#pragma unroll
+    for (int u = 0; u < CB; ++u) {
+      copy16(rk, dst + (uint32_t)((wave * CB + u) * 1024), coff[u] + t * TB);
+      copy16(rv, dst + (uint32_t)(TB + (wave * CB + u) * 1024), coff[u] + t * TB);
+    }
+  };
+
+  const int roff = TL::row_offset(lane), doff = TL::dim_offset(lane);
+  f32x16 dq[TL::DB];
+#pragma unroll
+  for (int db = 0; db < TL::DB; ++db) dq[db] = f32x16{};
+  const float held = __builtin_ldexpf(1.f, scale_exp - (is_half<T> ? kShift : 0));
+
+  auto tile = [&](auto masked, const char* st, int j0) __attribute__((always_inline)) {
+    constexpr bool MASKED = decltype(masked)::value;
+    const char* vt = st + TB;
+    f32x16 s = f32x16{}, x = f32x16{};
+#pragma unroll
+    for (int kx = 0; kx < TL::KX; ++kx) s = E::mfma(TL::rows(st, roff, kx), qf[kx], s);
+#pragma unroll
+    for (int kx = 0; kx < TL::KX; ++kx) x = E::mfma(TL::rows(vt, roff, kx), gf[kx], x);
+    // This lane's row sees key j: lo < j - j0 - 4 hh <= hi.
+    int hi = p.Lk - 1, lo = -1;
+    if (CAUSAL) hi = min(hi, row + off);
+    if (CAUSAL && W > 0) lo = row + off - W;
+    hi -= j0 + 4 * hh;
+    lo -= j0 + 4 * hh;
+    const float base = ALIBI ? __builtin_fmaf(sl2, (float)(j0 + 4 * hh - iw - off), add) : add;
+    Weights<T> w;
+#pragma unroll
+    for (int r = 0; r < 16; r += 2) {
+      float y[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int k = kconst(r + i);
+        float f = 1.f, a;
+        if constexpr (CAP) a = fast_exp2(capped(s[r + i], p, add, f)) * f;
+        else a = fast_exp2(__builtin_fmaf(s[r + i], c, ALIBI ? __builtin_fmaf(sl2, (float)k, base) : base));
+        y[i] = a * (x[r + i] + nd);
+        if (is_half<T>) y[i] *= held;
+        if (MASKED && (k > hi || k <= lo)) y[i] = 0.f;
+      }
+      w.set(r, y[0], y[1]);
+    }
+#pragma unroll
+    for (int c16 = 0; c16 < 2; ++c16)
+#pragma unroll
+      for (int db = 0; db < TL::DB; ++db) dq[db] = E::mfma(TL::dims(st, doff, c16, db), w.operand(c16), dq[db]);
+  };
+
+  for (int u = 0; u < kStages - 1; ++u) copy_tile(t0 + u);
+  for (int t = t0; t < t1; ++t) {
+    if (t + kStages - 2 < t1) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"((kStages - 2) * CPW) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    copy_tile(t + kStages - 1);
+    const char* st = lds + (t - t0) % kStages * STAGE;
+    const int j0 = t * TN;
+    if (iw >= rows) continue;
+    if (!CAUSAL) {
+      if (j0 + TN <= p.Lk) tile(std::false_type{}, st, j0);
+      else tile(std::true_type{}, st, j0);
+    } else if (j0 <= wlast + off && (W == 0 || j0 + TN - 1 > iw + off - W)) {
+      if (j0 + TN - 1 <= iw + off && (W == 0 || j0 > wlast + off - W)) tile(std::false_type{}, st, j0);
+      else tile(std::true_type{}, st, j0);
+    }
+  }
+
+  if (iw + n < rows) {
+    const size_t at = (head * p.Lq + p.row0 + iw + n) * D;
+    float* pq = S > 1 ? p.ws_dq + part * ((size_t)p.B * p.Hq * p.Lq * D) + at : nullptr;
+    store<D, T>(dq, __builtin_ldexpf(p.scale, -scale_exp), reinterpret_cast<T*>(p.dq) + at, pq, hh);
+  }
+}
+
+// The partials of several parts, summed in their order.
+struct BwdSum {
+  const float* ws;      // part s of element i: ws[s step + i]
+  void* out;
+  size_t step, n;       // n: elements, a multiple of 4
+  int parts;
+  int skip, len, D;     // rows i % len below `skip` are left as they are
+};
+template <typename T>
+__global__ __launch_bounds__(256) void bwd_sum_kernel(BwdSum p) {
+  const size_t i = 4 * ((size_t)blockIdx.x * 256 + threadIdx.x);
+  if (i >= p.n) return;
+  if (p.skip && (int)(i / p.D % p.len) < p.skip) return;
+  f32x4 a = *reinterpret_cast<const f32x4*>(p.ws + i);
+  for (int s = 1; s < p.parts; ++s) a += *reinterpret_cast<const f32x4*>(p.ws + s * p.step + i);
+  *reinterpret_cast<uint2*>(reinterpret_cast<T*>(p.out) + i) =
+      make_uint2(Elem<T>::pack2(a[0], a[1]), Elem<T>::pack2(a[2], a[3]));
+}
+
+template <typename T>
+hipError_t launch_sum(const BwdSum& p, hipStream_t stream) {
+  hipLaunchKernelGGL((bwd_sum_kernel<T>), dim3((unsigned)((p.n / 4 + 255) / 256)), dim3(256), 0, stream, p);
+  return hipGetLastError();
+}
+
+int grid_of(int64_t items, bool shares) { return (int)(shares ? (items + kXcds - 1) / kXcds * kXcds : items); }
+
+template <int D, typename T, bool CAUSAL, bool ALIBI, bool CAP>
+hipError_t launch_t(const BwdParams& p, hipStream_t stream) {
+  const int64_t units = (int64_t)p.B * p.Hkv, heads = (int64_t)p.B * p.Hq;
+  int64_t pre = heads * p.row_blocks + heads * ((p.row0 + kRowsBlock - 1) / kRowsBlock);
+  if (is_half<T>) pre += units * p.key_blocks;
+  hipLaunchKernelGGL((bwd_rows_kernel<D, T>), dim3((unsigned)pre), dim3(kThreads), 0, stream, p);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const int64_t nk = units * ((p.Lk + BLK - 1) / BLK) * p.dkv_parts;
+  hipLaunchKernelGGL((bwd_dkv_kernel<D, T, CAUSAL, ALIBI, CAP>), dim3(grid_of(nk, p.shares)), dim3(kThreads), 0, stream, p);
+  if ((e = hipGetLastError()) != hipSuccess) return e;
+  const int bm = TN * (kWaves / p.hg);
+  const int64_t nq = units * (p.group / p.hg) * ((p.rows + bm - 1) / bm) * p.dq_parts;
+  hipLaunchKernelGGL((bwd_dq_kernel<D, T, CAUSAL, ALIBI, CAP>), dim3(grid_of(nq, p.shares)), dim3(kThreads), 0, stream, p);
+  if ((e = hipGetLastError()) != hipSuccess) return e;
+  if (p.dkv_parts > 1) {
+    const size_t n = (size_t)units * p.Lk * D;
+    if ((e = launch_sum<T>({p.ws_dkv, p.dk, 2 * n, n, p.dkv_parts, 0, 1, D}, stream)) != hipSuccess) return e;
+    if ((e = launch_sum<T>({p.ws_dkv + n, p.dv, 2 * n, n, p.dkv_parts, 0, 1, D}, stream)) != hipSuccess) return e;
+  }
+  if (p.dq_parts > 1) {
+    const size_t n = (size_t)heads * p.Lq * D;
+    return launch_sum<T>({p.ws_dq, p.dq, n, n, p.dq_parts, p.row0, p.Lq, D}, stream);
+  }
+  return hipSuccess;
+}
+
+template <int D, typename T>
+hipError_t launch_d(const BwdParams& p, hipStream_t s) {
+  if (p.cap_cl != 0.f) return launch_t<D, T, true, false, true>(p, s);
+  if (p.causal) return p.slopes ? launch_t<D, T, true, true, false>(p, s) : launch_t<D, T, true, false, false>(p, s);
+  return p.slopes ? launch_t<D, T, false, true, false>(p, s) : launch_t<D, T, false, false, false>(p, s);
+}
+
+}  // namespace
+
+int bwd_block_keys() { return BLK; }
+int bwd_rows_per_block() { return kRowsBlock; }
+
+hipError_t launch_attn_bwd(const BwdParams& p, hipStream_t stream) {
+  if (p.D == 64) return p.bf16 ? launch_d<64, __bf16>(p, stream) : launch_d<64, _Float16>(p, stream);
+  return p.bf16 ? launch_d<128, __bf16>(p, stream) : launch_d<128, _Float16>(p, stream);
+}
+
+}  // namespace attn

@@ -27,6 +27,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "../../include/attn.h"
+#include "../../include/attn_bwd.h"
 #include "../../include/kv4.h"
 #include "../../include/norms.h"
 #include "../../include/rope.h"
@@ -579,6 +580,99 @@ PyObject* py_attn_decode_kv4(PyObject*, PyObject* const* x, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
+// q, k, v of attention in training on the current device, and what modifies its scores.
+struct Train {
+  const at::Tensor *q, *k, *v;
+  at::ScalarType type;
+  attn_dtype dtype;
+  int B, Hq, Hkv, Lq, Lk, D;
+  bool causal;
+  float scale, cap = 0.f;
+  const float* slopes = nullptr;
+  int window = 0;
+};
+
+// q, k, v at x, and (causal, scale, alibi_slopes, softcap, window) at m; false if not plainly valid.
+bool train_args(PyObject* const* x, PyObject* const* m, Train& a) {
+  if (!truth(m[0], a.causal) || (m[3] != Py_None && !number(m[3], a.cap))) return false;
+  if (m[4] != Py_None && !whole(m[4], a.window)) return false;
+  a.q = here(x[0]);
+  a.k = here(x[1]);
+  if (!a.q || !a.k || a.q->dim() != 4 || a.k->dim() != 4) return false;
+  a.type = a.q->scalar_type();
+  if ((a.type != at::kHalf && a.type != at::kBFloat16) || a.k->scalar_type() != a.type) return false;
+  a.v = here(x[2], a.type, a.k->sizes());
+  if (!a.v || a.k->size(0) != a.q->size(0) || a.k->size(3) != a.q->size(3)) return false;
+  a.dtype = a.type == at::kHalf ? ATTN_F16 : ATTN_BF16;
+  a.B = (int)a.q->size(0);
+  a.Hq = (int)a.q->size(1);
+  a.Lq = (int)a.q->size(2);
+  a.D = (int)a.q->size(3);
+  a.Hkv = (int)a.k->size(1);
+  a.Lk = (int)a.k->size(2);
+  if (m[2] != Py_None) {
+    const at::Tensor* t = here(m[2]);
+    if (!t || t->scalar_type() != at::kFloat || t->numel() != a.Hq) return false;
+    a.slopes = static_cast<const float*>(t->data_ptr());
+  }
+  if (m[1] != Py_None) return number(m[1], a.scale);
+  a.scale = (float)(1.0 / std::sqrt((double)a.D));
+  return a.D >= 1;
+}
+
+// (q, k, v, o, lse, causal, scale, alibi_slopes, softcap, window, stream) -> (o, lse)
+PyObject* py_attn_fwd_lse(PyObject*, PyObject* const* x, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  Train a;
+  if (n != 11 || x[10] != Py_None || !train_args(x, x + 5, a)) return none();
+  at::Tensor o, lse;
+  if (!output(x[3], *a.q, a.type, a.q->sizes(), o) || !output(x[4], *a.q, at::kFloat, {a.B, a.Hq, a.Lq}, lse)) return none();
+  const void *q = a.q->data_ptr(), *k = a.k->data_ptr(), *v = a.v->data_ptr();
+  void* op = o.data_ptr();
+  float* lp = static_cast<float*>(lse.data_ptr());
+  const hipStream_t s = stream();
+  const int rc = unlocked([&] {
+    return attn_fwd_lse(q, k, v, op, lp, a.B, a.Hq, a.Hkv, a.Lq, a.Lk, a.D, a.causal, a.scale, a.slopes, a.cap, a.window,
+                        a.dtype, s);
+  });
+  return results(rc, {{x[3], &o}, {x[4], &lse}});
+  END_HANDLE_TH_ERRORS
+}
+
+// (do, q, k, v, o, lse, dq, dk, dv, causal, scale, alibi_slopes, softcap, window, workspace, stream) -> (dq, dk, dv)
+PyObject* py_attn_bwd(PyObject*, PyObject* const* x, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  Train a;
+  long long strides[3];
+  if (n != 16 || x[15] != Py_None || !train_args(x + 1, x + 9, a)) return none();
+  const at::Tensor *d = rows(x[0], strides), *o = here(x[4], a.type, a.q->sizes()),
+                   *lse = here(x[5], at::kFloat, {a.B, a.Hq, a.Lq});
+  if (!d || !o || !lse || d->scalar_type() != a.type || d->sizes() != a.q->sizes()) return none();
+  at::Tensor dq, dk, dv, ws;
+  if (!output(x[6], *a.q, a.type, a.q->sizes(), dq) || !output(x[7], *a.q, a.type, a.k->sizes(), dk) ||
+      !output(x[8], *a.q, a.type, a.k->sizes(), dv))
+    return none();
+  if (x[14] != Py_None) {
+    const at::Tensor* t = here(x[14]);
+    if (!t) return none();
+    ws = *t;
+  } else {
+    const size_t need = attn_bwd_workspace_bytes(a.B, a.Hq, a.Hkv, a.Lq, a.Lk, a.D, a.causal, a.window);
+    ws = fresh({(int64_t)std::max<size_t>(need, 16)}, at::kByte, *a.q);
+  }
+  const void *dp = d->data_ptr(), *q = a.q->data_ptr(), *k = a.k->data_ptr(), *v = a.v->data_ptr(), *op = o->data_ptr();
+  const float* lp = static_cast<const float*>(lse->data_ptr());
+  void *dqp = dq.data_ptr(), *dkp = dk.data_ptr(), *dvp = dv.data_ptr(), *wp = ws.data_ptr();
+  const size_t bytes = ws.nbytes();
+  const hipStream_t s = stream();
+  const int rc = unlocked([&] {
+    return attn_bwd(dp, strides, q, k, v, op, lp, dqp, dkp, dvp, a.B, a.Hq, a.Hkv, a.Lq, a.Lk, a.D, a.causal, a.scale,
+                    a.slopes, a.cap, a.window, wp, bytes, a.dtype, s);
+  });
+  return results(rc, {{x[6], &dq}, {x[7], &dk}, {x[8], &dv}});
+  END_HANDLE_TH_ERRORS
+}
+
 template <PyObject* (*F)(PyObject*, PyObject* const*, Py_ssize_t)>
 PyCFunction fast() {
   return reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(F));
@@ -595,6 +689,8 @@ PyMethodDef methods[] = {
     {"kv4_append", fast<py_kv4_append>(), METH_FASTCALL, nullptr},
     {"kv4_load", fast<py_kv4_load>(), METH_FASTCALL, nullptr},
     {"attn_decode_kv4", fast<py_attn_decode_kv4>(), METH_FASTCALL, nullptr},
+    {"attn_fwd_lse", fast<py_attn_fwd_lse>(), METH_FASTCALL, nullptr},
+    {"attn_bwd", fast<py_attn_bwd>(), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -34,6 +34,11 @@ struct PrefillParams {
 // 25.9 us call.)
 static_assert(sizeof(PrefillParams) + 4 <= 128, "arguments and grid size within two lines");
 
+// The same with each row's log-sum-exp (prefill.hip, shards 4 to 7).
+struct PrefillLseParams : PrefillParams {
+  float* lse;           // [B, Hq, Lq], natural units
+};
+
 struct PrefillSplitParams : PrefillParams {
   int splits;           // key ranges (1: none)
   float* ws;            // partials, for splits > 1: [splits, B*Hq*Lq, D], then (max, sum) [splits, B*Hq*Lq, 2]
@@ -99,6 +104,11 @@ hipError_t launch_prefill_d128_f16(const PrefillParams& p, hipStream_t stream);
 hipError_t launch_prefill_d128_bf16(const PrefillParams& p, hipStream_t stream);
 hipError_t launch_prefill_d64_f16(const PrefillParams& p, hipStream_t stream);
 hipError_t launch_prefill_d64_bf16(const PrefillParams& p, hipStream_t stream);
+hipError_t launch_prefill_lse(const PrefillLseParams& p, hipStream_t stream);
+hipError_t launch_prefill_lse_d128_f16(const PrefillLseParams& p, hipStream_t stream);
+hipError_t launch_prefill_lse_d128_bf16(const PrefillLseParams& p, hipStream_t stream);
+hipError_t launch_prefill_lse_d64_f16(const PrefillLseParams& p, hipStream_t stream);
+hipError_t launch_prefill_lse_d64_bf16(const PrefillLseParams& p, hipStream_t stream);
 hipError_t launch_decode(const DecodeParams& p, hipStream_t stream);
 
 // Bytes of the static decode workspace of attn_decode_noalloc.
@@ -106,6 +116,42 @@ constexpr size_t kDecodeScratchBytes = size_t(16) << 20;
 // Device address of that workspace on the current device (resolved once per
 // device, then cached).
 hipError_t decode_scratch(void** ptr);
+
+// Attention's backward pass (attn_bwd.hip).
+struct BwdParams {
+  const void* q;
+  const void* k;
+  const void* v;
+  const void* o;
+  const void* d_o;
+  const float* lse;
+  const float* slopes;  // device, [Hq], or nullptr
+  void* dq;
+  void* dk;
+  void* dv;
+  float* stats;         // [B * Hq, row_tiles, 64]
+  float* peaks;         // fp16: [B * Hq, row_blocks], then [B * Hkv, key_blocks]
+  float* ws_dkv;        // partials [dkv_parts, 2, B * Hkv, Lk, D]
+  float* ws_dq;         // partials [dq_parts, B * Hq, Lq, D]
+  int64_t do_sb, do_sh, do_sl;   // strides of d_o in elements
+  int B, Hq, Hkv, Lq, Lk, D;
+  int group;            // Hq / Hkv
+  int row0, rows;       // the first rows see no key (causal, Lq > Lk): rows row0 .. row0 + rows - 1 do
+  int row_tiles, row_blocks, key_blocks;   // tiles of 32, blocks of 64
+  int window;           // 0 for none
+  int hg;               // query heads of a workgroup of the dQ kernel
+  int dkv_parts, dq_parts;
+  bool causal, bf16;
+  bool shares;          // every XCD a contiguous share of the workgroups' items
+  unsigned sign;        // 0x80008000 where the scale is negative
+  float c;              // |scale| * log2(e), or a tiny number
+  float scale;
+  float cap_k2;         // SoftCap: 2 / cap * c
+  float cap_cl;         // SoftCap: cap * log2(e), or 0 for no cap
+};
+int bwd_block_keys();
+int bwd_rows_per_block();
+hipError_t launch_attn_bwd(const BwdParams& p, hipStream_t stream);
 
 // Row reductions (norms.hip): the stable L2 norm, or RMSNorm with its row max.
 struct NormParams {

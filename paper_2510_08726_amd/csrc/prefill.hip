@@ -59,6 +59,13 @@
 // Scores are in log2 units: t = s * scale * log2(e) (+ ALiBi bias * log2(e)),
 // so each exponential is one v_exp_f32.  With ALiBi at D = 64 the key part of
 // the bias starts the S^T accumulator, so that preparing a score is one FMA.
+//
+// attn_fwd_lse's kernels (prefill_lse_kernel, shards 4 to 7) also write each row's
+// log-sum-exp.  Their l is the sum of the exponentials as they are, before P is
+// rounded: a backward pass that recomputes P = exp(s - lse) has no other error in
+// its weights than that of 32 bits, where the rounded ones' sum is 2^-9 (bf16) off in rows of few
+// keys.  It is kept in a VGPR per lane (two additions beside each pair of
+// exponentials), in the place of the rowsum MFMAs.
 
 #include <algorithm>
 #include <atomic>
@@ -92,6 +99,9 @@ constexpr float kMcInit = -1e30f;
 // Accelerator dies (XCDs), each with its own L2; consecutive workgroups of a
 // launch are dealt to them in turn.
 constexpr int kXcds = 8;
+
+__device__ __forceinline__ float* lse_of(const PrefillLseParams& p) { return p.lse; }
+__device__ __forceinline__ float* lse_of(const PrefillParams&) { return nullptr; }
 
 __device__ __forceinline__ float as_f(unsigned u) { return __builtin_bit_cast(float, u); }
 __device__ __forceinline__ unsigned as_u(float f) { return __builtin_bit_cast(unsigned, f); }
@@ -128,12 +138,21 @@ __device__ __forceinline__ void hazard_pad() {
 }
 
 // This file is compiled once per (head dim, element type) shard, selected by
-// ATTN_PREFILL_SHARD (0, 1: D = 128; 2, 3: D = 64), so the instantiations
-// build in parallel and each shard gets the register split of its head dim.
+// ATTN_PREFILL_SHARD (0, 1: D = 128; 2, 3: D = 64; 4 to 7 the same with the
+// log-sum-exp), so the instantiations build in parallel and each shard gets the
+// register split of its head dim.
 #ifndef ATTN_PREFILL_SHARD
 #define ATTN_PREFILL_SHARD 0
 #endif
-constexpr int kShardD = ATTN_PREFILL_SHARD >= 2 ? 64 : 128;
+constexpr int kShardD = ATTN_PREFILL_SHARD % 4 >= 2 ? 64 : 128;
+constexpr bool kLse = ATTN_PREFILL_SHARD >= 4;   // attn_fwd_lse's kernels
+#if ATTN_PREFILL_SHARD >= 4
+#define ATTN_PREFILL_KERNEL prefill_lse_kernel
+typedef PrefillLseParams Params;
+#else
+#define ATTN_PREFILL_KERNEL prefill_kernel
+typedef PrefillParams Params;
+#endif
 
 // Register files.  The S^T accumulators, P and the LDS operands are ordinary
 // values in VGPRs, allocated by the compiler.  The operands that live through
@@ -143,12 +162,19 @@ constexpr int kShardD = ATTN_PREFILL_SHARD >= 2 ? 64 : 128;
 // a[kOnesAgpr .. + 1]: 102 AGPRs for D = 128, 54 for D = 64.  The build sets
 // each kernel's AGPR allocation to that count rounded up to 4 (104 or 56),
 // which leaves 152 or 200 of a wave's 256 registers (two waves per SIMD) to
-// the VGPRs.  Every statement that touches the fixed AGPRs lists all of them
+// the VGPRs (with the log-sum-exp 96 or 48 AGPRs, 160 or 208 VGPRs).  Every statement that touches the fixed AGPRs lists all of them
 // as clobbered, so the compiler keeps none of its own values there, and
 // counts them as used.
 #define ATTN_A10(p) "a" #p "0", "a" #p "1", "a" #p "2", "a" #p "3", "a" #p "4", \
                     "a" #p "5", "a" #p "6", "a" #p "7", "a" #p "8", "a" #p "9"
-#if ATTN_PREFILL_SHARD >= 2
+#if ATTN_PREFILL_SHARD >= 6
+#define ATTN_AGPRS "a0", "a1", "a2", "a3", "a4", "a5", "a6", "a7", "a8", "a9", \
+    ATTN_A10(1), ATTN_A10(2), ATTN_A10(3), "a40", "a41", "a42", "a43", "a44", "a45", "a46", "a47"
+#elif ATTN_PREFILL_SHARD >= 4
+#define ATTN_AGPRS "a0", "a1", "a2", "a3", "a4", "a5", "a6", "a7", "a8", "a9", \
+    ATTN_A10(1), ATTN_A10(2), ATTN_A10(3), ATTN_A10(4), ATTN_A10(5), ATTN_A10(6), ATTN_A10(7), ATTN_A10(8), \
+    "a90", "a91", "a92", "a93", "a94", "a95"
+#elif ATTN_PREFILL_SHARD >= 2
 #define ATTN_AGPRS "a0", "a1", "a2", "a3", "a4", "a5", "a6", "a7", "a8", "a9", \
     ATTN_A10(1), ATTN_A10(2), ATTN_A10(3), ATTN_A10(4), "a50", "a51", "a52", "a53"
 #else
@@ -160,7 +186,7 @@ constexpr int kOAgpr = 0;
 constexpr int kQAgpr = kOAgpr + kShardD / 2;
 constexpr int kLAgpr = kQAgpr + kShardD / 4;    // exp-sum accumulator
 constexpr int kOnesAgpr = kLAgpr + 4;           // two registers holding (1.0, 1.0)
-constexpr int kAgprAlloc = (kOnesAgpr + 2 + 3) / 4 * 4;
+constexpr int kAgprAlloc = kLse ? kLAgpr : (kOnesAgpr + 2 + 3) / 4 * 4;   // (kLse: neither l nor the ones)
 constexpr int kVgprBudget = 256 - kAgprAlloc;
 static_assert(kOnesAgpr + 2 == (kShardD == 64 ? 54 : 102), "the clobber list names every fixed AGPR");
 
@@ -355,6 +381,7 @@ struct Prefill {
   struct State {
     float mc;     // reference max of the row, times ce (log2 units)
     float alpha;  // rescale factor of O^T and l set by the slow path
+    float l;      // kLse: this lane's half of the exp-sum
   };
   static constexpr int oagpr(int db) { return kOAgpr + 16 * db; }
   static constexpr int qagpr(int kx) { return kQAgpr + 4 * kx; }
@@ -374,6 +401,7 @@ struct Prefill {
     int lim;      // last visible key offset (key - j0 - 4 hh) of this lane's row
     int llo;      // first visible key offset of this lane's row (sliding window)
     float t;      // this lane's maximum score of the tile
+    float s;      // kLse: this lane's sum of the tile's exponentials
   };
 
   // HBM -> LDS copy of 1 KB block `blk` of tile t (rows t BN .. t BN + BN -
@@ -520,6 +548,10 @@ struct Prefill {
       constexpr int r = 2 * P::exp_index(K);
       const float p0 = fast_exp2(REL ? sc[r] : __builtin_fmaf(sc[r], ce, -st.mc));
       const float p1 = fast_exp2(REL ? sc[r + 1] : __builtin_fmaf(sc[r + 1], ce, -st.mc));
+      if constexpr (kLse) {
+        ta.s = r == 0 ? p0 + p1 : ta.s + (p0 + p1);
+        pin(ta.s);
+      }
       uint32_t w = E::pack2(p0, p1);
       pin(w);
       pr.w[r / 8][(r % 8) / 2] = w;
@@ -669,7 +701,7 @@ struct Prefill {
                 // Exp-sum of the same weights: words 2 db, 2 db + 1 of the
                 // slice, at fragments db = 0 and 1 (a large MFMA always
                 // separates two rowsum MFMAs on one accumulator).
-                if constexpr (db < 2)
+                if constexpr (db < 2 && !kLse)
                   M::template rowsum<kLAgpr>(make_uint2(p_prev.w[c16][2 * db], p_prev.w[c16][2 * db + 1]));
               }
             }
@@ -688,7 +720,7 @@ struct Prefill {
   static __device__ __forceinline__ void repair(float alpha) {
     hazard_pad();
     static_for<DB * 16>([&](auto ic) { agpr_scale<kOAgpr + decltype(ic)::value>(alpha); });
-    static_for<4>([&](auto ic) { agpr_scale<kLAgpr + decltype(ic)::value>(alpha); });
+    if constexpr (!kLse) static_for<4>([&](auto ic) { agpr_scale<kLAgpr + decltype(ic)::value>(alpha); });
     hazard_pad();
   }
 };
@@ -699,7 +731,7 @@ struct Prefill {
 // are used; the build sets the kernels' AGPR allocation to kAgprAlloc in the
 // device IR.)
 template <int D, typename T, bool CAUSAL, bool ALIBI, bool CAP, bool WIN>
-__global__ __launch_bounds__(kThreads, kWgPerCu) __attribute__((amdgpu_num_vgpr(kVgprBudget))) void prefill_kernel(PrefillParams p) {
+__global__ __launch_bounds__(kThreads, kWgPerCu) __attribute__((amdgpu_num_vgpr(kVgprBudget))) void ATTN_PREFILL_KERNEL(Params p) {
   static_assert(D == kShardD, "one head dim per shard");
   typedef Prefill<D, T, CAUSAL, ALIBI, CAP, WIN> PF;
   constexpr bool REV = ALIBI;
@@ -927,8 +959,10 @@ __global__ __launch_bounds__(kThreads, kWgPerCu) __attribute__((amdgpu_num_vgpr(
 
   Item cur;
   if (!item_at(0, cur)) return;
-  agpr_write<kOnesAgpr>(PF::M::kOnes);
-  agpr_write<kOnesAgpr + 1>(PF::M::kOnes);
+  if constexpr (!kLse) {
+    agpr_write<kOnesAgpr>(PF::M::kOnes);
+    agpr_write<kOnesAgpr + 1>(PF::M::kOnes);
+  }
   stage_kv(cur);
   stage_q(cur);
 
@@ -996,13 +1030,16 @@ __global__ __launch_bounds__(kThreads, kWgPerCu) __attribute__((amdgpu_num_vgpr(
       typename PF::M::v8 z8 = {};
       pin(z8);
       static_for<DB>([&](auto dc) { PF::M::template zero16<PF::oagpr(decltype(dc)::value)>(z8); });
-      uint2 z2 = make_uint2(0u, 0u);
-      pin(z2);
-      PF::M::template zero4<kLAgpr>(z2);
+      if constexpr (!kLse) {
+        uint2 z2 = make_uint2(0u, 0u);
+        pin(z2);
+        PF::M::template zero4<kLAgpr>(z2);
+      }
     }
     State st;
     st.mc = kMcInit;
     st.alpha = 1.f;
+    st.l = 0.f;
     TileArgs ta;
     ta.c = p.c;
     ta.sl2 = ALIBI ? p.slopes[cur.hq] * kLog2e : 0.f;
@@ -1073,7 +1110,9 @@ __global__ __launch_bounds__(kThreads, kWgPerCu) __attribute__((amdgpu_num_vgpr(
         if (__builtin_amdgcn_ballot_w64(PF::template exceeds<REL>(st, ta)) != 0) {
           PF::template resolve<REL>(st, sc[par], pr[par], ta);
           if (j != jfirst && __builtin_amdgcn_ballot_w64(st.alpha != 1.f) != 0) PF::repair(st.alpha);
+          if constexpr (kLse) st.l *= st.alpha;
         }
+        if constexpr (kLse) st.l += ta.s;
       }
       // 16 wait states between this iteration's last MFMAs and the next
       // iteration's first reads of their results; this iteration's copies
@@ -1147,7 +1186,9 @@ __global__ __launch_bounds__(kThreads, kWgPerCu) __attribute__((amdgpu_num_vgpr(
     // touches that tile), then the wave stores the tile row-major, 16 bytes a
     // lane, whole rows per instruction.
     {
-      const float lt = sum_halves(agpr_read<kLAgpr>());
+      float ll = st.l;
+      if constexpr (!kLse) ll = agpr_read<kLAgpr>();
+      const float lt = sum_halves(ll);
       const float inv = lt > 0.f ? 1.f / lt : 0.f;
       char* xo = reinterpret_cast<char*>(const_cast<T*>(xl));
       // The lane index passes through an opaque copy, so that the addresses
@@ -1166,6 +1207,12 @@ __global__ __launch_bounds__(kThreads, kWgPerCu) __attribute__((amdgpu_num_vgpr(
         w.y = PF::E::pack2(agpr_read<a0 + 2>() * inv, agpr_read<a0 + 3>() * inv);
         *reinterpret_cast<uint2*>(xo + 2 * (n2 * D + 8 * ((4 * db + g) ^ sw) + 4 * h2)) = w;
       });
+      if constexpr (kLse) {
+        // The bias was written relative to the wave's first row (soft_step): its
+        // last term comes back here.  (-inf for a row that sees no key.)
+        const float x = st.mc + __builtin_amdgcn_logf(lt) - (ALIBI ? ta.sl2 * (float)n2 : 0.f);
+        if (h2 == 0 && iw + n2 < Lq) lse_of(p)[(size_t)cur.head * Lq + iw + n2] = lt == 0.f ? kNegInf : x * kLn2;
+      }
       constexpr int RPI = 64 / CPR;   // rows per store instruction
       const int pos = ln % CPR;
       T* op = reinterpret_cast<T*>(p.o) + ((size_t)cur.head * Lq + iw) * D;
@@ -1197,8 +1244,8 @@ int compute_units() {
 }
 
 template <int D, typename T, bool CAUSAL, bool ALIBI, bool CAP, bool WIN = false>
-hipError_t launch_t(const PrefillParams& p, hipStream_t stream) {
-  PrefillParams q = p;
+hipError_t launch_t(const Params& p, hipStream_t stream) {
+  Params q = p;
   // Query heads per workgroup: the largest power of two (up to the wave
   // count) that divides the GQA group.
   q.hg = 1;
@@ -1214,12 +1261,12 @@ hipError_t launch_t(const PrefillParams& p, hipStream_t stream) {
   q.sorted = order != 0;
   const int grid = q.sorted ? slots : std::min(q.nitems, slots);
   q.nxcd = order == 2 || grid % kXcds != 0 ? 1 : kXcds;
-  hipLaunchKernelGGL((prefill_kernel<D, T, CAUSAL, ALIBI, CAP, WIN>), dim3(grid), dim3(kThreads), 0, stream, q);
+  hipLaunchKernelGGL((ATTN_PREFILL_KERNEL<D, T, CAUSAL, ALIBI, CAP, WIN>), dim3(grid), dim3(kThreads), 0, stream, q);
   return hipGetLastError();
 }
 
 template <int D, typename T>
-hipError_t launch_d(const PrefillParams& p, hipStream_t s) {
+hipError_t launch_d(const Params& p, hipStream_t s) {
   const PrefillFlags f = prefill_flags(p.causal, p.slopes != nullptr, p.cap_cl != 0.f, p.window > 0);
   if (f.win) {
     if (f.cap) return launch_t<D, T, true, false, true, true>(p, s);
@@ -1241,6 +1288,14 @@ hipError_t launch_prefill_d128_bf16(const PrefillParams& p, hipStream_t s) { ret
 hipError_t launch_prefill_d64_f16(const PrefillParams& p, hipStream_t s) { return launch_d<64, _Float16>(p, s); }
 #elif ATTN_PREFILL_SHARD == 3
 hipError_t launch_prefill_d64_bf16(const PrefillParams& p, hipStream_t s) { return launch_d<64, __bf16>(p, s); }
+#elif ATTN_PREFILL_SHARD == 4
+hipError_t launch_prefill_lse_d128_f16(const PrefillLseParams& p, hipStream_t s) { return launch_d<128, _Float16>(p, s); }
+#elif ATTN_PREFILL_SHARD == 5
+hipError_t launch_prefill_lse_d128_bf16(const PrefillLseParams& p, hipStream_t s) { return launch_d<128, __bf16>(p, s); }
+#elif ATTN_PREFILL_SHARD == 6
+hipError_t launch_prefill_lse_d64_f16(const PrefillLseParams& p, hipStream_t s) { return launch_d<64, _Float16>(p, s); }
+#elif ATTN_PREFILL_SHARD == 7
+hipError_t launch_prefill_lse_d64_bf16(const PrefillLseParams& p, hipStream_t s) { return launch_d<64, __bf16>(p, s); }
 #endif
 
 #if ATTN_PREFILL_SHARD == 0
@@ -1277,6 +1332,11 @@ int prefill_order(int nitems, int nqb, int slots, bool causal, int window, int L
 hipError_t launch_prefill(const PrefillParams& p, hipStream_t stream) {
   if (p.D == 64) return p.bf16 ? launch_prefill_d64_bf16(p, stream) : launch_prefill_d64_f16(p, stream);
   return p.bf16 ? launch_prefill_d128_bf16(p, stream) : launch_prefill_d128_f16(p, stream);
+}
+
+hipError_t launch_prefill_lse(const PrefillLseParams& p, hipStream_t stream) {
+  if (p.D == 64) return p.bf16 ? launch_prefill_lse_d64_bf16(p, stream) : launch_prefill_lse_d64_f16(p, stream);
+  return p.bf16 ? launch_prefill_lse_d128_bf16(p, stream) : launch_prefill_lse_d128_f16(p, stream);
 }
 #endif
 

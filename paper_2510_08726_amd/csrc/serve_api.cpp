@@ -11,8 +11,14 @@
 #include "../../include/kv4.h"
 #include "../../include/rope.h"
 #include "launch.h"
+#include "span.h"
 
 namespace {
+
+using attn::apart;
+using attn::misaligned;
+using attn::Span;
+using attn::span;
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int64_t kMaxInt = std::numeric_limits<int32_t>::max();
@@ -20,8 +26,6 @@ constexpr int64_t kMaxElements = int64_t(1) << 40;
 constexpr int64_t kMaxTokens = int64_t(1) << 30;   // that a sequence's table row may hold
 
 constexpr int64_t kMaxGroups = (int64_t(1) << 24) - 1;   // workgroups of 256 threads in a row of a grid: under 2^32 threads
-
-bool misaligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) != 0; }
 
 // log2 of a page size, or -1.
 int page_shift(int page) {
@@ -70,35 +74,6 @@ bool tokens_ok(int L, int D) { return L <= kMaxGroups * (2048 / D); }
 
 bool kv4_type(int D, attn_dtype dtype) {
   return (D == 64 || D == 128) && (dtype == ATTN_F16 || dtype == ATTN_BF16);
-}
-
-// The bytes that an operand spans.
-struct Span {
-  uintptr_t begin, end;
-};
-
-Span span(const void* p, int64_t bytes) {
-  const uintptr_t at = reinterpret_cast<uintptr_t>(p);
-  return {at, p ? at + (uintptr_t)bytes : at};
-}
-
-// Those of rows of D 16-bit elements, with strides of batches, heads and tokens of either sign.
-Span span(const void* p, const long long* strides, int B, int H, int L, int D) {
-  const int n[3] = {B, H, L};
-  __int128 low = 0, high = D;
-  for (int i = 0; i < 3; ++i) {
-    const __int128 reach = (__int128)(n[i] - 1) * strides[i];
-    (reach < 0 ? low : high) += reach;
-  }
-  const uintptr_t at = reinterpret_cast<uintptr_t>(p);
-  return {at + (uintptr_t)(2 * low), at + (uintptr_t)(2 * high)};
-}
-
-// Whether `out`, which a call writes, lies apart from all the others.
-bool apart(Span out, std::initializer_list<Span> others) {
-  for (const Span& x : others)
-    if (x.begin < out.end && out.begin < x.end) return false;
-  return true;
 }
 
 // (More than 2^62 bytes are no cache.)

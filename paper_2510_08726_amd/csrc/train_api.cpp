@@ -1,0 +1,172 @@
+// C ABI of the operators of a training step (include/attn_bwd.h):
+// argument validation on the host, before anything is enqueued.
+
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+#include <limits>
+
+#include "../../include/attn.h"
+#include "../../include/attn_bwd.h"
+#include "launch.h"
+#include "span.h"
+
+namespace {
+
+using attn::apart;
+using attn::misaligned;
+using attn::Span;
+using attn::span;
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr int64_t kMaxInt = std::numeric_limits<int32_t>::max();
+constexpr int64_t kMaxElements = int64_t(1) << 40;
+constexpr int64_t kMaxGroups = (int64_t(1) << 24) - 1;   // workgroups of 256 threads in a row of a grid: under 2^32 threads
+
+int done(hipError_t e) { return e == hipSuccess ? ATTN_OK : attn::hip_fail(e); }
+
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// Sizes that both passes take: a head's rows are addressed with 32-bit byte offsets.
+bool sizes_ok(int B, int Hq, int Hkv, int Lq, int Lk, int D) {
+  if (B < 1 || Hq < 1 || Hkv < 1 || Lq < 1 || Lk < 1 || Hq % Hkv) return false;
+  if ((int64_t)Lq * D * 2 > kMaxInt || (int64_t)Lk * D * 2 > kMaxInt) return false;
+  return (int64_t)B * Hq <= kMaxInt && (int64_t)B * Hq * Lq <= kMaxElements / D && (int64_t)B * Hkv * Lk <= kMaxElements / D;
+}
+
+// What both passes refuse beside their pointers; ATTN_OK for none.
+int check(int B, int Hq, int Hkv, int Lq, int Lk, int D, int causal, float scale, const float* alibi_slopes,
+          float softcap, int window, attn_dtype dtype) {
+  if ((D != 64 && D != 128) || (dtype != ATTN_F16 && dtype != ATTN_BF16)) {
+    return B < 1 || Hq < 1 || Hkv < 1 || Lq < 1 || Lk < 1 || Hq % Hkv ? ATTN_ERR_SHAPE : ATTN_ERR_UNSUPPORTED;
+  }
+  if (!sizes_ok(B, Hq, Hkv, Lq, Lk, D) || !std::isfinite(scale)) return ATTN_ERR_SHAPE;
+  if (!std::isfinite(softcap) || softcap < 0.f || window < 0) return ATTN_ERR_SHAPE;
+  if (softcap > 0.f && (!causal || alibi_slopes)) return ATTN_ERR_UNSUPPORTED;
+  if (window > 0 && !causal) return ATTN_ERR_UNSUPPORTED;
+  if (softcap > ATTN_TRAIN_MAX_SOFTCAP) return ATTN_ERR_UNSUPPORTED;
+  return ATTN_OK;
+}
+
+// Sizes, parts and workspace of a backward pass.
+struct BwdPlan {
+  attn::BwdParams p;
+  int64_t stats, peaks, dkv, dq;     // floats of each part of the workspace
+  size_t bytes() const { return (size_t)(stats + peaks + dkv + dq) * sizeof(float); }
+  int64_t groups;                    // the most workgroups of a kernel
+};
+
+BwdPlan plan(int B, int Hq, int Hkv, int Lq, int Lk, int D, bool causal, int window) {
+  BwdPlan r{};
+  attn::BwdParams& p = r.p;
+  p.B = B; p.Hq = Hq; p.Hkv = Hkv; p.Lq = Lq; p.Lk = Lk; p.D = D;
+  p.group = Hq / Hkv;
+  p.causal = causal;
+  p.window = std::min(window, Lk);      // (that many mask nothing)
+  p.row0 = causal ? std::max(0, Lq - Lk) : 0;
+  p.rows = Lq - p.row0;
+  p.row_tiles = (int)ceil_div(p.rows, 32);
+  p.row_blocks = (int)ceil_div(p.rows, attn::bwd_rows_per_block());
+  p.key_blocks = (int)ceil_div(Lk, attn::bwd_rows_per_block());
+  p.hg = 1;
+  while (p.hg < 4 && p.group % (2 * p.hg) == 0) p.hg *= 2;
+  const int64_t units = (int64_t)B * Hkv, heads = (int64_t)B * Hq;
+  p.shares = units % 8 == 0;
+  p.dkv_parts = p.dq_parts = 1;
+  const auto floats = [](int64_t n) { return (n + 63) / 64 * 64; };
+  r.stats = floats(heads * p.row_tiles * 64);
+  r.peaks = floats(heads * p.row_blocks + units * p.key_blocks);
+  r.dkv = p.dkv_parts > 1 ? floats(2 * p.dkv_parts * units * Lk * D) : 0;
+  r.dq = p.dq_parts > 1 ? floats(p.dq_parts * heads * Lq * D) : 0;
+  const int64_t bm = attn::bwd_block_keys() / p.hg;
+  r.groups = std::max({heads * (p.row_blocks + ceil_div(p.row0, attn::bwd_rows_per_block())) + units * p.key_blocks,
+                       units * ceil_div(Lk, attn::bwd_block_keys()) * p.dkv_parts + 8,
+                       heads / p.hg * ceil_div(p.rows, bm) * p.dq_parts + 8,
+                       ceil_div(units * Lk * D, 1024), ceil_div(heads * Lq * D, 1024)});
+  return r;
+}
+
+}  // namespace
+
+extern "C" {
+
+int attn_fwd_lse(const void* Q, const void* K, const void* V, void* O, float* lse, int B, int Hq, int Hkv, int Lq,
+                 int Lk, int D, int causal, float scale, const float* alibi_slopes, float softcap, int window,
+                 attn_dtype dtype, hipStream_t stream) {
+  if (!Q || !K || !V || !O || !lse) return ATTN_ERR_NULL;
+  if (int rc = check(B, Hq, Hkv, Lq, Lk, D, causal, scale, alibi_slopes, softcap, window, dtype); rc != ATTN_OK) return rc;
+  const int64_t nqb = ceil_div(Lq, attn::prefill_block_rows());
+  if (nqb * 4 * B * Hq > kMaxInt) return ATTN_ERR_SHAPE;
+  const int64_t q = 2LL * B * Hq * Lq * D, k = 2LL * B * Hkv * Lk * D, l = 4LL * B * Hq * Lq;
+  const Span in[] = {span(Q, q), span(K, k), span(V, k), span(alibi_slopes, 4LL * Hq)};
+  if (!apart(span(O, q), {in[0], in[1], in[2], in[3], span(lse, l)}) || !apart(span(lse, l), {in[0], in[1], in[2], in[3]}))
+    return ATTN_ERR_SHAPE;
+  attn::PrefillLseParams p{};
+  p.q = Q; p.k = K; p.v = V; p.o = O; p.lse = lse;
+  p.slopes = alibi_slopes;
+  p.B = B; p.Hq = Hq; p.Hkv = Hkv; p.Lq = Lq; p.Lk = Lk; p.D = D;
+  p.group = Hq / Hkv;
+  p.causal = causal != 0;
+  p.bf16 = dtype == ATTN_BF16;
+  p.cap_k2 = softcap > 0.f ? 2.f / softcap : 0.f;
+  p.cap_cl = softcap > 0.f ? softcap * kLog2e : 0.f;
+  p.window = std::min(window, Lk);
+  if (alibi_slopes || softcap > 0.f) {
+    p.c = scale * kLog2e;
+  } else {     // above zero, so that masked (-inf) scores stay so
+    p.c = std::fmax(std::fabs(scale) * kLog2e, 1e-30f);
+    p.qsign = std::signbit(scale) ? 0x80008000u : 0u;
+  }
+  return done(attn::launch_prefill_lse(p, stream));
+}
+
+size_t attn_bwd_workspace_bytes(int B, int Hq, int Hkv, int Lq, int Lk, int D, int causal, int window) {
+  if ((D != 64 && D != 128) || !sizes_ok(B, Hq, Hkv, Lq, Lk, D) || window < 0) return 0;
+  return plan(B, Hq, Hkv, Lq, Lk, D, causal != 0, window).bytes();
+}
+
+int attn_bwd(const void* dO, const long long* do_strides, const void* Q, const void* K, const void* V, const void* O,
+             const float* lse, void* dQ, void* dK, void* dV, int B, int Hq, int Hkv, int Lq, int Lk, int D, int causal,
+             float scale, const float* alibi_slopes, float softcap, int window, void* workspace,
+             size_t workspace_bytes, attn_dtype dtype, hipStream_t stream) {
+  if (!dO || !do_strides || !Q || !K || !V || !O || !lse || !dQ || !dK || !dV || !workspace) return ATTN_ERR_NULL;
+  if (int rc = check(B, Hq, Hkv, Lq, Lk, D, causal, scale, alibi_slopes, softcap, window, dtype); rc != ATTN_OK) return rc;
+  for (const void* x : {dO, Q, K, V, O, (const void*)dQ, (const void*)dK, (const void*)dV})
+    if (misaligned(x)) return ATTN_ERR_SHAPE;
+  const int n[3] = {B, Hq, Lq};
+  for (int i = 0; i < 3; ++i)
+    if (do_strides[i] < 0 || do_strides[i] % 8 || do_strides[i] > kMaxElements / n[i]) return ATTN_ERR_SHAPE;
+  const long long row = Lq > 1 ? do_strides[2] : D;
+  if (2 * row * Lq > kMaxInt) return ATTN_ERR_SHAPE;
+  BwdPlan w = plan(B, Hq, Hkv, Lq, Lk, D, causal != 0, window);
+  if (w.groups > kMaxGroups) return ATTN_ERR_SHAPE;
+  if (workspace_bytes < w.bytes() || misaligned(workspace)) return ATTN_ERR_WORKSPACE;
+  const int64_t q = 2LL * B * Hq * Lq * D, k = 2LL * B * Hkv * Lk * D;
+  const Span out[] = {span(dQ, q), span(dK, k), span(dV, k), span(workspace, (int64_t)w.bytes())};
+  const Span in[] = {span(dO, do_strides, B, Hq, Lq, D), span(Q, q), span(K, k), span(V, k), span(O, q),
+                     span(lse, 4LL * B * Hq * Lq), span(alibi_slopes, 4LL * Hq)};
+  for (int i = 0; i < 4; ++i) {
+    if (!apart(out[i], {in[0], in[1], in[2], in[3], in[4], in[5], in[6]})) return ATTN_ERR_SHAPE;
+    for (int j = 0; j < i; ++j)
+      if (!apart(out[i], {out[j]})) return ATTN_ERR_SHAPE;
+  }
+  attn::BwdParams& p = w.p;
+  p.q = Q; p.k = K; p.v = V; p.o = O; p.d_o = dO; p.lse = lse;
+  p.slopes = alibi_slopes;
+  p.dq = dQ; p.dk = dK; p.dv = dV;
+  p.stats = static_cast<float*>(workspace);
+  p.peaks = p.stats + w.stats;
+  p.ws_dkv = p.peaks + w.peaks;
+  p.ws_dq = p.ws_dkv + w.dkv;
+  p.do_sb = do_strides[0]; p.do_sh = do_strides[1]; p.do_sl = row;
+  p.bf16 = dtype == ATTN_BF16;
+  p.sign = std::signbit(scale) ? 0x80008000u : 0u;
+  // Above zero: a row's log-sum-exp starts its scores, divided by it.
+  p.c = std::fmax(std::fabs(scale) * kLog2e, 1e-30f);
+  p.scale = scale;
+  p.cap_k2 = softcap > 0.f ? 2.f / softcap * p.c : 0.f;
+  p.cap_cl = softcap > 0.f ? softcap * kLog2e : 0.f;
+  return done(attn::launch_attn_bwd(p, stream));
+}
+
+}  // extern "C"
