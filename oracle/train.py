@@ -65,3 +65,45 @@ def attention_grad(do, q, k, v, *, scale, causal=False, alibi_slopes=None, softc
             r["dk_abs"][b, kh] += np.abs(dS).T @ np.abs(qq)
             r["dk_delta"][b, kh] += off.T @ np.abs(qq)
     return r
+
+
+def rmsnorm(h, weight, eps, offset):
+    """y and rstd of rows h [N, M] in float64 (weight None: ones, without the offset)."""
+    rstd = 1.0 / np.sqrt((h * h).mean(-1) + eps)
+    return h * rstd[:, None] * (1.0 if weight is None else weight + offset), rstd
+
+
+def rmsnorm_grad(dy, h, rstd, weight, dh, offset):
+    """dx and dweight, and their sums of magnitudes: (dx, dw, of dx's terms, of the mean behind dx, of dw)."""
+    n = h * rstd[:, None]
+    g = dy * (1.0 if weight is None else weight + offset)
+    mean, size = (g * n).mean(-1, keepdims=True), np.abs(g * n).mean(-1, keepdims=True)
+    r = rstd[:, None]
+    d = r * (g - n * mean) + (0.0 if dh is None else dh)
+    terms = r * (np.abs(g) + np.abs(n * mean)) + (0.0 if dh is None else np.abs(dh))
+    return d, (dy * n).sum(0), terms, r * np.abs(n) * size, np.abs(dy * n).sum(0)
+
+
+def codes8(y, code, group):
+    """The values of the codes nearest to y / scale (ties to even), and the scales in fp32: y [N, M] in groups."""
+    N, M = y.shape
+    step = group or M
+    values, scales = np.zeros_like(y), []
+    if code == "int8":
+        grid = np.arange(128.0)
+    else:     # 4 bits of exponent (bias 7), 3 of mantissa
+        grid = np.array([(m * 2.0 ** -9 if e == 0 else (8 + m) * 2.0 ** (e - 10)) for e in range(16) for m in range(8)][:127])
+    for a in range(0, M, step):
+        part = y[:, a:a + step]
+        with np.errstate(invalid="ignore", over="ignore"):
+            s = (np.abs(part).max(-1) / grid[-1]).astype(np.float32)
+        s = np.where(np.isfinite(s), s, np.float32(np.nan))
+        scales.append(s)
+        fine = np.isfinite(s) & (s > 0)
+        z = np.where(fine[:, None], np.abs(part) / np.where(fine, s, 1.0).astype(np.float64)[:, None], 0.0)
+        hi = np.clip(np.searchsorted(grid, z), 1, len(grid) - 1)
+        lo = hi - 1
+        below, above = z - grid[lo], grid[hi] - z
+        at = np.where((below < above) | ((below == above) & (lo % 2 == 0)), lo, hi)
+        values[:, a:a + step] = grid[at] * np.where(fine[:, None], np.sign(part), 0.0)
+    return values, np.stack(scales, -1)

@@ -27,6 +27,7 @@ __all__ = [
     "rope_frequencies", "rope_fwd", "rope_bwd", "kv4_page_bytes", "kv_slots", "kv4_append", "kv4_load",
     "attn_decode_kv4", "attn_decode_kv4_workspace_bytes",
     "attn_fwd_lse", "attn_bwd", "attn_bwd_workspace_bytes",
+    "rmsnorm_add", "rmsnorm_add_quant", "quant8_load", "rmsnorm_add_bwd", "rmsnorm_add_bwd_workspace_bytes",
     "attn_status_string", "attn_last_hip_error", "library_path", "load_library", "AttnError",
     "ATTN_OK", "ATTN_ERR_NULL", "ATTN_ERR_SHAPE", "ATTN_ERR_UNSUPPORTED", "ATTN_ERR_WORKSPACE",
     "ATTN_ERR_HIP",
@@ -142,6 +143,16 @@ def load_library():
     lib.attn_bwd_workspace_bytes.restype = cs
     lib.attn_bwd.argtypes = [vp] * 10 + [ci] * 7 + [cf, vp, cf, ci, vp, cs, ci, vp]
     lib.attn_bwd.restype = ci
+    lib.rmsnorm_add.argtypes = [vp] * 6 + [ci, ci, cd, cf, ci, ci, vp]
+    lib.rmsnorm_add.restype = ci
+    lib.rmsnorm_add_quant.argtypes = [vp] * 7 + [ci, ci, ci, ci, cd, cf, ci, ci, vp]
+    lib.rmsnorm_add_quant.restype = ci
+    lib.quant8_load.argtypes = [vp, vp, vp, ci, ci, ci, ci, ci, vp]
+    lib.quant8_load.restype = ci
+    lib.rmsnorm_add_bwd_workspace_bytes.argtypes = [ci, ci]
+    lib.rmsnorm_add_bwd_workspace_bytes.restype = cs
+    lib.rmsnorm_add_bwd.argtypes = [vp] * 8 + [ci, ci, cf, vp, cs, ci, ci, vp]
+    lib.rmsnorm_add_bwd.restype = ci
     lib.attn_status_string.argtypes = [ci]
     lib.attn_status_string.restype = ctypes.c_char_p
     lib.attn_last_hip_error.argtypes = []
@@ -160,7 +171,7 @@ class _NotBuilt:
 
     attn_fwd = attn_decode = attn_decode_noalloc = norm_l2 = rmsnorm_rowmax = _none
     rope = kv_slots = kv4_append = kv4_load = attn_decode_kv4 = _none
-    attn_fwd_lse = attn_bwd = _none
+    attn_fwd_lse = attn_bwd = rmsnorm_add = rmsnorm_add_quant = quant8_load = rmsnorm_add_bwd = _none
 
 
 def _load_binding():
@@ -958,6 +969,181 @@ def attn_bwd(do, q, k, v, o, lse, dq=None, dk=None, dv=None, *, causal=False, sc
                                        workspace.numel() * workspace.element_size(), _DTYPE_CODE[q.dtype],
                                        _stream(stream)))
     return dq, dk, dv
+
+
+# The norm between a model's layers.
+
+_QUANT8_CODE = {torch.float8_e4m3fn: 0, torch.int8: 1}
+
+
+def _norm_rows(name, x):
+    """Rows and their length of x [..., M]."""
+    _require(x.dim() >= 1 and x.is_contiguous(), f"{name} must be contiguous [..., M]")
+    _require(x.dtype in _NORM_CODE, f"{name} must be float16, bfloat16 or float32")
+    M = x.shape[-1]
+    _require(M >= 1 and x.numel() >= 1, f"{name} must not be empty")
+    N = x.numel() // M
+    _same_device(x)
+    _require(_fits(N, M), "sizes must fit 32 bits")
+    return N, M
+
+
+def _norm_inputs(x, residual, weight):
+    N, M = _norm_rows("x", x)
+    if residual is not None:
+        _same_device(x, residual=residual)
+        _require(residual.shape == x.shape and residual.is_contiguous() and residual.dtype in (x.dtype, torch.float32),
+                 "residual must be a contiguous tensor shaped like x, of its dtype or float32")
+    _norm_weight(x, weight, M)
+    return N, M, x.dtype if residual is None else residual.dtype
+
+
+def _norm_weight(x, weight, M):
+    if weight is not None:
+        _same_device(x, weight=weight)
+        _ints("weight", weight, x.dtype, (M,))
+
+
+def rmsnorm_add(x, residual=None, weight=None, y=None, h=None, rstd=None, *, eps=1e-6, weight_offset=0.0, stream=None):
+    """h = x + residual, rstd = 1 / sqrt(mean(h^2) + eps), y = h rstd (weight + weight_offset).
+
+    x [..., M] (float16, bfloat16 or float32, contiguous, M at most 32768),
+    ``residual`` like x or in float32, ``weight`` [M] of x's dtype (None: ones, and no
+    offset).  h has the residual's dtype, and is x itself without a residual; y has x's; ``rstd`` [...]
+    is float32.  y may be x itself and h the residual; otherwise outputs share
+    memory with nothing.  Nothing is recorded for autograd: a program that trains
+    calls rmsnorm_add_bwd.  Returns (y, h, rstd).
+    """
+    r = (_BINDING or _load_binding()).rmsnorm_add(x, residual, weight, y, h, rstd, eps, weight_offset, stream)
+    if r is not None:
+        return _result(r)
+    N, M, wide = _norm_inputs(x, residual, weight)
+    _require(residual is not None or h is None, "h without a residual is x")
+    stream = _on_device(x, stream)
+    y = _given("y", y, x, stream)
+    h = x if residual is None else _given("h", h, residual, stream)
+    rstd = _given("rstd", rstd, x, stream, x.shape[:-1], torch.float32)
+    with torch.cuda.device(x.device):
+        _check(load_library().rmsnorm_add(_ptr(x), _ptr(residual), _ptr(weight), _ptr(y),
+                                          None if residual is None else _ptr(h), _ptr(rstd), N, M, float(eps),
+                                          float(weight_offset), _NORM_CODE[x.dtype], _NORM_CODE[wide], _stream(stream)))
+    return y, h, rstd
+
+
+def _quant_groups(M, group):
+    group = int(group)
+    _require(group in (0, 32, 64, 128, 256), "group must be 0 (the whole row), 32, 64, 128 or 256")
+    return group, -(-M // group) if group else 1
+
+
+def rmsnorm_add_quant(x, residual=None, weight=None, q=None, scales=None, h=None, rstd=None, *,
+                      dtype=torch.float8_e4m3fn, group=0, eps=1e-6, weight_offset=0.0, stream=None):
+    """rmsnorm_add with y in 8 bits: codes q [..., M] (``dtype``: float8_e4m3fn or int8)
+    and scales [..., groups] (float32), y ~ q * scale.
+
+    ``group`` elements share a scale: 0 for the whole row (one scale), or 32, 64, 128
+    or 256 (the last one may be short).  The scale is the group's largest |y| over 448 or 127;
+    y / scale is rounded to the nearest, ties to even.  Zeros have scale 0; a group with an infinity or NaN
+    has scale NaN.  ``rstd`` [...] float32 is written if given.  h may be the residual
+    itself; otherwise outputs share memory with nothing.  Returns (q, scales, h).
+    """
+    r = (_BINDING or _load_binding()).rmsnorm_add_quant(x, residual, weight, q, scales, h, rstd, dtype, group, eps,
+                                                        weight_offset, stream)
+    if r is not None:
+        return _result(r)
+    N, M, wide = _norm_inputs(x, residual, weight)
+    _require(dtype in _QUANT8_CODE, "dtype must be float8_e4m3fn or int8")
+    group, groups = _quant_groups(M, group)
+    _require(residual is not None or h is None, "h without a residual is x")
+    stream = _on_device(x, stream)
+    q = _given("q", q, x, stream, dtype=dtype)
+    scales = _given("scales", scales, x, stream, (*x.shape[:-1], groups), torch.float32)
+    h = x if residual is None else _given("h", h, residual, stream)
+    if rstd is not None:
+        rstd = _given("rstd", rstd, x, stream, x.shape[:-1], torch.float32)
+    with torch.cuda.device(x.device):
+        _check(load_library().rmsnorm_add_quant(_ptr(x), _ptr(residual), _ptr(weight), _ptr(q), _ptr(scales),
+                                                None if residual is None else _ptr(h), _ptr(rstd), N, M, group,
+                                                _QUANT8_CODE[dtype], float(eps), float(weight_offset),
+                                                _NORM_CODE[x.dtype], _NORM_CODE[wide], _stream(stream)))
+    return q, scales, h
+
+
+def quant8_load(q, scales, y=None, *, group=0, dtype=torch.bfloat16, stream=None):
+    """What rows in 8 bits stand for: y [..., M] = q * scale, formed in 32 bits and
+    rounded to ``dtype`` (float16, bfloat16 or float32).  q [..., M] float8_e4m3fn or int8, scales [..., groups]
+    float32 and ``group`` as for rmsnorm_add_quant.  Returns y."""
+    r = (_BINDING or _load_binding()).quant8_load(q, scales, y, group, dtype, stream)
+    if r is not None:
+        return _result(r)
+    _require(q.dim() >= 1 and q.is_contiguous() and q.numel() >= 1, "q must be contiguous [..., M], not empty")
+    _require(q.dtype in _QUANT8_CODE, "q must be float8_e4m3fn or int8")
+    _require(dtype in _NORM_CODE, "dtype must be float16, bfloat16 or float32")
+    M = q.shape[-1]
+    group, groups = _quant_groups(M, group)
+    _same_device(q, scales=scales)
+    _ints("scales", scales, torch.float32, (*q.shape[:-1], groups))
+    N = q.numel() // M
+    _require(_fits(N, M), "sizes must fit 32 bits")
+    stream = _on_device(q, stream)
+    y = _given("y", y, q, stream, dtype=dtype)
+    with torch.cuda.device(q.device):
+        _check(load_library().quant8_load(_ptr(q), _ptr(scales), _ptr(y), N, M, group, _QUANT8_CODE[q.dtype],
+                                          _NORM_CODE[dtype], _stream(stream)))
+    return y
+
+
+def rmsnorm_add_bwd_workspace_bytes(N, M):
+    return load_library().rmsnorm_add_bwd_workspace_bytes(N, M) if _fits(N, M) else 0
+
+
+def rmsnorm_add_bwd(dy, h, rstd, weight=None, dh=None, dx=None, dresidual=None, dweight=None, *, weight_offset=0.0,
+                    workspace=None, stream=None):
+    """Gradients of rmsnorm_add.
+
+    ``dy`` [..., M] is the gradient of y, ``h`` and ``rstd`` what rmsnorm_add
+    returned, ``dh`` (like h, or None) the gradient that reaches h past the norm, as a
+    residual stream has one.  Returns (dx, dresidual, dweight): dx of dy's dtype;
+    dresidual of h's, which is dx itself where they are one dtype; dweight [M] float32, None
+    without a weight.  ``workspace`` (uint8 GPU tensor of rmsnorm_add_bwd_workspace_bytes(N, M)) is allocated
+    when not given.  dx may be dy itself, or dh of its dtype, and dresidual dh; otherwise what is
+    written shares memory with nothing.
+    """
+    r = (_BINDING or _load_binding()).rmsnorm_add_bwd(dy, h, rstd, weight, dh, dx, dresidual, dweight, weight_offset,
+                                                      workspace, stream)
+    if r is not None:
+        return _result(r)
+    N, M = _norm_rows("dy", dy)
+    _same_device(dy, h=h, rstd=rstd)
+    _require(h.shape == dy.shape and h.is_contiguous() and h.dtype in (dy.dtype, torch.float32),
+             "h must be a contiguous tensor shaped like dy, of its dtype or float32")
+    _ints("rstd", rstd, torch.float32, dy.shape[:-1])
+    _norm_weight(dy, weight, M)
+    if dh is not None:
+        _same_device(dy, dh=dh)
+        _ints("dh", dh, h.dtype, h.shape)
+    same = h.dtype == dy.dtype
+    _require(not same or dresidual is None, "dresidual of dx's dtype is dx")
+    _require(weight is not None or dweight is None, "dweight needs a weight")
+    stream = _on_device(dy, stream)
+    dx = _given("dx", dx, dy, stream)
+    if not same:
+        dresidual = _given("dresidual", dresidual, h, stream)
+    if weight is not None:
+        dweight = _given("dweight", dweight, dy, stream, (M,), torch.float32)
+        if workspace is None:
+            _require(isinstance(stream, torch.cuda.Stream), "a stream of this kind needs a workspace of the caller's")
+            workspace = _allocate((max(rmsnorm_add_bwd_workspace_bytes(N, M), 16),), dy, stream, torch.uint8)
+    if workspace is not None:
+        _same_device(dy, workspace=workspace)
+        _require(workspace.is_contiguous(), "workspace must be contiguous")
+    with torch.cuda.device(dy.device):
+        _check(load_library().rmsnorm_add_bwd(_ptr(dy), _ptr(h), _ptr(rstd), _ptr(weight), _ptr(dh), _ptr(dx),
+                                              None if same else _ptr(dresidual), _ptr(dweight), N, M,
+                                              float(weight_offset), _ptr(workspace),
+                                              0 if workspace is None else workspace.numel() * workspace.element_size(),
+                                              _NORM_CODE[dy.dtype], _NORM_CODE[h.dtype], _stream(stream)))
+    return dx, dx if same else dresidual, dweight
 
 
 def norm_partials(workspace, N, chunks):

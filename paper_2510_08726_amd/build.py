@@ -56,7 +56,7 @@ UNITS = [(f"prefill{k}", "prefill.hip", ["-fno-honor-nans", f"-DATTN_PREFILL_SHA
             ("prefill_split", "prefill_split.hip", ["-fno-honor-nans", "-save-temps"]),
             ("rope", "rope.hip", ["-save-temps"]), ("kv4", "kv4.hip", ["-save-temps"]),
             ("decode_kv4", "decode_kv4.hip", ["-save-temps"]),
-            ("attn_bwd", "attn_bwd.hip", ["-save-temps"]),
+            ("attn_bwd", "attn_bwd.hip", ["-save-temps"]), ("rmsnorm", "rmsnorm.hip", ["-save-temps"]),
             ("attn_api", "attn_api.cpp", []), ("serve_api", "serve_api.cpp", []),
             ("train_api", "train_api.cpp", [])]
 

@@ -18,6 +18,7 @@
 #include <cmath>
 #include <initializer_list>
 #include <utility>
+#include <vector>
 
 #include <ATen/ATen.h>
 #include <ATen/hip/EmptyTensor.h>
@@ -30,6 +31,7 @@
 #include "../../include/attn_bwd.h"
 #include "../../include/kv4.h"
 #include "../../include/norms.h"
+#include "../../include/rmsnorm.h"
 #include "../../include/rope.h"
 
 namespace {
@@ -673,6 +675,180 @@ PyObject* py_attn_bwd(PyObject*, PyObject* const* x, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
+bool real(PyObject* obj, double& x) {
+  if (!PyFloat_CheckExact(obj)) return false;
+  x = PyFloat_AS_DOUBLE(obj);
+  return true;
+}
+
+bool norm_type(at::ScalarType t, norm_dtype& d) {
+  if (t == at::kHalf) d = NORM_F16;
+  else if (t == at::kBFloat16) d = NORM_BF16;
+  else if (t == at::kFloat) d = NORM_F32;
+  else return false;
+  return true;
+}
+
+bool code_type(at::ScalarType t, quant8_code& c) {
+  if (t == at::kFloat8_e4m3fn) c = QUANT8_E4M3;
+  else if (t == at::kChar) c = QUANT8_INT8;
+  else return false;
+  return true;
+}
+
+// Rows [..., M] on the current device.
+const at::Tensor* norm_rows(PyObject* obj, int& N, int& M) {
+  const at::Tensor* t = here(obj);
+  if (!t || t->dim() < 1 || t->numel() < 1) return nullptr;
+  const int64_t m = t->size(-1), n = t->numel() / m;
+  if (n > INT_MAX) return nullptr;
+  N = (int)n;
+  M = (int)m;
+  return t;
+}
+
+// x, its residual and its weight.
+struct Rows {
+  const at::Tensor *x, *residual = nullptr, *weight = nullptr;
+  norm_dtype dtype, wide;
+  at::ScalarType type;
+  int N, M;
+  float offset;
+  double eps;
+  const void* ptr(const at::Tensor* t) const { return t ? t->data_ptr() : nullptr; }
+};
+
+bool norm_inputs(PyObject* x, PyObject* residual, PyObject* weight, PyObject* eps, PyObject* offset, Rows& a) {
+  a.x = norm_rows(x, a.N, a.M);
+  if (!a.x || !real(eps, a.eps) || !number(offset, a.offset)) return false;
+  a.type = a.x->scalar_type();
+  if (!norm_type(a.type, a.dtype)) return false;
+  a.wide = a.dtype;
+  if (residual != Py_None) {
+    a.residual = here(residual);
+    if (!a.residual || a.residual->sizes() != a.x->sizes()) return false;
+    if (!norm_type(a.residual->scalar_type(), a.wide) || (a.wide != a.dtype && a.wide != NORM_F32)) return false;
+  }
+  if (weight != Py_None && !(a.weight = here(weight, a.type, {a.M}))) return false;
+  return true;
+}
+
+// (x, residual, weight, y, h, rstd, eps, weight_offset, stream) -> (y, h, rstd)
+PyObject* py_rmsnorm_add(PyObject*, PyObject* const* x, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  Rows a;
+  if (n != 9 || x[8] != Py_None || !norm_inputs(x[0], x[1], x[2], x[6], x[7], a)) return none();
+  if (!a.residual && x[4] != Py_None) return none();
+  at::Tensor y, h, rstd;
+  if (!output(x[3], *a.x, a.type, a.x->sizes(), y)) return none();
+  if (a.residual && !output(x[4], *a.x, a.residual->scalar_type(), a.x->sizes(), h)) return none();
+  if (!output(x[5], *a.x, at::kFloat, a.x->sizes().slice(0, a.x->dim() - 1), rstd)) return none();
+  const void *px = a.x->data_ptr(), *pr = a.ptr(a.residual), *pw = a.ptr(a.weight);
+  void *py = y.data_ptr(), *ph = a.residual ? h.data_ptr() : nullptr;
+  float* ps = static_cast<float*>(rstd.data_ptr());
+  const hipStream_t s = stream();
+  const int rc =
+      unlocked([&] { return rmsnorm_add(px, pr, pw, py, ph, ps, a.N, a.M, a.eps, a.offset, a.dtype, a.wide, s); });
+  // (Without a residual h is x.)
+  return results(rc, {{x[3], &y}, {a.residual ? x[4] : x[0], &h}, {x[5], &rstd}});
+  END_HANDLE_TH_ERRORS
+}
+
+// (x, residual, weight, q, scales, h, rstd, dtype, group, eps, weight_offset, stream) -> (q, scales, h)
+PyObject* py_rmsnorm_add_quant(PyObject*, PyObject* const* x, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  Rows a;
+  int group;
+  quant8_code code;
+  if (n != 12 || x[11] != Py_None || !THPDtype_Check(x[7]) || !whole(x[8], group)) return none();
+  const auto type = reinterpret_cast<THPDtype*>(x[7])->scalar_type;
+  if (!code_type(type, code) || !norm_inputs(x[0], x[1], x[2], x[9], x[10], a)) return none();
+  if ((!a.residual && x[5] != Py_None) || (group != 0 && group != 32 && group != 64 && group != 128 && group != 256))
+    return none();
+  const auto lead = a.x->sizes().slice(0, a.x->dim() - 1);
+  std::vector<int64_t> shape(lead.begin(), lead.end());
+  shape.push_back(group ? ((int64_t)a.M + group - 1) / group : 1);
+  at::Tensor q, scales, h, rstd;
+  if (!output(x[3], *a.x, type, a.x->sizes(), q) || !output(x[4], *a.x, at::kFloat, shape, scales)) return none();
+  if (a.residual && !output(x[5], *a.x, a.residual->scalar_type(), a.x->sizes(), h)) return none();
+  if (x[6] != Py_None && !output(x[6], *a.x, at::kFloat, lead, rstd)) return none();
+  const void *px = a.x->data_ptr(), *pr = a.ptr(a.residual), *pw = a.ptr(a.weight);
+  void *pq = q.data_ptr(), *ph = a.residual ? h.data_ptr() : nullptr;
+  float *pc = static_cast<float*>(scales.data_ptr()), *ps = x[6] != Py_None ? static_cast<float*>(rstd.data_ptr()) : nullptr;
+  const hipStream_t s = stream();
+  const int rc = unlocked([&] {
+    return rmsnorm_add_quant(px, pr, pw, pq, pc, ph, ps, a.N, a.M, group, code, a.eps, a.offset, a.dtype, a.wide, s);
+  });
+  return results(rc, {{x[3], &q}, {x[4], &scales}, {a.residual ? x[5] : x[0], &h}});
+  END_HANDLE_TH_ERRORS
+}
+
+// (q, scales, y, group, dtype, stream) -> y
+PyObject* py_quant8_load(PyObject*, PyObject* const* x, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  int N, M, group;
+  quant8_code code;
+  norm_dtype dtype;
+  if (n != 6 || x[5] != Py_None || !whole(x[3], group) || !THPDtype_Check(x[4])) return none();
+  if (group != 0 && group != 32 && group != 64 && group != 128 && group != 256) return none();
+  const auto type = reinterpret_cast<THPDtype*>(x[4])->scalar_type;
+  const at::Tensor* q = norm_rows(x[0], N, M);
+  if (!q || !code_type(q->scalar_type(), code) || !norm_type(type, dtype)) return none();
+  const auto lead = q->sizes().slice(0, q->dim() - 1);
+  std::vector<int64_t> shape(lead.begin(), lead.end());
+  shape.push_back(group ? ((int64_t)M + group - 1) / group : 1);
+  const at::Tensor* scales = here(x[1], at::kFloat, shape);
+  at::Tensor y;
+  if (!scales || !output(x[2], *q, type, q->sizes(), y)) return none();
+  const void* pq = q->data_ptr();
+  const float* pc = static_cast<const float*>(scales->data_ptr());
+  void* py = y.data_ptr();
+  const hipStream_t s = stream();
+  const int rc = unlocked([&] { return quant8_load(pq, pc, py, N, M, group, code, dtype, s); });
+  return result(rc, x[2], std::move(y));
+  END_HANDLE_TH_ERRORS
+}
+
+// (dy, h, rstd, weight, dh, dx, dresidual, dweight, weight_offset, workspace, stream) -> (dx, dresidual, dweight)
+PyObject* py_rmsnorm_add_bwd(PyObject*, PyObject* const* x, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  int N, M;
+  float offset;
+  norm_dtype dtype, wide;
+  if (n != 11 || x[10] != Py_None || !number(x[8], offset)) return none();
+  const at::Tensor *dy = norm_rows(x[0], N, M), *h = here(x[1]), *weight = nullptr, *dh = nullptr;
+  if (!dy || !h || h->sizes() != dy->sizes()) return none();
+  const auto type = dy->scalar_type(), wide_type = h->scalar_type();
+  if (!norm_type(type, dtype) || !norm_type(wide_type, wide) || (wide != dtype && wide != NORM_F32)) return none();
+  const at::Tensor* rstd = here(x[2], at::kFloat, dy->sizes().slice(0, dy->dim() - 1));
+  if (!rstd || (x[3] != Py_None && !(weight = here(x[3], type, {M})))) return none();
+  if (x[4] != Py_None && !(dh = here(x[4], wide_type, h->sizes()))) return none();
+  const bool same = dtype == wide;
+  if ((same && x[6] != Py_None) || (!weight && x[7] != Py_None)) return none();
+  at::Tensor dx, dres, dw, ws;
+  if (!output(x[5], *dy, type, dy->sizes(), dx) || (!same && !output(x[6], *dy, wide_type, dy->sizes(), dres))) return none();
+  if (weight && !output(x[7], *dy, at::kFloat, {M}, dw)) return none();
+  if (x[9] != Py_None) {
+    const at::Tensor* t = here(x[9]);
+    if (!t) return none();
+    ws = *t;
+  } else if (weight) {
+    ws = fresh({(int64_t)std::max<size_t>(rmsnorm_add_bwd_workspace_bytes(N, M), 16)}, at::kByte, *dy);
+  }
+  const void *pd = dy->data_ptr(), *ph = h->data_ptr(), *pw = weight ? weight->data_ptr() : nullptr,
+             *pg = dh ? dh->data_ptr() : nullptr;
+  const float* ps = static_cast<const float*>(rstd->data_ptr());
+  void *px = dx.data_ptr(), *pr = same ? nullptr : dres.data_ptr(), *wp = ws.defined() ? ws.data_ptr() : nullptr;
+  float* pdw = weight ? static_cast<float*>(dw.data_ptr()) : nullptr;
+  const size_t bytes = ws.defined() ? ws.nbytes() : 0;
+  const hipStream_t s = stream();
+  const int rc =
+      unlocked([&] { return rmsnorm_add_bwd(pd, ph, ps, pw, pg, px, pr, pdw, N, M, offset, wp, bytes, dtype, wide, s); });
+  at::Tensor dx2 = dx;
+  return results(rc, {{x[5], &dx}, {same ? x[5] : x[6], same ? &dx2 : &dres}, {x[7], weight ? &dw : nullptr}});
+  END_HANDLE_TH_ERRORS
+}
+
 template <PyObject* (*F)(PyObject*, PyObject* const*, Py_ssize_t)>
 PyCFunction fast() {
   return reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(F));
@@ -691,6 +867,10 @@ PyMethodDef methods[] = {
     {"attn_decode_kv4", fast<py_attn_decode_kv4>(), METH_FASTCALL, nullptr},
     {"attn_fwd_lse", fast<py_attn_fwd_lse>(), METH_FASTCALL, nullptr},
     {"attn_bwd", fast<py_attn_bwd>(), METH_FASTCALL, nullptr},
+    {"rmsnorm_add", fast<py_rmsnorm_add>(), METH_FASTCALL, nullptr},
+    {"rmsnorm_add_quant", fast<py_rmsnorm_add_quant>(), METH_FASTCALL, nullptr},
+    {"quant8_load", fast<py_quant8_load>(), METH_FASTCALL, nullptr},
+    {"rmsnorm_add_bwd", fast<py_rmsnorm_add_bwd>(), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

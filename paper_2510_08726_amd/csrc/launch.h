@@ -180,6 +180,54 @@ inline bool norm_one_kernel(bool rms, long long M, int elem, int chunks) {
   return chunks == 1 && (!rms || M * elem <= kNormRowBytes);
 }
 
+// The norm with the residual's addition (rmsnorm.hip).
+struct RmsnormParams {
+  const void* x;
+  const void* residual; // or nullptr
+  const void* weight;   // or nullptr
+  void* y;              // [N, M]: dtype, or codes
+  float* scales;        // [N, groups] of codes, or nullptr
+  void* h;
+  float* rstd;          // or nullptr
+  double eps;
+  int N, M;
+  int group, groups;    // elements that share a scale (0: the row), and scales of a row
+  float offset;         // added to the weight
+  int lanes;            // lanes of a row, set by the launcher
+  int dtype;            // 0 fp16, 1 bf16, 2 fp32
+  bool wide;            // residual and h in fp32
+  bool int8;            // codes: int8, or e4m3
+};
+hipError_t launch_rmsnorm_add(const RmsnormParams& p, hipStream_t stream);
+
+struct RmsnormBwdParams {
+  const void* dy;
+  const void* h;
+  const float* rstd;
+  const void* weight;   // or nullptr
+  const void* dh;       // or nullptr
+  void* dx;
+  void* dresidual;      // or nullptr
+  float* ws;            // [partials, M], or nullptr
+  int N, M;
+  float offset;
+  int lanes;            // set by the launcher
+  int dtype;
+  bool wide;
+};
+int64_t rmsnorm_bwd_partials(int64_t N, int M);
+hipError_t launch_rmsnorm_add_bwd(const RmsnormBwdParams& p, float* dweight, hipStream_t stream);
+
+struct Quant8LoadParams {
+  const unsigned char* codes;
+  const float* scales;
+  void* y;
+  int N, M, group, groups;
+  int dtype;
+  bool int8;
+};
+hipError_t launch_quant8_load(const Quant8LoadParams& p, hipStream_t stream);
+
 // Rotary positions (rope.hip).
 struct RopeParams {
   const void* x[2];     // queries, keys (or nullptr)

@@ -1,4 +1,4 @@
-// C ABI of the operators of a training step (include/attn_bwd.h):
+// C ABI of the operators of a training step (include/attn_bwd.h, include/rmsnorm.h):
 // argument validation on the host, before anything is enqueued.
 
 #include <algorithm>
@@ -8,6 +8,7 @@
 
 #include "../../include/attn.h"
 #include "../../include/attn_bwd.h"
+#include "../../include/rmsnorm.h"
 #include "launch.h"
 #include "span.h"
 
@@ -84,6 +85,53 @@ BwdPlan plan(int B, int Hq, int Hkv, int Lq, int Lk, int D, bool causal, int win
                        heads / p.hg * ceil_div(p.rows, bm) * p.dq_parts + 8,
                        ceil_div(units * Lk * D, 1024), ceil_div(heads * Lq * D, 1024)});
   return r;
+}
+
+int element_size(norm_dtype t) { return t == NORM_F32 ? 4 : 2; }
+
+// Rows of a norm, their types; ATTN_OK for none refused.
+int check_norm(int N, int M, float offset, norm_dtype dtype, norm_dtype stream_dtype, bool alone) {
+  if (N < 1 || M < 1 || M > RMSNORM_MAX_M || !std::isfinite(offset)) return ATTN_ERR_SHAPE;
+  if ((int64_t)N * M >= kMaxElements) return ATTN_ERR_SHAPE;
+  if (dtype < NORM_F16 || dtype > NORM_F32 || (stream_dtype != dtype && (alone || stream_dtype != NORM_F32)))
+    return ATTN_ERR_UNSUPPORTED;
+  return ATTN_OK;
+}
+
+// Scales of a row of M with one for each `group` elements, 0 for a group that is none.
+int groups_of(int M, int group) {
+  if (group == 0) return 1;
+  return group == 32 || group == 64 || group == 128 || group == 256 ? (int)ceil_div(M, group) : 0;
+}
+
+// Whether `out` is apart from what else is given, or is `same` itself.
+bool apart_or(Span out, Span same, std::initializer_list<Span> others) {
+  return ((out.begin == same.begin && out.end == same.end) || apart(out, {same})) && apart(out, others);
+}
+
+int norm_add(const void* X, const void* residual, const void* weight, void* Y, float* scales, void* H, float* rstd, int N,
+             int M, int group, int code, double eps, float offset, norm_dtype dtype, norm_dtype stream_dtype,
+             hipStream_t stream) {
+  if (!X || !Y || (residual && !H)) return ATTN_ERR_NULL;
+  if (int rc = check_norm(N, M, offset, dtype, stream_dtype, !residual); rc != ATTN_OK) return rc;
+  if (!std::isfinite(eps) || eps < 0.0) return ATTN_ERR_SHAPE;
+  const int groups = scales ? groups_of(M, group) : 1;
+  if (!groups) return ATTN_ERR_SHAPE;
+  const int64_t n = (int64_t)N * M, e = element_size(dtype), r = element_size(stream_dtype);
+  const Span x = span(X, n * e), res = span(residual, n * r), w = span(weight, M * e), y = span(Y, scales ? n : n * e),
+             sc = span(scales, 4LL * N * groups), h = span(residual ? H : nullptr, n * r), rs = span(rstd, 4LL * N);
+  // In place: a lane reads what it writes before it writes it.
+  if (!(scales ? apart(y, {x, res, w, sc, h, rs}) : apart_or(y, x, {res, w, h, rs}))) return ATTN_ERR_SHAPE;
+  if (!apart_or(h, res, {x, w, sc, rs}) || !apart(sc, {x, res, w, rs}) || !apart(rs, {x, res, w})) return ATTN_ERR_SHAPE;
+  attn::RmsnormParams p{};
+  p.x = X; p.residual = residual; p.weight = weight; p.y = Y; p.scales = scales; p.h = H; p.rstd = rstd;
+  p.eps = eps;
+  p.N = N; p.M = M; p.group = group; p.groups = groups;
+  p.offset = offset;
+  p.dtype = dtype;
+  p.wide = stream_dtype == NORM_F32;
+  p.int8 = code == QUANT8_INT8;
+  return done(attn::launch_rmsnorm_add(p, stream));
 }
 
 }  // namespace
@@ -167,6 +215,70 @@ int attn_bwd(const void* dO, const long long* do_strides, const void* Q, const v
   p.cap_k2 = softcap > 0.f ? 2.f / softcap * p.c : 0.f;
   p.cap_cl = softcap > 0.f ? softcap * kLog2e : 0.f;
   return done(attn::launch_attn_bwd(p, stream));
+}
+
+int rmsnorm_add(const void* X, const void* residual, const void* weight, void* Y, void* H, float* rstd, int N, int M,
+                double eps, float weight_offset, norm_dtype dtype, norm_dtype stream_dtype, hipStream_t stream) {
+  return norm_add(X, residual, weight, Y, nullptr, H, rstd, N, M, 0, 0, eps, weight_offset, dtype, stream_dtype, stream);
+}
+
+int rmsnorm_add_quant(const void* X, const void* residual, const void* weight, void* codes, float* scales, void* H,
+                      float* rstd, int N, int M, int group, quant8_code code, double eps, float weight_offset,
+                      norm_dtype dtype, norm_dtype stream_dtype, hipStream_t stream) {
+  if (!scales) return ATTN_ERR_NULL;
+  if (code != QUANT8_E4M3 && code != QUANT8_INT8) return ATTN_ERR_UNSUPPORTED;
+  return norm_add(X, residual, weight, codes, scales, H, rstd, N, M, group, code, eps, weight_offset, dtype, stream_dtype,
+                  stream);
+}
+
+int quant8_load(const void* codes, const float* scales, void* Y, int N, int M, int group, quant8_code code,
+                norm_dtype dtype, hipStream_t stream) {
+  if (!codes || !scales || !Y) return ATTN_ERR_NULL;
+  if (int rc = check_norm(N, M, 0.f, dtype, dtype, true); rc != ATTN_OK) return rc;
+  if (code != QUANT8_E4M3 && code != QUANT8_INT8) return ATTN_ERR_UNSUPPORTED;
+  const int groups = groups_of(M, group);
+  if (!groups) return ATTN_ERR_SHAPE;
+  const int64_t n = (int64_t)N * M;
+  if (!apart(span(Y, n * element_size(dtype)), {span(codes, n), span(scales, 4LL * N * groups)})) return ATTN_ERR_SHAPE;
+  attn::Quant8LoadParams p{};
+  p.codes = static_cast<const unsigned char*>(codes);
+  p.scales = scales; p.y = Y;
+  p.N = N; p.M = M; p.group = group; p.groups = groups;
+  p.dtype = dtype;
+  p.int8 = code == QUANT8_INT8;
+  return done(attn::launch_quant8_load(p, stream));
+}
+
+size_t rmsnorm_add_bwd_workspace_bytes(int N, int M) {
+  if (N < 1 || M < 1 || M > RMSNORM_MAX_M) return 0;
+  return ((size_t)attn::rmsnorm_bwd_partials(N, M) * M * sizeof(float) + 255) & ~(size_t)255;
+}
+
+int rmsnorm_add_bwd(const void* dY, const void* H, const float* rstd, const void* weight, const void* dH, void* dX,
+                    void* dresidual, float* dweight, int N, int M, float weight_offset, void* workspace,
+                    size_t workspace_bytes, norm_dtype dtype, norm_dtype stream_dtype, hipStream_t stream) {
+  if (!dY || !H || !rstd || !dX) return ATTN_ERR_NULL;
+  if (int rc = check_norm(N, M, weight_offset, dtype, stream_dtype, false); rc != ATTN_OK) return rc;
+  if (dresidual && dtype == stream_dtype) return ATTN_ERR_SHAPE;       // dX is that
+  const size_t need = dweight ? rmsnorm_add_bwd_workspace_bytes(N, M) : 0;
+  if (need && (!workspace || workspace_bytes < need || misaligned(workspace))) return ATTN_ERR_WORKSPACE;
+  const int64_t n = (int64_t)N * M, e = element_size(dtype), r = element_size(stream_dtype);
+  const Span dy = span(dY, n * e), h = span(H, n * r), rs = span(rstd, 4LL * N), w = span(weight, M * e),
+             dh = span(dH, n * r), dx = span(dX, n * e), dres = span(dresidual, n * r), dw = span(dweight, 4LL * M),
+             ws = span(need ? workspace : nullptr, (int64_t)need);
+  // In place: dX may be dY or a dH of its type, dresidual may be dH.
+  const bool on_dh = dtype == stream_dtype && dX == dH;
+  if (!(on_dh ? apart(dx, {dy, h, rs, w, dres, dw, ws}) : apart_or(dx, dy, {h, rs, w, dh, dres, dw, ws}))) return ATTN_ERR_SHAPE;
+  if (!apart_or(dres, dh, {dy, h, rs, w, dw, ws}) || !apart(dw, {dy, h, rs, w, dh, ws}) || !apart(ws, {dy, h, rs, w, dh}))
+    return ATTN_ERR_SHAPE;
+  attn::RmsnormBwdParams p{};
+  p.dy = dY; p.h = H; p.rstd = rstd; p.weight = weight; p.dh = dH; p.dx = dX; p.dresidual = dresidual;
+  p.ws = need ? static_cast<float*>(workspace) : nullptr;
+  p.N = N; p.M = M;
+  p.offset = weight_offset;
+  p.dtype = dtype;
+  p.wide = stream_dtype == NORM_F32;
+  return done(attn::launch_rmsnorm_add_bwd(p, dweight, stream));
 }
 
 }  // extern "C"
