@@ -28,6 +28,7 @@
 
 #include <algorithm>
 #include <type_traits>
+#include <utility>
 
 #include "kernel_common.h"
 #include "launch.h"
@@ -44,6 +45,10 @@ constexpr int kXcds = 8;
 constexpr int kRowsBlock = 64;          // rows of a workgroup of bwd_rows_kernel
 constexpr int kShift = 15;              // fp16: P is held times 2^kShift
 
+typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
+typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
+typedef __attribute__((address_space(3))) float lds_float;
+
 template <typename T> constexpr bool is_half = std::is_same_v<T, _Float16>;
 
 // A tile of 32 rows of D 16-bit values in LDS, 16-byte chunks swizzled (swz).
@@ -56,13 +61,15 @@ struct Tile {
   static constexpr int KX = D / 16;             // MFMA steps over D
   static constexpr int DB = D / 32;             // 32-dim blocks
   // Operand with the rows along M (or N) and the dims along K, step kx: lane (n, hh)
-  // reads row n, dims 16 kx + 8 hh ..: the lane's offset for step 0; step kx is at its xor with 32 kx.
+  // reads row n, dims 16 kx + 8 hh ...  row_offset is the lane's LDS address for step 0 of a tile at 0; step kx
+  // is at its xor with 32 kx, which leaves the tile's own address (a multiple of 256) alone.
   static __device__ __forceinline__ int row_offset(int lane) {
     const int n = lane & 31, hh = lane >> 5;
     return 2 * n * D + 16 * (hh ^ swz<D>(n));
   }
-  static __device__ __forceinline__ vec8 rows(const char* tile, int off, int kx) {
-    return __builtin_bit_cast(vec8, *reinterpret_cast<const u32x4*>(tile + (off ^ (32 * kx))));
+  template <int KX0>
+  static __device__ __forceinline__ vec8 rows(uint32_t at, int imm) {
+    return __builtin_bit_cast(vec8, *(lds_u32x4*)(uintptr_t)(flip<32 * KX0>(at) + imm));
   }
   // Operand with the dims along M and the rows along K: block db, rows 16 c16 ..:
   // lane (m, hh) receives rows 16 c16 + 4 hh + 0..3 and 16 c16 + 8 + 4 hh + 0..3 of dim 32 db + m, the
@@ -72,13 +79,32 @@ struct Tile {
     const int d = 16 * (G & 1) + 4 * (i & 3), k = 4 * (G >> 1) + (i >> 2);
     return 2 * k * D + 16 * ((d >> 3) ^ swz<D>(k)) + 2 * (d & 7);
   }
-  static __device__ __forceinline__ vec8 dims(const char* tile, int off, int c16, int db) {
-    const char* at = tile + c16 * 32 * D;
-    const uint2 lo = lds_read_tr(at + (off ^ (64 * db)));
-    const uint2 hi = lds_read_tr(at + 16 * D + (off ^ (64 * db) ^ 32));
+  template <int C16, int DB0>
+  static __device__ __forceinline__ vec8 dims(uint32_t at, int imm) {
+    const uint2 lo = read_tr(flip<64 * DB0>(at) + imm + C16 * 32 * D);
+    const uint2 hi = read_tr(flip<64 * DB0 ^ 32>(at) + imm + C16 * 32 * D + 16 * D);
     return __builtin_bit_cast(vec8, make_uint4(lo.x, lo.y, hi.x, hi.y));
   }
+  // at ^ X, here and now: as an ordinary expression the compiler computes all of a tile's addresses before the
+  // loop and keeps them in registers that the loop does not have.
+  template <int X>
+  static __device__ __forceinline__ uint32_t flip(uint32_t at) {
+    if constexpr (X == 0) return at;
+    uint32_t r;
+    asm volatile("v_xor_b32 %0, %2, %1" : "=v"(r) : "v"(at), "n"(X));
+    return r;
+  }
+  static __device__ __forceinline__ uint2 read_tr(uint32_t at) {
+    const v4s r = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)(uintptr_t)at);
+    return __builtin_bit_cast(uint2, r);
+  }
 };
+
+template <int N, typename F>
+__device__ __forceinline__ void static_for(F&& f) {
+  [&]<int... Is>(std::integer_sequence<int, Is...>) { (f(std::integral_constant<int, Is>{}), ...); }(
+      std::make_integer_sequence<int, N>{});
+}
 
 // Rows of an accumulator: register r of lane (n, hh) is row kconst(r) + 4 hh of column n.
 constexpr __host__ __device__ int kconst(int r) { return 8 * (r / 4) + r % 4; }
@@ -280,6 +306,9 @@ __device__ __forceinline__ void store(const f32x16 (&acc)[D / 32], float f, T* o
 // Stages of a workgroup's ring (a tile pair and 64 floats each): two workgroups
 // share a compute unit's 160 KB.
 constexpr int kStages = 4;
+// Operands read ahead of their MFMA, and the registers (of 16 bytes a lane) that they pass through.
+constexpr int kAhead = 2;
+constexpr int kFrags = 4;
 
 // dK and dV of 128 keys of a KV head: the tiles of 32 queries that see them, of all query heads of
 // the group, or the share `part` of them (partials in fp32, summed by bwd_sum_kernel).
@@ -351,25 +380,32 @@ __global__ __launch_bounds__(kThreads, 2) void bwd_dkv_kernel(BwdParams p) {
     goff[u] = (int)(r * p.do_sl + c) * 2;
   }
   const int gstep = (int)(TN * p.do_sl) * 2;
-  int cu = u0, cg = nt ? u0 / nt : 0, ct = ta + (nt ? u0 % nt : 0);    // the next tile to copy
+  // The next tile to copy, tile ct of head h0 + cg; cut off the resources of its head's rows.
+  int cu = u0, cg = nt ? u0 / nt : 0, ct = ta + (nt ? u0 % nt : 0);
+  u32x4 rq, rg;
+  auto next_head = [&]() __attribute__((always_inline)) {
+    const size_t head = (size_t)b * p.Hq + h0 + cg;
+    rq = resource(reinterpret_cast<const T*>(p.q) + (head * p.Lq + p.row0) * D, (unsigned)rows * D * 2);
+    rg = resource(reinterpret_cast<const T*>(p.d_o) + b * p.do_sb + (h0 + cg) * p.do_sh + p.row0 * p.do_sl,
+                  (unsigned)((rows - 1) * p.do_sl + D) * 2);
+  };
+  next_head();
+  const u32x4 rx = resource(p.stats + ((size_t)b * p.Hq + h0) * p.row_tiles * (2 * TN),
+                            (unsigned)(p.group * p.row_tiles) * (8 * TN));
   auto copy_next = [&]() __attribute__((always_inline)) {
     if (cu >= u1) return;
     const uint32_t dst = lds0 + (uint32_t)((cu - u0) % kStages * STAGE);
-    const size_t head = (size_t)b * p.Hq + h0 + cg;
-    const u32x4 rq = resource(reinterpret_cast<const T*>(p.q) + (head * p.Lq + p.row0) * D, (unsigned)rows * D * 2);
-    const u32x4 rg = resource(reinterpret_cast<const T*>(p.d_o) + b * p.do_sb + (h0 + cg) * p.do_sh + p.row0 * p.do_sl,
-                              (unsigned)((rows - 1) * p.do_sl + D) * 2);
-    const u32x4 rx = resource(p.stats + (head * p.row_tiles + ct) * (2 * TN), 8 * TN);
 #pragma unroll
     for (int u = 0; u < CB; ++u) {
       copy16(rq, dst + (uint32_t)((wave * CB + u) * 1024), qoff[u] + ct * TB);
       copy16(rg, dst + (uint32_t)(TB + (wave * CB + u) * 1024), goff[u] + ct * gstep);
     }
-    copy4(rx, dst + 2 * TB, 4 * lane);
+    copy4(rx, dst + 2 * TB, 4 * lane + (cg * p.row_tiles + ct) * (8 * TN));
     ++cu;
     if (++ct == ta + nt) {
       ct = ta;
       ++cg;
+      next_head();
     }
   };
 
@@ -380,57 +416,62 @@ __global__ __launch_bounds__(kThreads, 2) void bwd_dkv_kernel(BwdParams p) {
   const float c = p.c;
   const float held = __builtin_ldexpf(1.f, scale_exp - (is_half<T> ? kShift : 0));
 
-  // One tile: queries i0 .. i0 + 31 of a head against the wave's keys.
-  auto tile = [&](auto masked, const char* st, int i0, float sl2) __attribute__((always_inline)) {
-    constexpr bool MASKED = decltype(masked)::value;
-    const char* gt = st + TB;
-    const char* sx = st + 2 * TB + 16 * hh;
-    f32x16 s = f32x16{};
-    if constexpr (!CAP) {
+  // A tile's MFMAs, each with one operand from LDS: first S (rows of Q), dP (rows of dO), dV (dims of
+  // dO) and dK (dims of Q), n of each.  Operand i is read kAhead MFMAs before its own, the first ones of a tile
+  // at the end of the tile before, and so are the starts of its scores.
+  constexpr int n1 = TL::KX, n2 = 2 * TL::KX, n3 = 3 * TL::KX, NF = 4 * TL::KX;
+  static_assert(2 * TL::DB == TL::KX, "as many steps over dims as over rows");
+  vec8 fr[kFrags];
+  f32x16 s, x;
+  auto read = [&](auto ic, uint32_t st, uint32_t next) __attribute__((always_inline)) {
+    constexpr int i = decltype(ic)::value;
+    vec8& f = fr[i % kFrags];
+    if constexpr (i < n1) f = TL::template rows<i>(st + roff, 0);
+    else if constexpr (i < n2) f = TL::template rows<i - n1>(st + roff, TB);
+    else if constexpr (i < n3) f = TL::template dims<(i - n2) / TL::DB, (i - n2) % TL::DB>(st + doff, TB);
+    else if constexpr (i < NF) f = TL::template dims<(i - n3) / TL::DB, (i - n3) % TL::DB>(st + doff, 0);
+    else f = TL::template rows<i - NF>(next + roff, 0);
+  };
+  auto starts = [&](f32x16& a, uint32_t at) __attribute__((always_inline)) {
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const f32x4 a = *reinterpret_cast<const f32x4*>(sx + 32 * g);
+    for (int g = 0; g < 4; ++g) {
+      const f32x4 v = *(lds_f32x4*)(uintptr_t)(at + 16 * hh + 32 * g);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s[4 * g + i] = a[i];
-      }
+      for (int i = 0; i < 4; ++i) a[4 * g + i] = v[i];
     }
-#pragma unroll
-    for (int kx = 0; kx < TL::KX; ++kx) s = E::mfma(TL::rows(st, roff, kx), kf[kx], s);
+  };
+  auto prime = [&](uint32_t st) __attribute__((always_inline)) {
+    if constexpr (CAP) s = f32x16{};
+    else starts(s, st + 2 * TB);
+    static_for<kAhead>([&](auto ic) { read(ic, st, st); });
+  };
+
+  // One tile: queries i0 .. i0 + 31 of a head against the wave's keys.  The vector work runs beside the MFMAs that do not
+  // wait for it: the exponentials beside dP (and the start of dV), dS beside dV (and the start of dK).
+  auto tile = [&](auto masked, uint32_t st, uint32_t next, int i0, float sl2) __attribute__((always_inline)) {
+    constexpr bool MASKED = decltype(masked)::value;
     // Query i sees this lane's key: lo <= i - i0 - 4 hh < hi.
     const int lo = key - off - i0 - 4 * hh, hi = W > 0 ? lo + W : 1 << 30;
     const float bias = ALIBI ? sl2 * (float)(key - off - i0) : 0.f;
-    Weights<T> w;
-#pragma unroll
-    for (int r = 0; r < 16; r += 2) {
-      float x[2], f[2];
+    Weights<T> pw, dw;
+    auto weigh = [&](auto kc) __attribute__((always_inline)) {       // registers 2 k, 2 k + 1
+      constexpr int r = 2 * decltype(kc)::value;
+      float y[2], f[2];
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         if constexpr (CAP) {
-          const float a = *reinterpret_cast<const float*>(sx + 4 * kconst(r + i));
-          x[i] = fast_exp2(capped(s[r + i], p, a, f[i]));
+          const float a = *(lds_float*)(uintptr_t)(st + 2 * TB + 16 * hh + 4 * kconst(r + i));
+          y[i] = fast_exp2(capped(s[r + i], p, a, f[i]));
         } else {
-          x[i] = fast_exp2(ALIBI ? __builtin_fmaf(s[r + i], c, bias) : s[r + i] * c);
+          y[i] = fast_exp2(ALIBI ? __builtin_fmaf(s[r + i], c, bias) : s[r + i] * c);
         }
-        if (MASKED && (kconst(r + i) < lo || kconst(r + i) >= hi)) x[i] = 0.f;
-        s[r + i] = CAP ? x[i] * f[i] : x[i];
+        if (MASKED && (kconst(r + i) < lo || kconst(r + i) >= hi)) y[i] = 0.f;
+        s[r + i] = CAP ? y[i] * f[i] : y[i];
       }
-      w.set(r, x[0], x[1]);
-    }
-#pragma unroll
-    for (int c16 = 0; c16 < 2; ++c16)
-#pragma unroll
-      for (int db = 0; db < TL::DB; ++db) dv[db] = E::mfma(TL::dims(gt, doff, c16, db), w.operand(c16), dv[db]);
-    f32x16 x;
-#pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      const f32x4 a = *reinterpret_cast<const f32x4*>(sx + 4 * TN + 32 * g);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) x[4 * g + i] = a[i];
-    }
-#pragma unroll
-    for (int kx = 0; kx < TL::KX; ++kx) x = E::mfma(TL::rows(gt, roff, kx), vf[kx], x);
-#pragma unroll
-    for (int r = 0; r < 16; r += 2) {
+      pw.set(r, y[0], y[1]);
+    };
+    auto differ = [&](auto kc) __attribute__((always_inline)) {
+      constexpr int r = 2 * decltype(kc)::value;
       float y[2];
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
@@ -438,35 +479,80 @@ __global__ __launch_bounds__(kThreads, 2) void bwd_dkv_kernel(BwdParams p) {
         if (is_half<T>) y[i] *= held;
         if (MASKED && (kconst(r + i) < lo || kconst(r + i) >= hi)) y[i] = 0.f;   // (0 times an infinity is NaN)
       }
-      w.set(r, y[0], y[1]);
-    }
-#pragma unroll
-    for (int c16 = 0; c16 < 2; ++c16)
-#pragma unroll
-      for (int db = 0; db < TL::DB; ++db) dk[db] = E::mfma(TL::dims(st, doff, c16, db), w.operand(c16), dk[db]);
+      dw.set(r, y[0], y[1]);
+    };
+    static_for<NF>([&](auto ic) {
+      constexpr int i = decltype(ic)::value;
+      read(std::integral_constant<int, i + kAhead>{}, st, next);
+      if constexpr (i == 0) starts(x, st + 2 * TB + 4 * TN);
+      const vec8 f = fr[i % kFrags];
+      if constexpr (i < n1) s = E::mfma(f, kf[i], s);
+      else if constexpr (i < n2) x = E::mfma(f, vf[i - n1], x);
+      else if constexpr (i < n3) dv[(i - n2) % TL::DB] = E::mfma(f, pw.operand((i - n2) / TL::DB), dv[(i - n2) % TL::DB]);
+      else dk[(i - n3) % TL::DB] = E::mfma(f, dw.operand((i - n3) / TL::DB), dk[(i - n3) % TL::DB]);
+      // Pair k of the weights after MFMA n1 + lag + k / per, of dS n MFMAs later.
+      constexpr int per = 8 / TL::KX, lag = TL::KX / 4;
+      static_for<per>([&](auto uc) {
+        constexpr int u = decltype(uc)::value;
+        constexpr int k = (i - n1 - lag) * per + u, j = (i - n2 - lag) * per + u;
+        if constexpr (i >= n1 + lag && k < 8) weigh(std::integral_constant<int, k>{});
+        if constexpr (i >= n2 + lag && j < 8) differ(std::integral_constant<int, j>{});
+      });
+      __builtin_amdgcn_sched_barrier(0);
+    });
+    if constexpr (CAP) s = f32x16{};
+    else starts(s, next + 2 * TB);
   };
 
+  // This wave's tiles of a head: none of a row sees a key before tile va and from vb on, and from wa to wb every row sees
+  // every key.
+  int va = ta, vb = ta + nt, wa = ta, wb = ta + nt;
+  if (CAUSAL) {
+    va = max(ta, (jw - off) / TN);                        // (a row i sees key jw from i = jw - off on)
+    if (jw < off) va = ta;
+    wa = max(va, (jw + TN - 1 - off + TN - 1) / TN);
+    if (jw + TN - 1 <= off) wa = va;
+    if (W > 0) {
+      vb = min(vb, max(va, (jw + TN - 1 - off + W - 1 + TN) / TN));     // rows below jw + 31 - off + W see some
+      wb = min(vb, max(0, jw - off + W) / TN);                          // rows below jw - off + W see all
+    }
+    wa = min(wa, vb);
+    wb = max(wa, min(wb, vb));
+  }
   for (int u = 0; u < kStages - 1; ++u) copy_next();
   int g = nt ? u0 / nt : 0, t = ta + (nt ? u0 % nt : 0);
-  for (int u = u0; u < u1; ++u) {
-    // The tile is in LDS when every wave has waited for its own copies; the stage of tile u - 1
-    // is free behind the same barrier.
-    if (u + kStages - 2 < u1) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"((kStages - 2) * CPW) : "memory");
-    else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    copy_next();
-    const char* st = lds + (u - u0) % kStages * STAGE;
-    const int i0 = t * TN;
+  // Runs of tiles of one kind, each its own loop: the kinds side by side in one loop cost moves of the
+  // accumulators at every tile.
+  int u = u0;
+  auto run = [&](auto kind, int end, float sl2) __attribute__((always_inline)) {      // to tile `end` of the head
+    constexpr int KIND = decltype(kind)::value;        // 0: no row sees a key, 1: some, 2: all
+    end = min(end, t + u1 - u);
+    for (; t < end; ++t, ++u) {
+      // Behind the barrier tile u + 1 is in LDS as well (every wave has waited for its own copies), and the
+      // stage of tile u - 1 is free.
+      if (u + kStages - 2 < u1) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"((kStages - 3) * CPW) : "memory");
+      else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+      copy_next();
+      const uint32_t st = lds0 + (uint32_t)((u - u0) % kStages * STAGE), next = lds0 + (uint32_t)((u + 1 - u0) % kStages * STAGE);
+      if (u == u0) prime(st);
+      if constexpr (KIND == 0) prime(next);
+      else tile(std::integral_constant<bool, KIND == 1>{}, st, next, t * TN, sl2);
+    }
+  };
+  while (u < u1) {
     const float sl2 = ALIBI ? p.slopes[h0 + g] * kLog2e : 0.f;
-    if (!CAUSAL) {
-      tile(std::false_type{}, st, i0, sl2);
-    } else if (i0 + TN - 1 + off >= jw && (W == 0 || i0 + off - W < jw + TN - 1)) {
-      if (i0 + off >= jw + TN - 1 && (W == 0 || i0 + TN - 1 + off - W < jw)) tile(std::false_type{}, st, i0, sl2);
-      else tile(std::true_type{}, st, i0, sl2);
+    if constexpr (CAUSAL) {
+      run(std::integral_constant<int, 0>{}, va, sl2);
+      for (int k = 0; k < 2; ++k) {      // (in a window a second time behind the whole ones)
+        run(std::integral_constant<int, 1>{}, k ? vb : wa, sl2);
+        run(std::integral_constant<int, 2>{}, wb, sl2);
+      }
+      run(std::integral_constant<int, 0>{}, ta + nt, sl2);
+    } else {
+      run(std::integral_constant<int, 2>{}, ta + nt, sl2);
     }
-    if (++t == ta + nt) {
-      t = ta;
-      ++g;
-    }
+    t = ta;
+    ++g;
   }
 
   if (key < p.Lk) {
@@ -564,14 +650,23 @@ __global__ __launch_bounds__(kThreads, 2) void bwd_dq_kernel(BwdParams p) {
   for (int db = 0; db < TL::DB; ++db) dq[db] = f32x16{};
   const float held = __builtin_ldexpf(1.f, scale_exp - (is_half<T> ? kShift : 0));
 
-  auto tile = [&](auto masked, const char* st, int j0) __attribute__((always_inline)) {
+  // A tile's MFMAs as in bwd_dkv_kernel: S (rows of K), dP (rows of V), dQ (dims of K).
+  constexpr int n1 = TL::KX, n2 = 2 * TL::KX, NF = 3 * TL::KX;
+  vec8 fr[kFrags];
+  auto read = [&](auto ic, uint32_t st, uint32_t next) __attribute__((always_inline)) {
+    constexpr int i = decltype(ic)::value;
+    vec8& f = fr[i % kFrags];
+    if constexpr (i < n1) f = TL::template rows<i>(st + roff, 0);
+    else if constexpr (i < n2) f = TL::template rows<i - n1>(st + roff, TB);
+    else if constexpr (i < NF) f = TL::template dims<(i - n2) / TL::DB, (i - n2) % TL::DB>(st + doff, 0);
+    else f = TL::template rows<i - NF>(next + roff, 0);
+  };
+  auto prime = [&](uint32_t st) __attribute__((always_inline)) {
+    static_for<kAhead>([&](auto ic) { read(ic, st, st); });
+  };
+  auto tile = [&](auto masked, uint32_t st, uint32_t next, int j0) __attribute__((always_inline)) {
     constexpr bool MASKED = decltype(masked)::value;
-    const char* vt = st + TB;
     f32x16 s = f32x16{}, x = f32x16{};
-#pragma unroll
-    for (int kx = 0; kx < TL::KX; ++kx) s = E::mfma(TL::rows(st, roff, kx), qf[kx], s);
-#pragma unroll
-    for (int kx = 0; kx < TL::KX; ++kx) x = E::mfma(TL::rows(vt, roff, kx), gf[kx], x);
     // This lane's row sees key j: lo < j - j0 - 4 hh <= hi.
     int hi = p.Lk - 1, lo = -1;
     if (CAUSAL) hi = min(hi, row + off);
@@ -580,43 +675,92 @@ __global__ __launch_bounds__(kThreads, 2) void bwd_dq_kernel(BwdParams p) {
     lo -= j0 + 4 * hh;
     const float base = ALIBI ? __builtin_fmaf(sl2, (float)(j0 + 4 * hh - iw - off), add) : add;
     Weights<T> w;
+    auto weigh = [&](auto kc) __attribute__((always_inline)) {       // registers 2 k, 2 k + 1
+      constexpr int r = 2 * decltype(kc)::value;
 #pragma unroll
-    for (int r = 0; r < 16; r += 2) {
+      for (int i = 0; i < 2; ++i) {
+        constexpr int r0 = r;
+        const int k = kconst(r0 + i);
+        float f = 1.f;
+        if constexpr (CAP) {
+          s[r + i] = fast_exp2(capped(s[r + i], p, add, f));
+          s[r + i] *= f;
+        } else {
+          s[r + i] = fast_exp2(__builtin_fmaf(s[r + i], c, ALIBI ? __builtin_fmaf(sl2, (float)k, base) : base));
+        }
+      }
+    };
+    auto differ = [&](auto kc) __attribute__((always_inline)) {
+      constexpr int r = 2 * decltype(kc)::value;
       float y[2];
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const int k = kconst(r + i);
-        float f = 1.f, a;
-        if constexpr (CAP) a = fast_exp2(capped(s[r + i], p, add, f)) * f;
-        else a = fast_exp2(__builtin_fmaf(s[r + i], c, ALIBI ? __builtin_fmaf(sl2, (float)k, base) : base));
-        y[i] = a * (x[r + i] + nd);
+        y[i] = s[r + i] * (x[r + i] + nd);
         if (is_half<T>) y[i] *= held;
         if (MASKED && (k > hi || k <= lo)) y[i] = 0.f;
       }
       w.set(r, y[0], y[1]);
-    }
-#pragma unroll
-    for (int c16 = 0; c16 < 2; ++c16)
-#pragma unroll
-      for (int db = 0; db < TL::DB; ++db) dq[db] = E::mfma(TL::dims(st, doff, c16, db), w.operand(c16), dq[db]);
+    };
+    static_for<NF>([&](auto ic) {
+      constexpr int i = decltype(ic)::value;
+      read(std::integral_constant<int, i + kAhead>{}, st, next);
+      const vec8 f = fr[i % kFrags];
+      constexpr int per = 8 / TL::KX, lag = TL::KX / 4;
+      // What the first half of dQ's MFMAs takes comes before them, the rest beside them.
+      if constexpr (i == n2) static_for<4>([&](auto kc) { differ(kc); });
+      if constexpr (i < n1) s = E::mfma(f, qf[i], s);
+      else if constexpr (i < n2) x = E::mfma(f, gf[i - n1], x);
+      else dq[(i - n2) % TL::DB] = E::mfma(f, w.operand((i - n2) / TL::DB), dq[(i - n2) % TL::DB]);
+      // The exponentials beside dP, the last ones in its last place.
+      static_for<per>([&](auto uc) {
+        constexpr int k = (i - n1 - lag) * per + decltype(uc)::value;
+        if constexpr (i >= n1 + lag && i < n2) weigh(std::integral_constant<int, k>{});
+      });
+      if constexpr (i == n2 - 1) static_for<lag * per>([&](auto uc) { weigh(std::integral_constant<int, 8 - lag * per + decltype(uc)::value>{}); });
+      if constexpr (i >= n2 && i < n2 + TL::DB) {
+        constexpr int per2 = 4 / TL::DB;
+        static_for<per2>([&](auto uc) { differ(std::integral_constant<int, 4 + (i - n2) * per2 + decltype(uc)::value>{}); });
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    });
   };
 
-  for (int u = 0; u < kStages - 1; ++u) copy_tile(t0 + u);
-  for (int t = t0; t < t1; ++t) {
-    if (t + kStages - 2 < t1) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"((kStages - 2) * CPW) : "memory");
-    else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    copy_tile(t + kStages - 1);
-    const char* st = lds + (t - t0) % kStages * STAGE;
-    const int j0 = t * TN;
-    if (iw >= rows) continue;
-    if (!CAUSAL) {
-      if (j0 + TN <= p.Lk) tile(std::false_type{}, st, j0);
-      else tile(std::true_type{}, st, j0);
-    } else if (j0 <= wlast + off && (W == 0 || j0 + TN - 1 > iw + off - W)) {
-      if (j0 + TN - 1 <= iw + off && (W == 0 || j0 > wlast + off - W)) tile(std::false_type{}, st, j0);
-      else tile(std::true_type{}, st, j0);
+  // This wave's tiles: its rows see keys of tiles [va, vb), each of them all keys of [wa, wb).
+  int va = t0, vb = t1, wa = t0, wb = min(t1, p.Lk / TN);
+  if (CAUSAL) {
+    vb = min(vb, (wlast + off) / TN + 1);
+    wb = min(wb, (iw + off + 1) / TN);
+    if (W > 0) {
+      va = max(va, max(0, iw + off - W + 1) / TN);
+      wa = max(va, (max(0, wlast + off - W + 1) + TN - 1) / TN);
     }
   }
+  if (iw >= rows) vb = va;
+  va = min(va, t1);
+  vb = max(va, min(vb, t1));
+  wa = min(max(wa, va), vb);
+  wb = max(wa, min(wb, vb));
+  for (int u = 0; u < kStages - 1; ++u) copy_tile(t0 + u);
+  int t = t0;
+  auto run = [&](auto kind, int end) __attribute__((always_inline)) {
+    constexpr int KIND = decltype(kind)::value;        // 0: no row sees a key, 1: some, 2: all
+    for (; t < end; ++t) {
+      if (t + kStages - 2 < t1) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"((kStages - 3) * CPW) : "memory");
+      else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+      copy_tile(t + kStages - 1);
+      const uint32_t st = lds0 + (uint32_t)((t - t0) % kStages * STAGE), next = lds0 + (uint32_t)((t + 1 - t0) % kStages * STAGE);
+      if (t == t0) prime(st);
+      if constexpr (KIND == 0) prime(next);
+      else tile(std::integral_constant<bool, KIND == 1>{}, st, next, t * TN);
+    }
+  };
+  run(std::integral_constant<int, 0>{}, va);
+  for (int k = 0; k < 2; ++k) {      // (the masked ones come before the whole ones in a window, and behind them)
+    run(std::integral_constant<int, 1>{}, k ? vb : wa);
+    run(std::integral_constant<int, 2>{}, wb);
+  }
+  run(std::integral_constant<int, 0>{}, t1);
 
   if (iw + n < rows) {
     const size_t at = (head * p.Lq + p.row0 + iw + n) * D;
