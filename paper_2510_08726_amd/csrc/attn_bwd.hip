@@ -8,9 +8,10 @@
 //
 // Three kernels, without atomics, so that a call's bits do not depend on timing:
 //   bwd_rows_kernel  what a row brings into its scores: (delta, lse), once
-//   bwd_dkv_kernel   a workgroup owns 128 keys and streams the tiles of 32 queries that see them
-//   bwd_dq_kernel    a workgroup owns 128 query rows and streams the tiles of 32 keys
-// The last two each form S and dP, seven products in the place of five.  (One loop for
+//   bwd_kernel       dkv_block: a workgroup owns 128 keys and streams the tiles of 32 queries that see them;
+//                    dq_block: a workgroup owns 128 query rows and streams the tiles of 32 keys
+//   bwd_sum_kernel   adds up the blocks that were divided into parts, where few blocks are long
+// Both kinds of blocks form S and dP, seven products in the place of five.  (One loop for
 // both would need the partial dQ of every key block in memory, 1 KB a row and block of 256 keys
 // against 131 kflop saved: no less time at this card's rates, and a sum over blocks.)
 //
@@ -152,15 +153,29 @@ __device__ __forceinline__ float capped(float x, const BwdParams& p, float add, 
   return __builtin_fmaf(-2.f * p.cap_cl, r, p.cap_cl + add);
 }
 
-// What item of `n` a workgroup takes: an XCD a contiguous share (workgroup g runs on XCD g mod
+// What item of `n` workgroup g takes: an XCD a contiguous share (workgroup g runs on XCD g mod
 // 8), so that those that read the same rows share its L2; -1 for none.
-__device__ __forceinline__ int item_of(int n, bool shares) {
-  const int g = blockIdx.x;
+__device__ __forceinline__ int item_of(int g, int n, bool shares) {
   if (!shares) return g < n ? g : -1;
   const int x = g % kXcds;
   const int s0 = (int)((long long)n * x / kXcds), s1 = (int)((long long)n * (x + 1) / kXcds);
   const int i = s0 + g / kXcds;
   return i < s1 ? i : -1;
+}
+
+// The block and the part of it that is number r of a unit's list, and its first piece (of the blocks in several parts).
+struct Place {
+  int block, part, parts, piece;
+};
+__device__ __forceinline__ Place place_of(const BwdSplit& s, int r) {
+  if (s.multi == 0) return {r, 0, 1, 0};
+  int block = 0, piece = 0;
+  for (;; ++block) {
+    const int n = s.parts[block];
+    if (r < n) return {block, r, n, piece};
+    r -= n;
+    piece += n > 1 ? n : 0;
+  }
 }
 
 // fp16: the power of two that dS is held times, as an exponent: |dS| <= 2 |dO| |V| of the
@@ -303,42 +318,33 @@ __device__ __forceinline__ void store(const f32x16 (&acc)[D / 32], float f, T* o
     }
 }
 
-// Stages of a workgroup's ring (a tile pair and 64 floats each): two workgroups
+// Stages of a workgroup's ring, a tile pair and 64 floats each: two workgroups
 // share a compute unit's 160 KB.
 constexpr int kStages = 4;
+template <int D> constexpr int kStage = 2 * TN * D * 2 + 256;
 // Operands read ahead of their MFMA, and the registers (of 16 bytes a lane) that they pass through.
 constexpr int kAhead = 2;
 constexpr int kFrags = 4;
 
 // dK and dV of 128 keys of a KV head: the tiles of 32 queries that see them, of all query heads of
-// the group, or the share `part` of them (partials in fp32, summed by bwd_sum_kernel).
+// the group, or a part of them (a partial in fp32, summed by bwd_sum_kernel).
 template <int D, typename T, bool CAUSAL, bool ALIBI, bool CAP>
-__global__ __launch_bounds__(kThreads, 2) void bwd_dkv_kernel(BwdParams p) {
+__device__ __forceinline__ void dkv_block(const BwdParams& p, char* lds, int item) {
   typedef Elem<T> E;
   typedef Tile<D, T> TL;
   typedef typename E::vec8 vec8;
-  constexpr int TB = TL::BYTES, STAGE = 2 * TB + 256, CPR = TL::CPR;
+  constexpr int TB = TL::BYTES, STAGE = kStage<D>, CPR = TL::CPR;
   constexpr int CB = TL::NBLK / kWaves;            // 1 KB copies of a tile that a wave makes
   constexpr int CPW = 2 * CB + 1;                  // copies in flight of a stage
   static_assert(CB >= 1, "a tile's copies divide over the waves");
-  __shared__ __attribute__((aligned(1024))) char lds[kStages * STAGE];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n = lane & 31, hh = lane >> 5;
 
-  const int units = p.B * p.Hkv, nkb = (p.Lk + BLK - 1) / BLK, S = p.dkv_parts;
-  const int item = item_of(units * nkb * S, p.shares);
-  if (item < 0) return;
   // Key blocks in order: the first ones see the most queries.
-  int unit, kb, part;
-  if (p.shares) {
-    unit = item / (nkb * S);
-    kb = item / S - unit * nkb;
-    part = item % S;
-  } else {
-    kb = item / (units * S);
-    unit = item / S - kb * units;
-    part = item % S;
-  }
+  const int units = p.B * p.Hkv;
+  const int unit = p.shares ? item / p.dkv.list : item % units;
+  const Place at = place_of(p.dkv, p.shares ? item - unit * p.dkv.list : item / units);
+  const int kb = at.block, part = at.part, S = at.parts;
   const int b = unit / p.Hkv, h0 = (unit - b * p.Hkv) * p.group;   // batch and first query head
   const int rows = p.rows, off = p.Lk - rows, W = p.window;
   const int j0 = kb * BLK, jw = j0 + TN * wave;
@@ -556,45 +562,35 @@ __global__ __launch_bounds__(kThreads, 2) void bwd_dkv_kernel(BwdParams p) {
   }
 
   if (key < p.Lk) {
-    const size_t at = ((size_t)unit * p.Lk + key) * D, all = (size_t)units * p.Lk * D;
-    float* pk = S > 1 ? p.ws_dkv + 2 * part * all + at : nullptr;
-    store<D, T>(dk, __builtin_ldexpf(p.scale, -scale_exp), reinterpret_cast<T*>(p.dk) + at, pk, hh);
-    store<D, T>(dv, is_half<T> ? __builtin_ldexpf(1.f, -kShift) : 1.f, reinterpret_cast<T*>(p.dv) + at,
-                pk ? pk + all : nullptr, hh);
+    const size_t to = ((size_t)unit * p.Lk + key) * D;
+    float* pk = S > 1 ? p.ws_dkv + (((size_t)unit * p.dkv.pieces + at.piece + part) * 2 * BLK + (key - j0)) * D : nullptr;
+    store<D, T>(dk, __builtin_ldexpf(p.scale, -scale_exp), reinterpret_cast<T*>(p.dk) + to, pk, hh);
+    store<D, T>(dv, is_half<T> ? __builtin_ldexpf(1.f, -kShift) : 1.f, reinterpret_cast<T*>(p.dv) + to,
+                pk ? pk + BLK * D : nullptr, hh);
   }
 }
 
 // dQ of 128 query rows (of p.hg heads that share a KV head, 128 / hg rows each): the tiles of 32
-// keys that they see, or the share `part` of them.
+// keys that they see, or a part of them.
 template <int D, typename T, bool CAUSAL, bool ALIBI, bool CAP>
-__global__ __launch_bounds__(kThreads, 2) void bwd_dq_kernel(BwdParams p) {
+__device__ __forceinline__ void dq_block(const BwdParams& p, char* lds, int item) {
   typedef Elem<T> E;
   typedef Tile<D, T> TL;
   typedef typename E::vec8 vec8;
-  constexpr int TB = TL::BYTES, STAGE = 2 * TB, CPR = TL::CPR;
+  constexpr int TB = TL::BYTES, STAGE = kStage<D>, CPR = TL::CPR;
   constexpr int CB = TL::NBLK / kWaves, CPW = 2 * CB;
-  __shared__ __attribute__((aligned(1024))) char lds[kStages * STAGE];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n = lane & 31, hh = lane >> 5;
 
   const int hg = p.hg, bm = TN * (kWaves / hg), ngrp = p.group / hg;
-  const int rows = p.rows, off = p.Lk - rows, W = p.window, S = p.dq_parts;
+  const int rows = p.rows, off = p.Lk - rows, W = p.window;
   const int units = p.B * p.Hkv, nqb = (rows + bm - 1) / bm;
-  const int item = item_of(units * ngrp * nqb * S, p.shares);
-  if (item < 0) return;
-  // Row blocks from the last, which sees the most keys.
-  int unit, rb, grp, part = item % S;
-  if (p.shares) {
-    unit = item / (nqb * ngrp * S);
-    const int rest = item / S - unit * nqb * ngrp;
-    rb = nqb - 1 - rest / ngrp;
-    grp = rest % ngrp;
-  } else {
-    const int rest = item / S, per = units * ngrp;
-    rb = nqb - 1 - rest / per;
-    unit = rest % per / ngrp;
-    grp = rest % ngrp;
-  }
+  // Row blocks from the last, which sees the most keys; the head groups of a block beside each other.
+  const int unit = p.shares ? item / (p.dq_.list * ngrp) : item / ngrp % units;
+  const int rest = p.shares ? item - unit * p.dq_.list * ngrp : item / (ngrp * units) * ngrp + item % ngrp;
+  const int grp = rest % ngrp;
+  const Place at = place_of(p.dq_, rest / ngrp);
+  const int rb = nqb - 1 - at.block, part = at.part, S = at.parts;
   const int b = unit / p.Hkv, hq = (unit - b * p.Hkv) * p.group + grp * hg + wave % hg;
   const size_t head = (size_t)b * p.Hq + hq;
   const int i0 = rb * bm, iw = i0 + TN * (wave / hg), wlast = min(iw + TN, rows) - 1;
@@ -650,7 +646,7 @@ __global__ __launch_bounds__(kThreads, 2) void bwd_dq_kernel(BwdParams p) {
   for (int db = 0; db < TL::DB; ++db) dq[db] = f32x16{};
   const float held = __builtin_ldexpf(1.f, scale_exp - (is_half<T> ? kShift : 0));
 
-  // A tile's MFMAs as in bwd_dkv_kernel: S (rows of K), dP (rows of V), dQ (dims of K).
+  // A tile's MFMAs as in dkv_block: S (rows of K), dP (rows of V), dQ (dims of K).
   constexpr int n1 = TL::KX, n2 = 2 * TL::KX, NF = 3 * TL::KX;
   vec8 fr[kFrags];
   auto read = [&](auto ic, uint32_t st, uint32_t next) __attribute__((always_inline)) {
@@ -763,38 +759,71 @@ __global__ __launch_bounds__(kThreads, 2) void bwd_dq_kernel(BwdParams p) {
   run(std::integral_constant<int, 0>{}, t1);
 
   if (iw + n < rows) {
-    const size_t at = (head * p.Lq + p.row0 + iw + n) * D;
-    float* pq = S > 1 ? p.ws_dq + part * ((size_t)p.B * p.Hq * p.Lq * D) + at : nullptr;
-    store<D, T>(dq, __builtin_ldexpf(p.scale, -scale_exp), reinterpret_cast<T*>(p.dq) + at, pq, hh);
+    const size_t to = (head * p.Lq + p.row0 + iw + n) * D;
+    float* pq = nullptr;
+    if (S > 1) pq = p.ws_dq + ((((size_t)unit * ngrp + grp) * p.dq_.pieces + at.piece + part) * BLK + TN * wave + n) * D;
+    store<D, T>(dq, __builtin_ldexpf(p.scale, -scale_exp), reinterpret_cast<T*>(p.dq) + to, pq, hh);
   }
 }
 
-// The partials of several parts, summed in their order.
-struct BwdSum {
-  const float* ws;      // part s of element i: ws[s step + i]
-  void* out;
-  size_t step, n;       // n: elements, a multiple of 4
-  int parts;
-  int skip, len, D;     // rows i % len below `skip` are left as they are
-};
-template <typename T>
-__global__ __launch_bounds__(256) void bwd_sum_kernel(BwdSum p) {
-  const size_t i = 4 * ((size_t)blockIdx.x * 256 + threadIdx.x);
-  if (i >= p.n) return;
-  if (p.skip && (int)(i / p.D % p.len) < p.skip) return;
-  f32x4 a = *reinterpret_cast<const f32x4*>(p.ws + i);
-  for (int s = 1; s < p.parts; ++s) a += *reinterpret_cast<const f32x4*>(p.ws + s * p.step + i);
-  *reinterpret_cast<uint2*>(reinterpret_cast<T*>(p.out) + i) =
-      make_uint2(Elem<T>::pack2(a[0], a[1]), Elem<T>::pack2(a[2], a[3]));
+// Both in one launch, the key blocks first: the row blocks fill what they leave free.
+template <int D, typename T, bool CAUSAL, bool ALIBI, bool CAP>
+__global__ __launch_bounds__(kThreads, 2) void bwd_kernel(BwdParams p) {
+  __shared__ __attribute__((aligned(1024))) char lds[kStages * kStage<D>];
+  const int units = p.B * p.Hkv, nk = units * p.dkv.list, gk = p.shares ? (nk + kXcds - 1) / kXcds * kXcds : nk;
+  const int g = blockIdx.x;
+  if (g < gk) {
+    const int item = item_of(g, nk, p.shares);
+    if (item >= 0) dkv_block<D, T, CAUSAL, ALIBI, CAP>(p, lds, item);
+  } else {
+    const int item = item_of(g - gk, units * (p.group / p.hg) * p.dq_.list, p.shares);
+    if (item >= 0) dq_block<D, T, CAUSAL, ALIBI, CAP>(p, lds, item);
+  }
 }
 
-template <typename T>
-hipError_t launch_sum(const BwdSum& p, hipStream_t stream) {
-  hipLaunchKernelGGL((bwd_sum_kernel<T>), dim3((unsigned)((p.n / 4 + 255) / 256)), dim3(256), 0, stream, p);
-  return hipGetLastError();
+// The partials of the blocks in several parts, summed in their order and rounded: 1024 values a workgroup,
+// first of dK and dV, then of dQ.
+template <int D, typename T>
+__global__ __launch_bounds__(256) void bwd_sum_kernel(BwdParams p) {
+  constexpr int PER = BLK * D / 1024;                      // workgroups of a piece
+  const int units = p.B * p.Hkv, nk = units * p.dkv.multi * 2 * PER;
+  int g = blockIdx.x;
+  const bool keys = g < nk;
+  const BwdSplit& s = keys ? p.dkv : p.dq_;
+  if (!keys) g -= nk;
+  const int sub = g % PER;
+  g /= PER;
+  int which = 0;
+  if (keys) {
+    which = g % 2;
+    g /= 2;
+  }
+  const int of = g / s.multi;                              // the unit (and head group)
+  int m = g - of * s.multi, block = 0, piece = 0;          // the m-th block in several parts
+  for (;; ++block) {
+    const int c = s.parts[block];
+    if (c > 1 && m-- == 0) break;
+    piece += c > 1 ? c : 0;
+  }
+  const int parts = s.parts[block], i = sub * 1024 + 4 * threadIdx.x, r = i / D, d = i % D;
+  const size_t step = (size_t)(keys ? 2 : 1) * BLK * D;
+  const float* at = (keys ? p.ws_dkv : p.ws_dq) + ((size_t)of * s.pieces + piece) * step + which * BLK * D + i;
+  T* out;
+  if (keys) {
+    const int key = block * BLK + r;
+    if (key >= p.Lk) return;
+    out = reinterpret_cast<T*>(which ? p.dv : p.dk) + ((size_t)of * p.Lk + key) * D + d;
+  } else {
+    const int hg = p.hg, bm = TN * (kWaves / hg), ngrp = p.group / hg, wave = r / TN;
+    const int unit = of / ngrp, row = ((p.rows + bm - 1) / bm - 1 - block) * bm + TN * (wave / hg) + r % TN;
+    if (row >= p.rows) return;
+    const size_t head = (size_t)unit * p.group + (of - unit * ngrp) * hg + wave % hg;
+    out = reinterpret_cast<T*>(p.dq) + (head * p.Lq + p.row0 + row) * D + d;
+  }
+  f32x4 a = *reinterpret_cast<const f32x4*>(at);
+  for (int k = 1; k < parts; ++k) a += *reinterpret_cast<const f32x4*>(at + k * step);
+  *reinterpret_cast<uint2*>(out) = make_uint2(Elem<T>::pack2(a[0], a[1]), Elem<T>::pack2(a[2], a[3]));
 }
-
-int grid_of(int64_t items, bool shares) { return (int)(shares ? (items + kXcds - 1) / kXcds * kXcds : items); }
 
 template <int D, typename T, bool CAUSAL, bool ALIBI, bool CAP>
 hipError_t launch_t(const BwdParams& p, hipStream_t stream) {
@@ -804,23 +833,13 @@ hipError_t launch_t(const BwdParams& p, hipStream_t stream) {
   hipLaunchKernelGGL((bwd_rows_kernel<D, T>), dim3((unsigned)pre), dim3(kThreads), 0, stream, p);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const int64_t nk = units * ((p.Lk + BLK - 1) / BLK) * p.dkv_parts;
-  hipLaunchKernelGGL((bwd_dkv_kernel<D, T, CAUSAL, ALIBI, CAP>), dim3(grid_of(nk, p.shares)), dim3(kThreads), 0, stream, p);
-  if ((e = hipGetLastError()) != hipSuccess) return e;
-  const int bm = TN * (kWaves / p.hg);
-  const int64_t nq = units * (p.group / p.hg) * ((p.rows + bm - 1) / bm) * p.dq_parts;
-  hipLaunchKernelGGL((bwd_dq_kernel<D, T, CAUSAL, ALIBI, CAP>), dim3(grid_of(nq, p.shares)), dim3(kThreads), 0, stream, p);
-  if ((e = hipGetLastError()) != hipSuccess) return e;
-  if (p.dkv_parts > 1) {
-    const size_t n = (size_t)units * p.Lk * D;
-    if ((e = launch_sum<T>({p.ws_dkv, p.dk, 2 * n, n, p.dkv_parts, 0, 1, D}, stream)) != hipSuccess) return e;
-    if ((e = launch_sum<T>({p.ws_dkv + n, p.dv, 2 * n, n, p.dkv_parts, 0, 1, D}, stream)) != hipSuccess) return e;
-  }
-  if (p.dq_parts > 1) {
-    const size_t n = (size_t)heads * p.Lq * D;
-    return launch_sum<T>({p.ws_dq, p.dq, n, n, p.dq_parts, p.row0, p.Lq, D}, stream);
-  }
-  return hipSuccess;
+  const auto whole = [&](int64_t n) { return p.shares ? (n + kXcds - 1) / kXcds * kXcds : n; };
+  const int64_t n = whole(units * p.dkv.list) + whole(units * (p.group / p.hg) * p.dq_.list);
+  hipLaunchKernelGGL((bwd_kernel<D, T, CAUSAL, ALIBI, CAP>), dim3((unsigned)n), dim3(kThreads), 0, stream, p);
+  if ((e = hipGetLastError()) != hipSuccess || p.dkv.multi + p.dq_.multi == 0) return e;
+  const int64_t sums = (units * p.dkv.multi * 2 + units * (p.group / p.hg) * p.dq_.multi) * (BLK * D / 1024);
+  hipLaunchKernelGGL((bwd_sum_kernel<D, T>), dim3((unsigned)sums), dim3(256), 0, stream, p);
+  return hipGetLastError();
 }
 
 template <int D, typename T>

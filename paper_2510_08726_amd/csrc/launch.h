@@ -118,6 +118,14 @@ constexpr size_t kDecodeScratchBytes = size_t(16) << 20;
 hipError_t decode_scratch(void** ptr);
 
 // Attention's backward pass (attn_bwd.hip).
+//
+// How the blocks of a unit are divided over workgroups: block i into parts[i], `list` of them in all.  Those of more than
+// one part are partials: `multi` blocks, of `pieces` parts in all.  (multi = 0: `parts` is not read.)
+constexpr int kBwdSplitBlocks = 256;
+struct BwdSplit {
+  int list, multi, pieces;
+  unsigned char parts[kBwdSplitBlocks];
+};
 struct BwdParams {
   const void* q;
   const void* k;
@@ -131,8 +139,8 @@ struct BwdParams {
   void* dv;
   float* stats;         // [B * Hq, row_tiles, 64]
   float* peaks;         // fp16: [B * Hq, row_blocks], then [B * Hkv, key_blocks]
-  float* ws_dkv;        // partials [dkv_parts, 2, B * Hkv, Lk, D]
-  float* ws_dq;         // partials [dq_parts, B * Hq, Lq, D]
+  float* ws_dkv;        // partials [B * Hkv, dkv.pieces, 2, 128, D]
+  float* ws_dq;         // partials [B * Hkv, group / hg, dq_.pieces, 128, D]
   int64_t do_sb, do_sh, do_sl;   // strides of d_o in elements
   int B, Hq, Hkv, Lq, Lk, D;
   int group;            // Hq / Hkv
@@ -140,7 +148,6 @@ struct BwdParams {
   int row_tiles, row_blocks, key_blocks;   // tiles of 32, blocks of 64
   int window;           // 0 for none
   int hg;               // query heads of a workgroup of the dQ kernel
-  int dkv_parts, dq_parts;
   bool causal, bf16;
   bool shares;          // every XCD a contiguous share of the workgroups' items
   unsigned sign;        // 0x80008000 where the scale is negative
@@ -148,6 +155,8 @@ struct BwdParams {
   float scale;
   float cap_k2;         // SoftCap: 2 / cap * c
   float cap_cl;         // SoftCap: cap * log2(e), or 0 for no cap
+  BwdSplit dkv;         // key blocks of a KV head
+  BwdSplit dq_;         // row blocks of hg heads
 };
 int bwd_block_keys();
 int bwd_rows_per_block();

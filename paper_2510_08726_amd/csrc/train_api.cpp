@@ -57,6 +57,47 @@ struct BwdPlan {
   int64_t groups;                    // the most workgroups of a kernel
 };
 
+// Tiles of 32 queries (of one head) that see keys [128 i, 128 (i + 1)), and of 32 keys that row block i sees, as
+// attn_bwd.hip counts them.
+int64_t query_tiles(const attn::BwdParams& p, int i) {
+  const int off = p.Lk - p.rows, j0 = i * attn::bwd_block_keys();
+  int64_t lo = 0, hi = p.rows;
+  if (p.causal) {
+    lo = std::max(0, j0 - off);
+    if (p.window > 0) hi = std::min<int64_t>(hi, (int64_t)std::min(j0 + attn::bwd_block_keys(), p.Lk) - off + p.window - 1);
+  }
+  return hi > lo ? (hi + 31) / 32 - lo / 32 : 0;
+}
+int64_t key_tiles(const attn::BwdParams& p, int i) {
+  const int bm = attn::bwd_block_keys() / p.hg, off = p.Lk - p.rows;
+  const int rb = (p.rows + bm - 1) / bm - 1 - i;             // (from the last)
+  int64_t lo = 0, hi = p.Lk;
+  if (p.causal) {
+    hi = std::min(p.Lk, std::min((rb + 1) * bm, p.rows) + off);
+    if (p.window > 0) lo = std::max(0, rb * bm + off + 1 - p.window);
+  }
+  return (hi + 31) / 32 - lo / 32;
+}
+
+// Parts of about `share` tiles.
+template <typename F>
+void divide(attn::BwdSplit& s, int blocks, double share, F&& tiles) {
+  s.list = blocks;
+  if (blocks > attn::kBwdSplitBlocks) return;
+  int list = 0;
+  for (int i = 0; i < blocks; ++i) {
+    const double w = (double)tiles(i);
+    const int n = w > 1.25 * share ? (int)std::min(std::ceil(w / share), 255.0) : 1;
+    s.parts[i] = (unsigned char)n;
+    list += n;
+    if (n > 1) {
+      ++s.multi;
+      s.pieces += n;
+    }
+  }
+  s.list = list;
+}
+
 BwdPlan plan(int B, int Hq, int Hkv, int Lq, int Lk, int D, bool causal, int window) {
   BwdPlan r{};
   attn::BwdParams& p = r.p;
@@ -73,17 +114,28 @@ BwdPlan plan(int B, int Hq, int Hkv, int Lq, int Lk, int D, bool causal, int win
   while (p.hg < 4 && p.group % (2 * p.hg) == 0) p.hg *= 2;
   const int64_t units = (int64_t)B * Hkv, heads = (int64_t)B * Hq;
   p.shares = units % 8 == 0;
-  p.dkv_parts = p.dq_parts = 1;
+  const int bm = attn::bwd_block_keys() / p.hg, nkb = (int)ceil_div(Lk, attn::bwd_block_keys()), nqb = (int)ceil_div(p.rows, bm);
+  // A tile of a key block is 4 products of 32 x 32 x D a wave, one of a row block 3: the whole call's tiles, for each
+  // workgroup that runs at a time.
+  double all = 0.0;
+  for (int i = 0; i < nkb; ++i) all += 4.0 * p.group * query_tiles(p, i);
+  for (int i = 0; i < nqb; ++i) all += 3.0 * (p.group / p.hg) * key_tiles(p, i);
+  // A longer block would be the last to end, and is divided.  Three quarters of an even share: 2 x 32 / 8 heads of 2048 rows
+  // (causal) take 297 us, 304 with half of it, 346 with all, 485 undivided; 40 / 2 heads 192, 219, 239 and 2420; 128 rows
+  // of 32 / 8 heads on 8192 keys 99, 96, 92 and 226.  At least 8 tiles: 8 heads of 1024 rows 41 us, 46 with 4, 49 with 16, 58
+  // undivided.
+  const double each = 0.75 * all * units / (2.0 * attn::compute_units());
+  divide(p.dkv, nkb, std::max(each / 4, 8.0), [&](int i) { return p.group * query_tiles(p, i); });
+  divide(p.dq_, nqb, std::max(each / 3, 8.0), [&](int i) { return key_tiles(p, i); });
   const auto floats = [](int64_t n) { return (n + 63) / 64 * 64; };
   r.stats = floats(heads * p.row_tiles * 64);
   r.peaks = floats(heads * p.row_blocks + units * p.key_blocks);
-  r.dkv = p.dkv_parts > 1 ? floats(2 * p.dkv_parts * units * Lk * D) : 0;
-  r.dq = p.dq_parts > 1 ? floats(p.dq_parts * heads * Lq * D) : 0;
-  const int64_t bm = attn::bwd_block_keys() / p.hg;
+  const int64_t block = (int64_t)attn::bwd_block_keys() * D;
+  r.dkv = 2 * units * p.dkv.pieces * block;
+  r.dq = heads / p.hg * p.dq_.pieces * block;
   r.groups = std::max({heads * (p.row_blocks + ceil_div(p.row0, attn::bwd_rows_per_block())) + units * p.key_blocks,
-                       units * ceil_div(Lk, attn::bwd_block_keys()) * p.dkv_parts + 8,
-                       heads / p.hg * ceil_div(p.rows, bm) * p.dq_parts + 8,
-                       ceil_div(units * Lk * D, 1024), ceil_div(heads * Lq * D, 1024)});
+                       units * p.dkv.list + heads / p.hg * p.dq_.list + 16,
+                       (2 * units * p.dkv.multi + heads / p.hg * p.dq_.multi) * (block / 1024)});
   return r;
 }
 
