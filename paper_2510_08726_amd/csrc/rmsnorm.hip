@@ -24,47 +24,78 @@ namespace {
 constexpr int kMaxThreads = 1024;
 constexpr int kMaxWaves = kMaxThreads / 64;
 
-// 16 bytes at any address that an element may have (the hardware takes them so).
-template <typename T> struct Packed {
-  typedef u32x4 vec;
-  struct __attribute__((packed, aligned(sizeof(T)))) type { vec v; };
+// 8 elements as they lie in memory.
+template <typename T>
+struct Raw {
+  static constexpr int W = sizeof(T) / 2;      // 16-byte words
+  u32x4 w[W];
 };
 
-template <typename T> __device__ __forceinline__ float to_float(T x) { return (float)x; }
+// 16 bytes at any address that an element may have (the hardware takes them so).
+template <typename T> struct __attribute__((packed, aligned(sizeof(T)))) Packed { u32x4 v; };
 
-// 8 elements at `at`, the first n of which are the row's; zeros for the others.
-template <typename T>
-__device__ __forceinline__ void get8(const T* at, int n, float (&x)[8]) {
-  if (n >= 8) {
-    if constexpr (sizeof(T) == 4) {
+// The chunk of a row that a lane holds: 8 columns from `col` on, of which [lo, hi) are the row's.  Without
+// ODD (M a multiple of 8) all or none.
+template <bool ODD>
+struct Chunk {
+  int col, lo, hi;
+  __device__ __forceinline__ bool whole() const { return ODD ? lo == 0 && hi == 8 : hi == 8; }
+  __device__ __forceinline__ bool part() const { return ODD && !whole(); }
+};
+
+// Elements at .. at + 7 of p, which has `end` of them; those outside the chunk are anything.  A chunk of part of a row is read
+// whole where its memory is the matrix's.
+template <typename T, bool ODD>
+__device__ __forceinline__ Raw<T> load(const void* ptr, int64_t at, int64_t end, const Chunk<ODD>& c) {
+  const T* p = reinterpret_cast<const T*>(ptr) + at;
+  Raw<T> r;
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const u32x4 w = reinterpret_cast<const typename Packed<T>::type*>(at + 4 * k)->v;
+  for (int k = 0; k < Raw<T>::W; ++k) r.w[k] = u32x4{0u, 0u, 0u, 0u};
+  if (c.whole() || (ODD && c.lo < c.hi && at >= 0 && at + 8 <= end)) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const unsigned u = w[i];
-          x[4 * k + i] = __builtin_bit_cast(float, u);
-        }
-      }
-    } else {
-      const u32x4 w = reinterpret_cast<const typename Packed<T>::type*>(at)->v;
+    for (int k = 0; k < Raw<T>::W; ++k) r.w[k] = reinterpret_cast<const Packed<T>*>(p + 16 / sizeof(T) * k)->v;
+  } else if constexpr (ODD) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const unsigned u = w[i];
-        x[2 * i] = Elem<T>::lo(u);
-        x[2 * i + 1] = Elem<T>::hi(u);
-      }
+    for (int i = 0; i < 8; ++i) {
+      if (i < c.lo || i >= c.hi) continue;
+      if constexpr (sizeof(T) == 4) r.w[i / 4][i % 4] = reinterpret_cast<const unsigned*>(p)[i];
+      else r.w[0][i / 2] |= (unsigned)reinterpret_cast<const unsigned short*>(p)[i] << (16 * (i % 2));
     }
-  } else {
+  }
+  return r;
+}
+
+// Its values, zeros outside the chunk.
+template <typename T, bool ODD>
+__device__ __forceinline__ void values(const Raw<T>& r, const Chunk<ODD>& c, float (&x)[8]) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = i < n ? to_float(at[i]) : 0.f;
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (sizeof(T) == 4) {
+      const unsigned a = r.w[0][i], b = r.w[1][i];
+      x[i] = __builtin_bit_cast(float, a);
+      x[4 + i] = __builtin_bit_cast(float, b);
+    } else {
+      const unsigned u = r.w[0][i];
+      x[2 * i] = Elem<T>::lo(u);
+      x[2 * i + 1] = Elem<T>::hi(u);
+    }
+  }
+  if (c.part()) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = i >= c.lo && i < c.hi ? x[i] : 0.f;
   }
 }
 
-// The first n of 8 values, rounded to T.
-template <typename T>
-__device__ __forceinline__ void put8(T* at, int n, const float (&x)[8]) {
-  if (n >= 8) {
+template <typename T, bool ODD>
+__device__ __forceinline__ void get8(const void* p, int64_t at, int64_t end, const Chunk<ODD>& c, float (&x)[8]) {
+  values<T>(load<T>(p, at, end, c), c, x);
+}
+
+// The chunk's values, rounded to T.
+template <typename T, bool ODD>
+__device__ __forceinline__ void put8(void* ptr, int64_t index, const Chunk<ODD>& c, const float (&x)[8]) {
+  T* at = reinterpret_cast<T*>(ptr) + index;
+  if (c.whole()) {
     if constexpr (sizeof(T) == 4) {
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
@@ -74,19 +105,29 @@ __device__ __forceinline__ void put8(T* at, int n, const float (&x)[8]) {
           const float f = x[4 * k + i];
           w[i] = __builtin_bit_cast(unsigned, f);
         }
-        reinterpret_cast<typename Packed<T>::type*>(at + 4 * k)->v = w;
+        reinterpret_cast<Packed<T>*>(at + 4 * k)->v = w;
       }
     } else {
       u32x4 w;
 #pragma unroll
       for (int i = 0; i < 4; ++i) w[i] = Elem<T>::pack2(x[2 * i], x[2 * i + 1]);
-      reinterpret_cast<typename Packed<T>::type*>(at)->v = w;
+      reinterpret_cast<Packed<T>*>(at)->v = w;
     }
-  } else {
+  } else if constexpr (ODD) {
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-      if (i < n) at[i] = (T)x[i];
+      if (i >= c.lo && i < c.hi) at[i] = (T)x[i];
   }
+}
+
+// A lane's chunk number i of a row of M that begins `shift` elements behind a multiple of 8: the chunks begin at
+// multiples of 8 of the matrix, so that they are whole 16-byte words of a matrix of any M.  (Rows of 5119: 277 us of a
+// backward pass over 8191 of them with chunks from the row's first element, whose words lie across two.)
+template <bool ODD>
+__device__ __forceinline__ Chunk<ODD> chunk_of(int i, int shift, int M) {
+  if constexpr (!ODD) return {8 * i, 0, 8 * i < M ? 8 : 0};
+  const int col = 8 * i - shift;
+  return {col, max(-col, 0), max(min(M - col, 8), 0)};
 }
 
 // Values as T holds them.
@@ -107,12 +148,49 @@ struct Most {
   }
 };
 
-// Joins x over the `lanes` lanes of a row (of several waves through `shared`, which the caller's next
-// join has to differ from).
+// x of the lane that a DPP control names.
+template <int CTRL, typename V>
+__device__ __forceinline__ V of_lane(V x) {
+  if constexpr (sizeof(V) == 4) {
+    return __builtin_bit_cast(V, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, 0xf, 0xf, true));
+  } else {
+    const uint64_t b = __builtin_bit_cast(uint64_t, x);
+    const uint64_t lo = (unsigned)__builtin_amdgcn_update_dpp(0, (int)(unsigned)b, CTRL, 0xf, 0xf, true);
+    const uint64_t hi = (unsigned)__builtin_amdgcn_update_dpp(0, (int)(b >> 32), CTRL, 0xf, 0xf, true);
+    return __builtin_bit_cast(V, hi << 32 | lo);
+  }
+}
+
+// x joined over groups of `n` lanes (4 to 64), each of which gets all of it.  By lane exchanges in the vector unit (six steps of
+// an fp64 sum 0.1 us; through LDS 0.4).
+template <typename J, typename V>
+__device__ __forceinline__ V join_lanes(V x, int n) {
+  x = J::join(x, of_lane<0xB1>(x));              // pairs
+  x = J::join(x, of_lane<0x4E>(x));              // fours
+  if (n > 4) x = J::join(x, of_lane<0x141>(x));  // eights: mirrored, the fours being alike
+  if (n > 8) x = J::join(x, of_lane<0x140>(x));  // sixteens
+  auto swap = [&](auto&& exchange) __attribute__((always_inline)) {
+    if constexpr (sizeof(V) == 4) {
+      const auto r = exchange(__builtin_bit_cast(unsigned, x));
+      const unsigned a = r[0], b = r[1];
+      x = J::join(__builtin_bit_cast(V, a), __builtin_bit_cast(V, b));
+    } else {
+      const uint64_t v = __builtin_bit_cast(uint64_t, x);
+      const auto lo = exchange((unsigned)v), hi = exchange((unsigned)(v >> 32));
+      const unsigned a0 = lo[0], a1 = hi[0], b0 = lo[1], b1 = hi[1];
+      x = J::join(__builtin_bit_cast(V, (uint64_t)a1 << 32 | a0), __builtin_bit_cast(V, (uint64_t)b1 << 32 | b0));
+    }
+  };
+  if (n > 16) swap([](unsigned u) __attribute__((always_inline)) { return __builtin_amdgcn_permlane16_swap(u, u, false, false); });
+  if (n > 32) swap([](unsigned u) __attribute__((always_inline)) { return __builtin_amdgcn_permlane32_swap(u, u, false, false); });
+  return x;
+}
+
+// Joins x over the `lanes` lanes of a row (of several waves through `shared`, which the caller's next join
+// has to differ from).
 template <typename J, typename V>
 __device__ __forceinline__ V join_row(V x, int lanes, V* shared) {
-#pragma unroll
-  for (int m = 32; m > 0; m >>= 1) x = J::join(x, __shfl_xor(x, m, 64));
+  x = join_lanes<J>(x, 64);
   if (lanes > 64) {
     if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = x;
     __syncthreads();
@@ -123,18 +201,16 @@ __device__ __forceinline__ V join_row(V x, int lanes, V* shared) {
   return x;
 }
 
-// z in fp32, rounded to odd: toward zero, its last bit set where that lost something, so that a
-// second rounding to fewer bits gives what one rounding of z would.
+// z in fp32, rounded to odd at 20 bits of mantissa (the upper word of z, its last bit set where the lower
+// one is not zero), so that a second rounding to fewer bits gives what one rounding of z would.
 __device__ __forceinline__ float to_odd(double z) {
-  const float f = (float)z;
-  const double d = (double)f;
-  unsigned b = __builtin_bit_cast(unsigned, f);
-  b -= __builtin_fabs(d) > __builtin_fabs(z) ? 1u : 0u;
-  b |= d != z ? 1u : 0u;
-  return __builtin_bit_cast(float, b);
+  const uint64_t b = __builtin_bit_cast(uint64_t, z);
+  const unsigned lo = (unsigned)b;
+  const uint64_t odd = (uint64_t)((unsigned)(b >> 32) | (lo < 1u ? lo : 1u)) << 32;
+  return (float)__builtin_bit_cast(double, odd);
 }
 
-// 8 codes of z, in two words.
+// 8 codes of z, in two words.  (Only under a scale that is no normal number is |z| over the largest code.)
 __device__ __forceinline__ uint2 codes8(const double (&z)[8], bool int8) {
   unsigned w[2] = {0u, 0u};
 #pragma unroll
@@ -145,12 +221,12 @@ __device__ __forceinline__ uint2 codes8(const double (&z)[8], bool int8) {
     if (int8) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const int c = (int)__builtin_rintf(fminf(fmaxf(f[i], -127.f), 127.f));
+        const int c = (int)__builtin_rintf(__builtin_amdgcn_fmed3f(f[i], -127.f, 127.f));
         w[k] |= ((unsigned)c & 255u) << (8 * i);
       }
     } else {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) f[i] = fminf(fmaxf(f[i], -448.f), 448.f);
+      for (int i = 0; i < 4; ++i) f[i] = __builtin_amdgcn_fmed3f(f[i], -448.f, 448.f);
       w[k] = (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(f[0], f[1], 0, false);
       w[k] = (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(f[2], f[3], (int)w[k], true);
     }
@@ -160,36 +236,71 @@ __device__ __forceinline__ uint2 codes8(const double (&z)[8], bool int8) {
 
 struct __attribute__((packed, aligned(1))) Bytes8 { uint2 v; };
 
+// The rows that a lane's place in its workgroup takes: from `first` in steps of `step`, those below `last`.  (A run
+// of rows for each XCD instead, so that the words which two rows share pass through one L2, was 3 to 10 % slower, rows
+// of 5119 among them.)
+struct Turns {
+  int64_t first, step, last;
+};
+__device__ __forceinline__ Turns turns_of(int64_t N, int rpb, int sub) {
+  return {(int64_t)blockIdx.x * rpb + sub, (int64_t)gridDim.x * rpb, N};
+}
+
 // T: the type of x, the weight and y; R: that of the residual and h.  C: steps of 8 elements a
-// lane.  QUANT: y in 8 bits.
-template <typename T, typename R, int C, bool QUANT>
+// lane.  QUANT: y in 8 bits.  A workgroup takes rows in turn, the next row's words on their way while one is worked on, in
+// one step and without ODD.  (More steps have no registers for it.  With ODD the stores are conditional, and the wait for the
+// next row's words is one for the stores behind them too: 8191 rows of 5119 take 131 us in turns, 101 with a workgroup each.)
+template <typename T, typename R, int C, bool QUANT, bool ODD>
 __global__ __launch_bounds__(kMaxThreads) void rmsnorm_add_kernel(RmsnormParams p) {
-  __shared__ double sums[kMaxWaves];
-  __shared__ double tops[kMaxWaves];
+  constexpr bool AHEAD = C == 1 && !ODD;
+  __shared__ double sums[2][kMaxWaves];
+  __shared__ double tops[2][kMaxWaves];
   const int lanes = p.lanes, rpb = blockDim.x / lanes;
   const int sub = threadIdx.x / lanes, t = threadIdx.x % lanes;
   const int M = p.M;
-  for (int64_t first = (int64_t)blockIdx.x * rpb; first < p.N; first += (int64_t)gridDim.x * rpb) {
-    const int64_t row = first + sub;
-    const bool in = row < p.N;
+  const int64_t end = (int64_t)p.N * M;
+  const Turns turns = turns_of(p.N, rpb, sub);
+  // (Groups begin at a chunk's first element.)
+  auto shift_of = [&](int64_t row) __attribute__((always_inline)) { return !ODD || (QUANT && p.group) ? 0 : (int)(row * M & 7); };
+  struct Words {
+    Raw<T> x[C];
+    Raw<R> r[C];
+  };
+  auto fetch = [&](int64_t row, Words& w) __attribute__((always_inline)) {
+    const bool in = row < turns.last;
+    const int64_t base = (in ? row : 0) * M;
+    const int shift = shift_of(row);
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const auto k = chunk_of<ODD>(c * lanes + t, shift, in ? M : 0);
+      w.x[c] = load<T>(p.x, base + k.col, end, k);
+      if (p.residual) w.r[c] = load<R>(p.residual, base + k.col, end, k);
+    }
+  };
+  Words now, next;
+  int turn = 0;
+  fetch(turns.first, now);
+  // (All rows of a workgroup take as many turns as its first.)
+  for (int64_t row = turns.first; row - sub < turns.last; row += turns.step, turn ^= 1) {
+    const bool in = row < turns.last;
     const int m = in ? M : 0;
     const int64_t base = (in ? row : 0) * M;
+    const int shift = shift_of(row);
+    auto chunk = [&](int c) __attribute__((always_inline)) { return chunk_of<ODD>(c * lanes + t, shift, m); };
+    const bool more = row - sub + turns.step < turns.last;
+    if (AHEAD && more) fetch(row + turns.step, next);
     float h[C][8];
     double ss = 0.0;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      const int col = 8 * (c * lanes + t);
-      get8(reinterpret_cast<const T*>(p.x) + base + col, m - col, h[c]);
-    }
-    if (p.residual) {
+      const auto k = chunk(c);
+      values(now.x[c], k, h[c]);
+      if (p.residual) {
+        float y[8];
+        values(now.r[c], k, y);
 #pragma unroll
-      for (int c = 0; c < C; ++c) {
-        const int col = 8 * (c * lanes + t);
-        float r[8];
-        get8(reinterpret_cast<const R*>(p.residual) + base + col, m - col, r);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) h[c][i] += r[i];
-        put8(reinterpret_cast<R*>(p.h) + base + col, m - col, h[c]);
+        for (int i = 0; i < 8; ++i) h[c][i] += y[i];
+        put8<R>(p.h, base + k.col, k, h[c]);
         round8<R>(h[c]);
       }
     }
@@ -197,110 +308,152 @@ __global__ __launch_bounds__(kMaxThreads) void rmsnorm_add_kernel(RmsnormParams 
     for (int c = 0; c < C; ++c)
 #pragma unroll
       for (int i = 0; i < 8; ++i) ss = __builtin_fma((double)h[c][i], (double)h[c][i], ss);
-    ss = join_row<Sum>(ss, lanes, sums);
+    ss = join_row<Sum>(ss, lanes, sums[turn]);
     const double rstd = 1.0 / __builtin_sqrt(ss / M + p.eps);
     if (p.rstd && in && t == 0) p.rstd[row] = (float)rstd;
     if constexpr (!QUANT) {
       const float r = (float)rstd;
 #pragma unroll
       for (int c = 0; c < C; ++c) {
-        const int col = 8 * (c * lanes + t);
+        const auto k = chunk(c);
         float w[8], y[8];
-        if (p.weight) get8(reinterpret_cast<const T*>(p.weight) + col, m - col, w);
+        if (p.weight) get8<T>(p.weight, k.col, M, k, w);
 #pragma unroll
         for (int i = 0; i < 8; ++i) y[i] = p.weight ? h[c][i] * r * (w[i] + p.offset) : h[c][i] * r;
-        put8(reinterpret_cast<T*>(p.y) + base + col, m - col, y);
+        put8<T>(p.y, base + k.col, k, y);
       }
     } else {
       const double most = p.int8 ? 127.0 : 448.0;
       const int G = p.group;
-      double top = 0.0;
-      double g = 0.0;          // rstd over the scale
       auto weighed = [&](int c, double (&z)[8]) __attribute__((always_inline)) {    // h (w + offset)
-        const int col = 8 * (c * lanes + t);
         float w[8];
-        if (p.weight) get8(reinterpret_cast<const T*>(p.weight) + col, m - col, w);
+        if (p.weight) {
+          get8<T>(p.weight, chunk(c).col, M, chunk(c), w);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) z[i] = p.weight ? (double)h[c][i] * ((double)w[i] + (double)p.offset) : (double)h[c][i];
+          for (int i = 0; i < 8; ++i) z[i] = (double)h[c][i] * ((double)w[i] + (double)p.offset);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) z[i] = (double)h[c][i];
+        }
       };
-      auto scaled = [&](double a, int64_t at, bool writes) {
+      // The largest magnitude, NaN where one of them is an infinity or NaN.
+      auto largest = [](const double (&z)[8]) __attribute__((always_inline)) {
+        double a = __builtin_fabs(z[0]), bad = z[0] * 0.0;
+#pragma unroll
+        for (int i = 1; i < 8; ++i) {
+          a = __builtin_fmax(a, __builtin_fabs(z[i]));
+          bad = __builtin_fma(z[i], 0.0, bad);
+        }
+        return __builtin_fabs(a + bad);
+      };
+      // rstd over the scale of a group whose largest |h (w + offset)| is a; 0 where its codes are zeros.
+      auto scaled = [&](double a, int64_t at, bool writes) __attribute__((always_inline)) {
         float s = (float)(a * rstd / most);
         const bool fine = s <= 3.4028234663852886e38f;     // (not an infinity or NaN)
         if (!fine) s = __builtin_nanf("");
         if (writes) p.scales[at] = s;
         return fine && s > 0.f ? rstd / (double)s : 0.0;
       };
+      auto put = [&](int c, double (&z)[8], double g) __attribute__((always_inline)) {
+        const auto k = chunk(c);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) z[i] *= g;
+        const uint2 w = g == 0.0 ? make_uint2(0u, 0u) : codes8(z, p.int8);
+        unsigned char* at = reinterpret_cast<unsigned char*>(p.y) + base + k.col;
+        if (k.whole()) {
+          reinterpret_cast<Bytes8*>(at)->v = w;
+        } else {
+          for (int i = k.lo; i < k.hi; ++i) at[i] = (unsigned char)((i < 4 ? w.x : w.y) >> (8 * (i & 3)));
+        }
+      };
       if (G == 0) {
+        double top = 0.0;
 #pragma unroll
         for (int c = 0; c < C; ++c) {
           double z[8];
           weighed(c, z);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) top = Most::join(top, __builtin_fabs(z[i]));
+          top = Most::join(top, largest(z));
         }
-        top = join_row<Most>(top, lanes, tops);
-        g = scaled(top, row, in && t == 0);
-      }
+        top = join_row<Most>(top, lanes, tops[turn]);
+        const double g = scaled(top, row, in && t == 0);
 #pragma unroll
-      for (int c = 0; c < C; ++c) {
-        const int col = 8 * (c * lanes + t);
-        double z[8];
-        weighed(c, z);
-        if (G != 0) {
-          double a = 0.0;
-#pragma unroll
-          for (int i = 0; i < 8; ++i) a = Most::join(a, __builtin_fabs(z[i]));
-          for (int k = G / 16; k > 0; k >>= 1) a = Most::join(a, __shfl_xor(a, k, 64));
-          g = scaled(a, row * p.groups + col / G, col < m && col % G == 0);
+        for (int c = 0; c < C; ++c) {
+          double z[8];
+          weighed(c, z);
+          put(c, z, g);
         }
+      } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) z[i] = g == 0.0 ? 0.0 : z[i] * g;
-        const uint2 w = codes8(z, p.int8);
-        unsigned char* at = reinterpret_cast<unsigned char*>(p.y) + base + col;
-        if (m - col >= 8) {
-          reinterpret_cast<Bytes8*>(at)->v = w;
-        } else {
-          for (int i = 0; i < m - col; ++i) at[i] = (unsigned char)((i < 4 ? w.x : w.y) >> (8 * (i & 3)));
+        for (int c = 0; c < C; ++c) {
+          const int col = 8 * (c * lanes + t);
+          double z[8];
+          weighed(c, z);
+          double a = largest(z);
+          a = join_lanes<Most>(a, G / 8);
+          put(c, z, scaled(a, row * p.groups + col / G, col < m && col % G == 0));
         }
       }
     }
-    if (lanes > 64) __syncthreads();      // before the next row's sums
+    if (AHEAD) now = next;
+    else if (more) fetch(row + turns.step, now);
   }
 }
 
 // Gradients.  A workgroup takes rows in turn, and its lanes keep the sum of dY n of their columns over
-// them: [partials, M] in fp32, summed by rmsnorm_dweight_kernel in a fixed order.
-template <typename T, typename R, int C>
+// them: [workgroups, M] in fp32, summed by rmsnorm_dweight_kernel in a fixed order.  The next row's words are on their
+// way while a row is worked on.
+template <typename T, typename R, int C, bool ODD>
 __global__ __launch_bounds__(kMaxThreads) void rmsnorm_add_bwd_kernel(RmsnormBwdParams p) {
+  constexpr bool AHEAD = C == 1;               // (more steps have no registers for it)
   __shared__ float sums[2][kMaxWaves];
+  __shared__ float joined[C == 1 ? 2048 : 1];      // rpb rows of at most 64 or 128 lanes
   const int lanes = p.lanes, rpb = blockDim.x / lanes;
   const int sub = threadIdx.x / lanes, t = threadIdx.x % lanes;
   const int M = p.M;
+  const int64_t end = (int64_t)p.N * M;
+  const Turns turns = turns_of(p.N, rpb, sub);
+  const int shift = ODD ? (int)(turns.first * M & 7) : 0;       // of all its rows: a lane's columns stay the same
+  auto chunk = [&](int c, bool in) __attribute__((always_inline)) { return chunk_of<ODD>(c * lanes + t, shift, in ? M : 0); };
   float dw[C][8];
 #pragma unroll
   for (int c = 0; c < C; ++c)
 #pragma unroll
     for (int i = 0; i < 8; ++i) dw[c][i] = 0.f;
-  int turn = 0;
-  for (int64_t first = (int64_t)blockIdx.x * rpb; first < p.N; first += (int64_t)gridDim.x * rpb, turn ^= 1) {
-    const int64_t row = first + sub;
-    const bool in = row < p.N;
-    const int m = in ? M : 0;
+  struct Words {
+    Raw<T> dy[C];
+    Raw<R> h[C], dh[C];
+    float rstd;
+  };
+  auto fetch = [&](int64_t row, Words& w) __attribute__((always_inline)) {
+    const bool in = row < turns.last;
     const int64_t base = (in ? row : 0) * M;
-    const float r = in ? p.rstd[row] : 0.f;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const auto k = chunk(c, in);
+      w.dy[c] = load<T>(p.dy, base + k.col, end, k);
+      w.h[c] = load<R>(p.h, base + k.col, end, k);
+      if (p.dh) w.dh[c] = load<R>(p.dh, base + k.col, end, k);
+    }
+    w.rstd = in ? p.rstd[row] : 0.f;
+  };
+  Words now, next;
+  fetch(turns.first, now);
+  int turn = 0;
+  for (int64_t row = turns.first; row - sub < turns.last; row += turns.step, turn ^= 1) {
+    const bool in = row < turns.last;
+    const int64_t base = (in ? row : 0) * M;
+    const bool more = row - sub + turns.step < turns.last;
+    if (AHEAD && more) fetch(row + turns.step, next);
+    const float r = now.rstd;
     float g[C][8], n[C][8];
     float s = 0.f;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      const int col = 8 * (c * lanes + t);
-      get8(reinterpret_cast<const T*>(p.dy) + base + col, m - col, g[c]);
-      get8(reinterpret_cast<const R*>(p.h) + base + col, m - col, n[c]);
-    }
-#pragma unroll
-    for (int c = 0; c < C; ++c) {
-      const int col = 8 * (c * lanes + t);
+      const auto k = chunk(c, in);
       float w[8];
-      if (p.weight) get8(reinterpret_cast<const T*>(p.weight) + col, m - col, w);
+      values(now.dy[c], k, g[c]);
+      values(now.h[c], k, n[c]);
+      if (p.weight) get8<T>(p.weight, k.col, M, k, w);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         n[c][i] *= r;
@@ -312,24 +465,37 @@ __global__ __launch_bounds__(kMaxThreads) void rmsnorm_add_bwd_kernel(RmsnormBwd
     s = join_row<Sum>(s, lanes, sums[turn]) / (float)M;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      const int col = 8 * (c * lanes + t);
+      const auto k = chunk(c, in);
       float d[8];
-      if (p.dh) get8(reinterpret_cast<const R*>(p.dh) + base + col, m - col, d);
+      if (p.dh) values(now.dh[c], k, d);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const float x = r * __builtin_fmaf(-n[c][i], s, g[c][i]);
         d[i] = p.dh ? d[i] + x : x;
       }
-      if (p.dresidual) put8(reinterpret_cast<R*>(p.dresidual) + base + col, m - col, d);
-      put8(reinterpret_cast<T*>(p.dx) + base + col, m - col, d);
+      if (p.dresidual) put8<R>(p.dresidual, base + k.col, k, d);
+      put8<T>(p.dx, base + k.col, k, d);
     }
+    if (AHEAD) now = next;
+    else if (more) fetch(row + turns.step, now);
   }
   if (!p.ws) return;
-  float* at = p.ws + ((int64_t)blockIdx.x * rpb + sub) * M;
+  float* at = p.ws + (int64_t)blockIdx.x * M;
+  if (C > 1 || rpb == 1) {
 #pragma unroll
-  for (int c = 0; c < C; ++c) {
-    const int col = 8 * (c * lanes + t);
-    put8(at + col, M - col, dw[c]);
+    for (int c = 0; c < C; ++c) put8<float>(at, chunk(c, true).col, chunk(c, true), dw[c]);
+    return;
+  }
+  // Several rows at a time: their sums are joined first.
+  const auto k = chunk(0, true);
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (i >= k.lo && i < k.hi) joined[sub * M + k.col + i] = dw[0][i];
+  __syncthreads();
+  for (int i = threadIdx.x; i < M; i += blockDim.x) {
+    float x = joined[i];
+    for (int u = 1; u < rpb; ++u) x += joined[u * M + i];
+    at[i] = x;
   }
 }
 
@@ -338,8 +504,17 @@ __global__ __launch_bounds__(256) void rmsnorm_dweight_kernel(const float* ws, f
   __shared__ float part[8][32];
   const int col = blockIdx.x * 32 + threadIdx.x % 32, k = threadIdx.x / 32;
   float s = 0.f;
-  if (col < M)
-    for (int i = k; i < parts; i += 8) s += ws[(int64_t)i * M + col];
+  if (col < M) {
+    int i = k;
+    for (; i + 56 < parts; i += 64) {
+      float x[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) x[u] = ws[(int64_t)(i + 8 * u) * M + col];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) s += x[u];
+    }
+    for (; i < parts; i += 8) s += ws[(int64_t)i * M + col];
+  }
   part[k][threadIdx.x % 32] = s;
   __syncthreads();
   if (k == 0 && col < M) {
@@ -349,30 +524,31 @@ __global__ __launch_bounds__(256) void rmsnorm_dweight_kernel(const float* ws, f
 }
 
 // What codes stand for: 8 of them a lane.
-template <typename T>
+template <typename T, bool ODD>
 __global__ __launch_bounds__(256) void quant8_load_kernel(Quant8LoadParams p) {
-  const int chunks = (p.M + 7) / 8;
+  const int chunks = (ODD && !p.group ? p.M + 14 : p.M + 7) / 8;
   const int64_t all = (int64_t)p.N * chunks;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
-    const int64_t row = i / chunks;
-    const int col = 8 * (int)(i - row * chunks), n = p.M - col;
-    const unsigned char* at = p.codes + row * p.M + col;
+    const int64_t row = i / chunks, base = row * p.M;
+    const auto c = chunk_of<ODD>((int)(i - row * chunks), p.group ? 0 : (int)(base & 7), p.M);
+    if (c.lo >= c.hi) continue;
+    const unsigned char* at = p.codes + base + c.col;
     unsigned w[2] = {0u, 0u};
-    if (n >= 8) {
+    if (c.whole()) {
       const uint2 v = reinterpret_cast<const Bytes8*>(at)->v;
       w[0] = v.x;
       w[1] = v.y;
     } else {
-      for (int k = 0; k < n; ++k) w[k / 4] |= (unsigned)at[k] << (8 * (k & 3));
+      for (int k = c.lo; k < c.hi; ++k) w[k / 4] |= (unsigned)at[k] << (8 * (k & 3));
     }
-    const float s = p.scales[row * p.groups + (p.group ? col / p.group : 0)];
+    const float s = p.scales[row * p.groups + (p.group ? c.col / p.group : 0)];
     float y[8];
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
       const unsigned b = w[k / 4] >> (8 * (k & 3));
       y[k] = s * (p.int8 ? (float)(signed char)(b & 255u) : __builtin_amdgcn_cvt_f32_fp8((int)b, 0));
     }
-    put8(reinterpret_cast<T*>(p.y) + row * p.M + col, n, y);
+    put8<T>(p.y, base + c.col, c, y);
   }
 }
 
@@ -380,26 +556,26 @@ __global__ __launch_bounds__(256) void quant8_load_kernel(Quant8LoadParams p) {
 struct Split {
   int lanes, steps;
 };
-// By the row's length alone, so that a row's bits do not depend on how many there are.
+// By the row's length alone, so that a row's bits do not depend on how many there are.  One step of a lane
+// up to 8192 elements, by as many waves as it takes.
 Split split(int M) {
-  int lanes = 64;
-  while (lanes < kMaxThreads && 8 * lanes < M) lanes *= 2;
-  const int s = (M + 8 * lanes - 1) / (8 * lanes);
-  return {lanes, s <= 1 ? 1 : s <= 2 ? 2 : 4};
+  const int m = M % 8 ? M + 7 : M;             // (a row may begin within a chunk)
+  const int s = (m + 8 * kMaxThreads - 1) / (8 * kMaxThreads), steps = s <= 2 ? s : 4;
+  return {((m + 8 * steps - 1) / (8 * steps) + 63) / 64 * 64, steps};
 }
 
-template <typename T, typename R, bool QUANT>
+template <typename T, typename R, bool QUANT, bool ODD>
 void launch_add(const RmsnormParams& p, const Split& s, dim3 grid, dim3 block, hipStream_t stream) {
-  if (s.steps == 1) hipLaunchKernelGGL((rmsnorm_add_kernel<T, R, 1, QUANT>), grid, block, 0, stream, p);
-  else if (s.steps == 2) hipLaunchKernelGGL((rmsnorm_add_kernel<T, R, 2, QUANT>), grid, block, 0, stream, p);
-  else hipLaunchKernelGGL((rmsnorm_add_kernel<T, R, 4, QUANT>), grid, block, 0, stream, p);
+  if (s.steps == 1) hipLaunchKernelGGL((rmsnorm_add_kernel<T, R, 1, QUANT, ODD>), grid, block, 0, stream, p);
+  else if (s.steps == 2) hipLaunchKernelGGL((rmsnorm_add_kernel<T, R, 2, QUANT, ODD>), grid, block, 0, stream, p);
+  else hipLaunchKernelGGL((rmsnorm_add_kernel<T, R, 4, QUANT, ODD>), grid, block, 0, stream, p);
 }
 
-template <typename T, typename R>
+template <typename T, typename R, bool ODD>
 void launch_bwd(const RmsnormBwdParams& p, const Split& s, dim3 grid, dim3 block, hipStream_t stream) {
-  if (s.steps == 1) hipLaunchKernelGGL((rmsnorm_add_bwd_kernel<T, R, 1>), grid, block, 0, stream, p);
-  else if (s.steps == 2) hipLaunchKernelGGL((rmsnorm_add_bwd_kernel<T, R, 2>), grid, block, 0, stream, p);
-  else hipLaunchKernelGGL((rmsnorm_add_bwd_kernel<T, R, 4>), grid, block, 0, stream, p);
+  if (s.steps == 1) hipLaunchKernelGGL((rmsnorm_add_bwd_kernel<T, R, 1, ODD>), grid, block, 0, stream, p);
+  else if (s.steps == 2) hipLaunchKernelGGL((rmsnorm_add_bwd_kernel<T, R, 2, ODD>), grid, block, 0, stream, p);
+  else hipLaunchKernelGGL((rmsnorm_add_bwd_kernel<T, R, 4, ODD>), grid, block, 0, stream, p);
 }
 
 // The call's types: dtype 0 fp16, 1 bf16, 2 fp32, and whether the residual stream is fp32.
@@ -412,16 +588,24 @@ void with_types(int dtype, bool wide, F&& f) {
   else f(_Float16{}, _Float16{});
 }
 
-int rows_per_block(const Split& s) { return std::max(256 / s.lanes, 1); }
+// Rows of a workgroup: of at least 256 lanes, where that many divide alike.
+int rows_per_block(const Split& s) { return s.lanes == 64 ? 4 : s.lanes == 128 ? 2 : 1; }
 
-constexpr int64_t kMaxBlocks = 1 << 20;      // more rows than that many workgroups take in turn
-constexpr int64_t kBwdBlocks = 1024;         // workgroups of the backward pass, each a partial of dweight
+constexpr int64_t kMaxBlocks = 1 << 20;      // (more rows are taken in turn)
+
+// Workgroups that take rows in turn: as many as 256 compute units hold at a time (20 waves each), a
+// multiple of 8.  (Each is a partial of dweight.)
+int64_t resident(const Split& s) {
+  const int waves = s.lanes * rows_per_block(s) / 64;
+  return 256 * std::max(20 / waves, 1);
+}
 
 }  // namespace
 
 int64_t rmsnorm_bwd_partials(int64_t N, int M) {
-  const int rpb = rows_per_block(split(M));
-  return std::min((N + rpb - 1) / rpb, kBwdBlocks) * rpb;
+  const Split s = split(M);
+  const int rpb = rows_per_block(s);
+  return std::min((N + rpb - 1) / rpb, resident(s));
 }
 
 hipError_t launch_rmsnorm_add(const RmsnormParams& p, hipStream_t stream) {
@@ -429,10 +613,18 @@ hipError_t launch_rmsnorm_add(const RmsnormParams& p, hipStream_t stream) {
   RmsnormParams q = p;
   q.lanes = s.lanes;
   const int rpb = rows_per_block(s);
-  const dim3 grid((unsigned)std::min(((int64_t)p.N + rpb - 1) / rpb, kMaxBlocks)), block(s.lanes * rpb);
+  const bool turns = s.steps == 1 && p.M % 8 == 0;
+  const dim3 grid((unsigned)std::min(((int64_t)p.N + rpb - 1) / rpb, turns ? resident(s) : kMaxBlocks)), block(s.lanes * rpb);
   with_types(p.dtype, p.wide, [&](auto t, auto r) {
-    if (p.scales) launch_add<decltype(t), decltype(r), true>(q, s, grid, block, stream);
-    else launch_add<decltype(t), decltype(r), false>(q, s, grid, block, stream);
+    typedef decltype(t) T;
+    typedef decltype(r) R;
+    if (p.M % 8 == 0) {
+      if (p.scales) launch_add<T, R, true, false>(q, s, grid, block, stream);
+      else launch_add<T, R, false, false>(q, s, grid, block, stream);
+    } else {
+      if (p.scales) launch_add<T, R, true, true>(q, s, grid, block, stream);
+      else launch_add<T, R, false, true>(q, s, grid, block, stream);
+    }
   });
   return hipGetLastError();
 }
@@ -444,7 +636,9 @@ hipError_t launch_rmsnorm_add_bwd(const RmsnormBwdParams& p, float* dweight, hip
   const int rpb = rows_per_block(s);
   const int64_t parts = rmsnorm_bwd_partials(p.N, p.M);
   with_types(p.dtype, p.wide, [&](auto t, auto r) {
-    launch_bwd<decltype(t), decltype(r)>(q, s, dim3((unsigned)(parts / rpb)), dim3(s.lanes * rpb), stream);
+    const dim3 grid((unsigned)parts), block(s.lanes * rpb);
+    if (p.M % 8 == 0) launch_bwd<decltype(t), decltype(r), false>(q, s, grid, block, stream);
+    else launch_bwd<decltype(t), decltype(r), true>(q, s, grid, block, stream);
   });
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || !dweight) return e;
@@ -453,11 +647,12 @@ hipError_t launch_rmsnorm_add_bwd(const RmsnormBwdParams& p, float* dweight, hip
 }
 
 hipError_t launch_quant8_load(const Quant8LoadParams& p, hipStream_t stream) {
-  const int64_t all = (int64_t)p.N * ((p.M + 7) / 8);
+  const int64_t all = (int64_t)p.N * ((p.M % 8 && !p.group ? p.M + 14 : p.M + 7) / 8);
   const dim3 grid((unsigned)std::min((all + 255) / 256, kMaxBlocks)), block(256);
-  if (p.dtype == 2) hipLaunchKernelGGL((quant8_load_kernel<float>), grid, block, 0, stream, p);
-  else if (p.dtype == 1) hipLaunchKernelGGL((quant8_load_kernel<__bf16>), grid, block, 0, stream, p);
-  else hipLaunchKernelGGL((quant8_load_kernel<_Float16>), grid, block, 0, stream, p);
+  with_types(p.dtype, false, [&](auto t, auto) {
+    if (p.M % 8 == 0) hipLaunchKernelGGL((quant8_load_kernel<decltype(t), false>), grid, block, 0, stream, p);
+    else hipLaunchKernelGGL((quant8_load_kernel<decltype(t), true>), grid, block, 0, stream, p);
+  });
   return hipGetLastError();
 }
 
