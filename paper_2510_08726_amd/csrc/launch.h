@@ -199,6 +199,7 @@ struct RmsnormParams {
   void* h;
   float* rstd;          // or nullptr
   double eps;
+  double inv;           // 1 / M, set by the launcher
   int N, M;
   int group, groups;    // elements that share a scale (0: the row), and scales of a row
   float offset;         // added to the weight
