@@ -121,11 +121,11 @@ __device__ __forceinline__ u32x4 resource(const void* base, unsigned bytes) {
 // past the resource's end zeros.
 __device__ __forceinline__ void copy16(const u32x4& rs, uint32_t dst, int off) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
-               : : "s"(dst), "v"(off), "s"(rs) : "memory", "m0");
+               : : "s"(__builtin_amdgcn_readfirstlane((int)dst)), "v"(off), "s"(rs) : "memory", "m0");
 }
 __device__ __forceinline__ void copy4(const u32x4& rs, uint32_t dst, int off) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds"
-               : : "s"(dst), "v"(off), "s"(rs) : "memory", "m0");
+               : : "s"(__builtin_amdgcn_readfirstlane((int)dst)), "v"(off), "s"(rs) : "memory", "m0");
 }
 
 template <typename T>
@@ -322,9 +322,33 @@ __device__ __forceinline__ void store(const f32x16 (&acc)[D / 32], float f, T* o
 // share a compute unit's 160 KB.
 constexpr int kStages = 4;
 template <int D> constexpr int kStage = 2 * TN * D * 2 + 256;
-// Operands read ahead of their MFMA, and the registers (of 16 bytes a lane) that they pass through.
+// Operands read ahead of their MFMA (LDS takes about four MFMAs' time, and two waves share a SIMD), and the registers of 16
+// bytes a lane that they pass through: kAhead + 1, and one more beside the first product, where the others are short by it
+// of a whole number of turns.
 constexpr int kAhead = 2;
 constexpr int kFrags = 4;
+template <int N1, int NF>
+constexpr int frag_of(int i) {
+  constexpr int R = kAhead + 1;
+  i %= NF;
+  if constexpr (NF % R == 0) return i % R;
+  else return i < N1 ? i % (R + 1) : (i - N1) % R;
+}
+// Operands i .. i + kAhead lie in different ones, also from one tile to the next.
+template <int N1, int NF>
+constexpr bool frags_apart() {
+  for (int i = 0; i < NF; ++i)
+    for (int j = 1; j <= kAhead; ++j)
+      if (frag_of<N1, NF>(i) == frag_of<N1, NF>(i + j)) return false;
+  return true;
+}
+
+// x as it is, computed here: the compiler otherwise adds the constants behind it before the loop, each into a register
+// of its own.
+__device__ __forceinline__ int here(int x) {
+  asm volatile("" : "+s"(x));
+  return x;
+}
 
 // dK and dV of 128 keys of a KV head: the tiles of 32 queries that see them, of all query heads of
 // the group, or a part of them (a partial in fp32, summed by bwd_sum_kernel).
@@ -376,15 +400,15 @@ __device__ __forceinline__ void dkv_block(const BwdParams& p, char* lds, int ite
   }
 
   // Copies: this wave's blocks of the Q and dO tiles and, every wave alike, the tile's 64 floats.
+  // Blocks wave, wave + 4 of a tile: 16 rows apart, where the swizzle is the same.
   const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_void*)lds;
-  int qoff[CB], goff[CB];
-#pragma unroll
-  for (int u = 0; u < CB; ++u) {
-    const int r = (wave * CB + u) * (1024 / (2 * D)) + lane / CPR;
-    const int c = 8 * ((lane % CPR) ^ swz<D>(r));
-    qoff[u] = (r * D + c) * 2;
-    goff[u] = (int)(r * p.do_sl + c) * 2;
+  int qoff, goff;
+  {
+    const int r = wave * (1024 / (2 * D)) + lane / CPR, c = 8 * ((lane % CPR) ^ swz<D>(r));
+    qoff = (r * D + c) * 2;
+    goff = (int)(r * p.do_sl + c) * 2;
   }
+  static_assert(CB == 1 || kWaves * 1024 / (2 * D) == 16, "a wave's blocks lie 16 rows apart");
   const int gstep = (int)(TN * p.do_sl) * 2;
   // The next tile to copy, tile ct of head h0 + cg; cut off the resources of its head's rows.
   int cu = u0, cg = nt ? u0 / nt : 0, ct = ta + (nt ? u0 % nt : 0);
@@ -400,13 +424,13 @@ __device__ __forceinline__ void dkv_block(const BwdParams& p, char* lds, int ite
                             (unsigned)(p.group * p.row_tiles) * (8 * TN));
   auto copy_next = [&]() __attribute__((always_inline)) {
     if (cu >= u1) return;
-    const uint32_t dst = lds0 + (uint32_t)((cu - u0) % kStages * STAGE);
+    const uint32_t dst = lds0 + (uint32_t)(cu - u0) % kStages * STAGE;
 #pragma unroll
     for (int u = 0; u < CB; ++u) {
-      copy16(rq, dst + (uint32_t)((wave * CB + u) * 1024), qoff[u] + ct * TB);
-      copy16(rg, dst + (uint32_t)(TB + (wave * CB + u) * 1024), goff[u] + ct * gstep);
+      copy16(rq, dst + (uint32_t)((wave + u * kWaves) * 1024), qoff + here(ct * TB + u * (TB / 2)));
+      copy16(rg, dst + (uint32_t)(TB + (wave + u * kWaves) * 1024), goff + here(ct * gstep + u * (gstep / 2)));
     }
-    copy4(rx, dst + 2 * TB, 4 * lane + (cg * p.row_tiles + ct) * (8 * TN));
+    copy4(rx, dst + 2 * TB, 4 * lane + here((cg * p.row_tiles + ct) * (8 * TN)));
     ++cu;
     if (++ct == ta + nt) {
       ct = ta;
@@ -427,11 +451,12 @@ __device__ __forceinline__ void dkv_block(const BwdParams& p, char* lds, int ite
   // at the end of the tile before, and so are the starts of its scores.
   constexpr int n1 = TL::KX, n2 = 2 * TL::KX, n3 = 3 * TL::KX, NF = 4 * TL::KX;
   static_assert(2 * TL::DB == TL::KX, "as many steps over dims as over rows");
+  static_assert(frags_apart<n1, NF>(), "an operand is not read into another's place");
   vec8 fr[kFrags];
   f32x16 s, x;
   auto read = [&](auto ic, uint32_t st, uint32_t next) __attribute__((always_inline)) {
     constexpr int i = decltype(ic)::value;
-    vec8& f = fr[i % kFrags];
+    vec8& f = fr[frag_of<n1, NF>(i)];
     if constexpr (i < n1) f = TL::template rows<i>(st + roff, 0);
     else if constexpr (i < n2) f = TL::template rows<i - n1>(st + roff, TB);
     else if constexpr (i < n3) f = TL::template dims<(i - n2) / TL::DB, (i - n2) % TL::DB>(st + doff, TB);
@@ -439,9 +464,11 @@ __device__ __forceinline__ void dkv_block(const BwdParams& p, char* lds, int ite
     else f = TL::template rows<i - NF>(next + roff, 0);
   };
   auto starts = [&](f32x16& a, uint32_t at) __attribute__((always_inline)) {
+    uint32_t to;
+    asm volatile("v_lshl_add_u32 %0, %1, 4, %2" : "=v"(to) : "v"(hh), "s"(at));
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
-      const f32x4 v = *(lds_f32x4*)(uintptr_t)(at + 16 * hh + 32 * g);
+      const f32x4 v = *(lds_f32x4*)(uintptr_t)(to + 32 * g);
 #pragma unroll
       for (int i = 0; i < 4; ++i) a[4 * g + i] = v[i];
     }
@@ -490,8 +517,8 @@ __device__ __forceinline__ void dkv_block(const BwdParams& p, char* lds, int ite
     static_for<NF>([&](auto ic) {
       constexpr int i = decltype(ic)::value;
       read(std::integral_constant<int, i + kAhead>{}, st, next);
-      if constexpr (i == 0) starts(x, st + 2 * TB + 4 * TN);
-      const vec8 f = fr[i % kFrags];
+      if constexpr (i == n1 - 2) starts(x, st + 2 * TB + 4 * TN);
+      const vec8 f = fr[frag_of<n1, NF>(i)];
       if constexpr (i < n1) s = E::mfma(f, kf[i], s);
       else if constexpr (i < n2) x = E::mfma(f, vf[i - n1], x);
       else if constexpr (i < n3) dv[(i - n2) % TL::DB] = E::mfma(f, pw.operand((i - n2) / TL::DB), dv[(i - n2) % TL::DB]);
@@ -525,8 +552,18 @@ __device__ __forceinline__ void dkv_block(const BwdParams& p, char* lds, int ite
     wa = min(wa, vb);
     wb = max(wa, min(wb, vb));
   }
-  for (int u = 0; u < kStages - 1; ++u) copy_next();
   int g = nt ? u0 / nt : 0, t = ta + (nt ? u0 % nt : 0);
+  // Behind this tile u + 2 is in LDS (every wave has waited for its own copies), and the stage of tile u is free.
+  auto advance = [&](int u) __attribute__((always_inline)) {
+    if (u + kStages - 1 < u1) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(%1)\n\ts_barrier" : : "n"((kStages - 3) * CPW), "n"(0) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    copy_next();
+  };
+  if (u1 > u0) {
+    for (int u = 0; u < kStages - 1; ++u) copy_next();
+    advance(u0 - 1);
+    prime(lds0);
+  }
   // Runs of tiles of one kind, each its own loop: the kinds side by side in one loop cost moves of the
   // accumulators at every tile.
   int u = u0;
@@ -534,15 +571,10 @@ __device__ __forceinline__ void dkv_block(const BwdParams& p, char* lds, int ite
     constexpr int KIND = decltype(kind)::value;        // 0: no row sees a key, 1: some, 2: all
     end = min(end, t + u1 - u);
     for (; t < end; ++t, ++u) {
-      // Behind the barrier tile u + 1 is in LDS as well (every wave has waited for its own copies), and the
-      // stage of tile u - 1 is free.
-      if (u + kStages - 2 < u1) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"((kStages - 3) * CPW) : "memory");
-      else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-      copy_next();
-      const uint32_t st = lds0 + (uint32_t)((u - u0) % kStages * STAGE), next = lds0 + (uint32_t)((u + 1 - u0) % kStages * STAGE);
-      if (u == u0) prime(st);
+      const uint32_t st = lds0 + (uint32_t)(u - u0) % kStages * STAGE, next = lds0 + (uint32_t)(u + 1 - u0) % kStages * STAGE;
       if constexpr (KIND == 0) prime(next);
       else tile(std::integral_constant<bool, KIND == 1>{}, st, next, t * TN, sl2);
+      advance(u);
     }
   };
   while (u < u1) {
@@ -622,21 +654,21 @@ __device__ __forceinline__ void dq_block(const BwdParams& p, char* lds, int item
   const float c = p.c, add = CAP ? start : start * c;
 
   const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_void*)lds;
-  int coff[CB];
-#pragma unroll
-  for (int u = 0; u < CB; ++u) {
-    const int r = (wave * CB + u) * (1024 / (2 * D)) + lane / CPR;
-    coff[u] = (r * D + 8 * ((lane % CPR) ^ swz<D>(r))) * 2;
+  int coff;
+  {
+    const int r = wave * (1024 / (2 * D)) + lane / CPR;
+    coff = (r * D + 8 * ((lane % CPR) ^ swz<D>(r))) * 2;
   }
   const u32x4 rk = resource(reinterpret_cast<const T*>(p.k) + (size_t)unit * p.Lk * D, (unsigned)p.Lk * D * 2);
   const u32x4 rv = resource(reinterpret_cast<const T*>(p.v) + (size_t)unit * p.Lk * D, (unsigned)p.Lk * D * 2);
   auto copy_tile = [&](int t) __attribute__((always_inline)) {
     if (t >= t1) return;
-    const uint32_t dst = lds0 + (uint32_t)((t - t0) % kStages * STAGE);
+    const uint32_t dst = lds0 + (uint32_t)(t - t0) % kStages * STAGE;
 #pragma unroll
     for (int u = 0; u < CB; ++u) {
-      copy16(rk, dst + (uint32_t)((wave * CB + u) * 1024), coff[u] + t * TB);
-      copy16(rv, dst + (uint32_t)(TB + (wave * CB + u) * 1024), coff[u] + t * TB);
+      const int at = coff + here(t * TB + u * (TB / 2));
+      copy16(rk, dst + (uint32_t)((wave + u * kWaves) * 1024), at);
+      copy16(rv, dst + (uint32_t)(TB + (wave + u * kWaves) * 1024), at);
     }
   };
 
@@ -648,10 +680,11 @@ __device__ __forceinline__ void dq_block(const BwdParams& p, char* lds, int item
 
   // A tile's MFMAs as in dkv_block: S (rows of K), dP (rows of V), dQ (dims of K).
   constexpr int n1 = TL::KX, n2 = 2 * TL::KX, NF = 3 * TL::KX;
+  static_assert(frags_apart<n1, NF>(), "an operand is not read into another's place");
   vec8 fr[kFrags];
   auto read = [&](auto ic, uint32_t st, uint32_t next) __attribute__((always_inline)) {
     constexpr int i = decltype(ic)::value;
-    vec8& f = fr[i % kFrags];
+    vec8& f = fr[frag_of<n1, NF>(i)];
     if constexpr (i < n1) f = TL::template rows<i>(st + roff, 0);
     else if constexpr (i < n2) f = TL::template rows<i - n1>(st + roff, TB);
     else if constexpr (i < NF) f = TL::template dims<(i - n2) / TL::DB, (i - n2) % TL::DB>(st + doff, 0);
@@ -701,7 +734,7 @@ __device__ __forceinline__ void dq_block(const BwdParams& p, char* lds, int item
     static_for<NF>([&](auto ic) {
       constexpr int i = decltype(ic)::value;
       read(std::integral_constant<int, i + kAhead>{}, st, next);
-      const vec8 f = fr[i % kFrags];
+      const vec8 f = fr[frag_of<n1, NF>(i)];
       constexpr int per = 8 / TL::KX, lag = TL::KX / 4;
       // What the first half of dQ's MFMAs takes comes before them, the rest beside them.
       if constexpr (i == n2) static_for<4>([&](auto kc) { differ(kc); });
@@ -737,18 +770,24 @@ __device__ __forceinline__ void dq_block(const BwdParams& p, char* lds, int item
   vb = max(va, min(vb, t1));
   wa = min(max(wa, va), vb);
   wb = max(wa, min(wb, vb));
-  for (int u = 0; u < kStages - 1; ++u) copy_tile(t0 + u);
+  auto advance = [&](int t) __attribute__((always_inline)) {     // as in dkv_block
+    if (t + kStages - 1 < t1) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(%1)\n\ts_barrier" : : "n"((kStages - 3) * CPW), "n"(0) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    copy_tile(t + kStages);
+  };
   int t = t0;
+  if (t1 > t0) {
+    for (int u = 0; u < kStages - 1; ++u) copy_tile(t0 + u);
+    advance(t0 - 1);
+    prime(lds0);
+  }
   auto run = [&](auto kind, int end) __attribute__((always_inline)) {
     constexpr int KIND = decltype(kind)::value;        // 0: no row sees a key, 1: some, 2: all
     for (; t < end; ++t) {
-      if (t + kStages - 2 < t1) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"((kStages - 3) * CPW) : "memory");
-      else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-      copy_tile(t + kStages - 1);
-      const uint32_t st = lds0 + (uint32_t)((t - t0) % kStages * STAGE), next = lds0 + (uint32_t)((t + 1 - t0) % kStages * STAGE);
-      if (t == t0) prime(st);
+      const uint32_t st = lds0 + (uint32_t)(t - t0) % kStages * STAGE, next = lds0 + (uint32_t)(t + 1 - t0) % kStages * STAGE;
       if constexpr (KIND == 0) prime(next);
       else tile(std::integral_constant<bool, KIND == 1>{}, st, next, t * TN);
+      advance(t);
     }
   };
   run(std::integral_constant<int, 0>{}, va);
