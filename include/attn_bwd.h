@@ -64,7 +64,9 @@ size_t attn_bwd_workspace_bytes(int B, int Hq, int Hkv, int Lq, int Lk, int D, i
  *              call's kernels end
  *
  * Every tensor of 16-bit values is 16-byte aligned and dO's strides are multiples of
- * 8.  Lq * D * 2, Lk * D * 2 and Lq times dO's row stride in bytes stay below 2^31.
+ * 8.  (Lq + 32) * D * 2, (Lk + 32) * D * 2, Lq + 32 times dO's row stride in bytes and (Lq + 32) * 8 * Hq / Hkv
+ * stay below 2^31.  A product with 0 of an infinity or NaN is NaN: one in a row of Q, K, V or dO reaches the
+ * rows and keys that share a tile of 32 with it, masked from it or not (attn_fwd's O alike).
  * Errors: as attn_fwd_lse; ATTN_ERR_WORKSPACE.
  */
 int attn_bwd(const void* dO, const long long* do_strides, const void* Q, const void* K, const void* V, const void* O,

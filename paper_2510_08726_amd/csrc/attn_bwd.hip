@@ -145,12 +145,12 @@ struct Weights {
   }
 };
 
-// SoftCap of a score x: the exponent of its weight, cap tanh(s / cap) log2 e + add,
-// and the derivative of the cap, 1 - tanh^2 = 4 r (1 - r) with r = 1 / (1 + e^2t).
-__device__ __forceinline__ float capped(float x, const BwdParams& p, float add, float& slope) {
+// SoftCap of a score x: the exponent of its weight, cap tanh(s / cap) log2 e - lse log2 e, where `add` is cap log2 e
+// less the latter, and a quarter of the derivative of the cap: 1 - tanh^2 = 4 r (1 - r) with r = 1 / (1 + e^2t).
+__device__ __forceinline__ float capped(float x, const BwdParams& p, float add, float& quarter) {
   const float r = __builtin_amdgcn_rcpf(1.f + fast_exp2(x * p.cap_k2));
-  slope = 4.f * r * (1.f - r);
-  return __builtin_fmaf(-2.f * p.cap_cl, r, p.cap_cl + add);
+  quarter = __builtin_fmaf(-r, r, r);
+  return __builtin_fmaf(-2.f * p.cap_cl, r, add);
 }
 
 // What item of `n` workgroup g takes: an XCD a contiguous share (workgroup g runs on XCD g mod
@@ -213,7 +213,7 @@ __device__ __forceinline__ int bwd_scale(const BwdParams& p, int unit, float* sh
 // A row's part of its scores and of dP, in tiles of 32 rows: [B Hq, tiles, 64] floats,
 // first what is added to a score before its exponential, (2^15's exponent - lse log2 e - the ALiBi bias of
 // the row within its tile) over the scale, so that it starts the accumulator of Q K^T (with
-// SoftCap: not over the scale); then -delta, which starts that of dO V^T.  fp16: the largest square sums of
+// SoftCap: not over the scale, and with the cap: see capped); then -delta, which starts that of dO V^T.  fp16: the largest square sums of
 // the rows of dO and V in each block of 64.  Rows that see no key (the first Lq - Lk with the causal mask)
 // take no part: their dQ is zero.  One pass over dO and O: bound by memory.
 template <int D, typename T>
@@ -258,6 +258,7 @@ __global__ __launch_bounds__(kThreads) void bwd_rows_kernel(BwdParams p) {
           const float lse = p.lse[(size_t)head * p.Lq + p.row0 + i];
           float e = (is_half<T> ? (float)kShift : 0.f) - lse * kLog2e;
           if (p.cap_cl == 0.f) e = (e - sl2 * (float)(i % TN)) / p.c;
+          else e += p.cap_cl;
           start = lse == kNegInf ? kNegInf : e;
           nd = -dot;
         }
@@ -322,6 +323,9 @@ __device__ __forceinline__ void store(const f32x16 (&acc)[D / 32], float f, T* o
 // share a compute unit's 160 KB.
 constexpr int kStages = 4;
 template <int D> constexpr int kStage = 2 * TN * D * 2 + 256;
+// Operands of V (of KX a wave) that a key block keeps in LDS behind the ring and not in registers, of which a bias or a cap
+// needs more: spilled by the compiler, they came back from memory through waits for the copies of later tiles.
+template <int D, bool MOD> constexpr int kHome = D == 128 && MOD ? 2 : 0;
 // Operands read ahead of their MFMA (LDS takes about four MFMAs' time, and two waves share a SIMD), and the registers of 16
 // bytes a lane that they pass through: kAhead + 1, and one more beside the first product, where the others are short by it
 // of a whole number of turns.
@@ -341,6 +345,14 @@ constexpr bool frags_apart() {
     for (int j = 1; j <= kAhead; ++j)
       if (frag_of<N1, NF>(i) == frag_of<N1, NF>(i + j)) return false;
   return true;
+}
+
+// Where a half of a wave's lanes read what belongs to their rows: an address, computed here, behind which constants are
+// offsets of the loads.
+__device__ __forceinline__ uint32_t stats_at(uint32_t at, int hh) {
+  uint32_t to;
+  asm volatile("v_lshl_add_u32 %0, %1, 4, %2" : "=v"(to) : "v"(hh), "s"(__builtin_amdgcn_readfirstlane((int)at)));
+  return to;
 }
 
 // x as it is, computed here: the compiler otherwise adds the constants behind it before the loop, each into a register
@@ -388,14 +400,18 @@ __device__ __forceinline__ void dkv_block(const BwdParams& p, char* lds, int ite
 
   // K and V of the wave's keys: lane (n, hh) holds key n, dims 16 kx + 8 hh ...  (A negative scale: K
   // negated, which only the scores see.)
-  vec8 kf[TL::KX], vf[TL::KX];
+  constexpr int VL = kHome<D, ALIBI || CAP>;
+  vec8 kf[TL::KX], vf[TL::KX - VL];
+  const uint32_t home = (uint32_t)(uintptr_t)(lds_void*)lds + kStages * STAGE + wave * VL * 1024;
   {
     const T* kg = reinterpret_cast<const T*>(p.k) + ((size_t)unit * p.Lk + krow) * D + 8 * hh;
     const T* vg = reinterpret_cast<const T*>(p.v) + ((size_t)unit * p.Lk + krow) * D + 8 * hh;
 #pragma unroll
     for (int kx = 0; kx < TL::KX; ++kx) {
       kf[kx] = load8(kg + 16 * kx, p.sign);
-      vf[kx] = load8(vg + 16 * kx);
+      const vec8 v = load8(vg + 16 * kx);
+      if (kx < TL::KX - VL) vf[kx] = v;
+      else *(lds_u32x4*)(uintptr_t)(home + (kx - TL::KX + VL) * 1024 + 16 * lane) = __builtin_bit_cast(u32x4, v);
     }
   }
 
@@ -452,20 +468,21 @@ __device__ __forceinline__ void dkv_block(const BwdParams& p, char* lds, int ite
   constexpr int n1 = TL::KX, n2 = 2 * TL::KX, n3 = 3 * TL::KX, NF = 4 * TL::KX;
   static_assert(2 * TL::DB == TL::KX, "as many steps over dims as over rows");
   static_assert(frags_apart<n1, NF>(), "an operand is not read into another's place");
-  vec8 fr[kFrags];
+  vec8 fr[kFrags], vl[VL ? VL : 1];
   f32x16 s, x;
+  // dP's steps begin with those whose V comes from LDS.
+  auto step = [](int j) constexpr { return (j + TL::KX - VL) % TL::KX; };
   auto read = [&](auto ic, uint32_t st, uint32_t next) __attribute__((always_inline)) {
     constexpr int i = decltype(ic)::value;
     vec8& f = fr[frag_of<n1, NF>(i)];
     if constexpr (i < n1) f = TL::template rows<i>(st + roff, 0);
-    else if constexpr (i < n2) f = TL::template rows<i - n1>(st + roff, TB);
+    else if constexpr (i < n2) f = TL::template rows<step(i - n1)>(st + roff, TB);
     else if constexpr (i < n3) f = TL::template dims<(i - n2) / TL::DB, (i - n2) % TL::DB>(st + doff, TB);
     else if constexpr (i < NF) f = TL::template dims<(i - n3) / TL::DB, (i - n3) % TL::DB>(st + doff, 0);
     else f = TL::template rows<i - NF>(next + roff, 0);
   };
   auto starts = [&](f32x16& a, uint32_t at) __attribute__((always_inline)) {
-    uint32_t to;
-    asm volatile("v_lshl_add_u32 %0, %1, 4, %2" : "=v"(to) : "v"(hh), "s"(at));
+    const uint32_t to = stats_at(at, hh);
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
       const f32x4 v = *(lds_f32x4*)(uintptr_t)(to + 32 * g);
@@ -487,13 +504,15 @@ __device__ __forceinline__ void dkv_block(const BwdParams& p, char* lds, int ite
     const int lo = key - off - i0 - 4 * hh, hi = W > 0 ? lo + W : 1 << 30;
     const float bias = ALIBI ? sl2 * (float)(key - off - i0) : 0.f;
     Weights<T> pw, dw;
+    uint32_t sx = 0;
+    if constexpr (CAP) sx = stats_at(st + 2 * TB, hh);
     auto weigh = [&](auto kc) __attribute__((always_inline)) {       // registers 2 k, 2 k + 1
       constexpr int r = 2 * decltype(kc)::value;
       float y[2], f[2];
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         if constexpr (CAP) {
-          const float a = *(lds_float*)(uintptr_t)(st + 2 * TB + 16 * hh + 4 * kconst(r + i));
+          const float a = *(lds_float*)(uintptr_t)(sx + 4 * kconst(r + i));
           y[i] = fast_exp2(capped(s[r + i], p, a, f[i]));
         } else {
           y[i] = fast_exp2(ALIBI ? __builtin_fmaf(s[r + i], c, bias) : s[r + i] * c);
@@ -518,9 +537,18 @@ __device__ __forceinline__ void dkv_block(const BwdParams& p, char* lds, int ite
       constexpr int i = decltype(ic)::value;
       read(std::integral_constant<int, i + kAhead>{}, st, next);
       if constexpr (i == n1 - 2) starts(x, st + 2 * TB + 4 * TN);
+      if constexpr (VL > 0 && i == n1 - 2) {
+        uint32_t to;
+        asm volatile("v_lshl_add_u32 %0, %1, 4, %2" : "=v"(to) : "v"(lane), "s"(home));
+        static_for<VL>([&](auto uc) {
+          constexpr int u = decltype(uc)::value;
+          vl[u] = __builtin_bit_cast(vec8, *(lds_u32x4*)(uintptr_t)(to + u * 1024));
+        });
+      }
       const vec8 f = fr[frag_of<n1, NF>(i)];
       if constexpr (i < n1) s = E::mfma(f, kf[i], s);
-      else if constexpr (i < n2) x = E::mfma(f, vf[i - n1], x);
+      else if constexpr (i < n1 + VL) x = E::mfma(f, vl[i - n1], x);
+      else if constexpr (i < n2) x = E::mfma(f, vf[step(i - n1)], x);
       else if constexpr (i < n3) dv[(i - n2) % TL::DB] = E::mfma(f, pw.operand((i - n2) / TL::DB), dv[(i - n2) % TL::DB]);
       else dk[(i - n3) % TL::DB] = E::mfma(f, dw.operand((i - n3) / TL::DB), dk[(i - n3) % TL::DB]);
       // Pair k of the weights after MFMA n1 + lag + k / per, of dS n MFMAs later.
@@ -596,7 +624,7 @@ __device__ __forceinline__ void dkv_block(const BwdParams& p, char* lds, int ite
   if (key < p.Lk) {
     const size_t to = ((size_t)unit * p.Lk + key) * D;
     float* pk = S > 1 ? p.ws_dkv + (((size_t)unit * p.dkv.pieces + at.piece + part) * 2 * BLK + (key - j0)) * D : nullptr;
-    store<D, T>(dk, __builtin_ldexpf(p.scale, -scale_exp), reinterpret_cast<T*>(p.dk) + to, pk, hh);
+    store<D, T>(dk, __builtin_ldexpf(CAP ? 4.f * p.scale : p.scale, -scale_exp), reinterpret_cast<T*>(p.dk) + to, pk, hh);
     store<D, T>(dv, is_half<T> ? __builtin_ldexpf(1.f, -kShift) : 1.f, reinterpret_cast<T*>(p.dv) + to,
                 pk ? pk + BLK * D : nullptr, hh);
   }
@@ -801,14 +829,14 @@ __device__ __forceinline__ void dq_block(const BwdParams& p, char* lds, int item
     const size_t to = (head * p.Lq + p.row0 + iw + n) * D;
     float* pq = nullptr;
     if (S > 1) pq = p.ws_dq + ((((size_t)unit * ngrp + grp) * p.dq_.pieces + at.piece + part) * BLK + TN * wave + n) * D;
-    store<D, T>(dq, __builtin_ldexpf(p.scale, -scale_exp), reinterpret_cast<T*>(p.dq) + to, pq, hh);
+    store<D, T>(dq, __builtin_ldexpf(CAP ? 4.f * p.scale : p.scale, -scale_exp), reinterpret_cast<T*>(p.dq) + to, pq, hh);
   }
 }
 
 // Both in one launch, the key blocks first: the row blocks fill what they leave free.
 template <int D, typename T, bool CAUSAL, bool ALIBI, bool CAP>
 __global__ __launch_bounds__(kThreads, 2) void bwd_kernel(BwdParams p) {
-  __shared__ __attribute__((aligned(1024))) char lds[kStages * kStage<D>];
+  __shared__ __attribute__((aligned(1024))) char lds[kStages * kStage<D> + kWaves * 1024 * kHome<D, ALIBI || CAP>];
   const int units = p.B * p.Hkv, nk = units * p.dkv.list, gk = p.shares ? (nk + kXcds - 1) / kXcds * kXcds : nk;
   const int g = blockIdx.x;
   if (g < gk) {

@@ -31,7 +31,9 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // Sizes that both passes take: a head's rows are addressed with 32-bit byte offsets.
 bool sizes_ok(int B, int Hq, int Hkv, int Lq, int Lk, int D) {
   if (B < 1 || Hq < 1 || Hkv < 1 || Lq < 1 || Lk < 1 || Hq % Hkv) return false;
-  if ((int64_t)Lq * D * 2 > kMaxInt || (int64_t)Lk * D * 2 > kMaxInt) return false;
+  // (To the end of the last tile, and of the group's rows of 256 bytes a tile.)
+  if (((int64_t)Lq + 32) * D * 2 > kMaxInt || ((int64_t)Lk + 32) * D * 2 > kMaxInt) return false;
+  if (((int64_t)Lq + 32) * 8 * (Hq / Hkv) > kMaxInt) return false;
   return (int64_t)B * Hq <= kMaxInt && (int64_t)B * Hq * Lq <= kMaxElements / D && (int64_t)B * Hkv * Lk <= kMaxElements / D;
 }
 
@@ -237,7 +239,7 @@ int attn_bwd(const void* dO, const long long* do_strides, const void* Q, const v
   for (int i = 0; i < 3; ++i)
     if (do_strides[i] < 0 || do_strides[i] % 8 || do_strides[i] > kMaxElements / n[i]) return ATTN_ERR_SHAPE;
   const long long row = Lq > 1 ? do_strides[2] : D;
-  if (2 * row * Lq > kMaxInt) return ATTN_ERR_SHAPE;
+  if (2 * row * ((int64_t)Lq + 32) > kMaxInt) return ATTN_ERR_SHAPE;
   BwdPlan w = plan(B, Hq, Hkv, Lq, Lk, D, causal != 0, window);
   if (w.groups > kMaxGroups) return ATTN_ERR_SHAPE;
   if (workspace_bytes < w.bytes() || misaligned(workspace)) return ATTN_ERR_WORKSPACE;
