@@ -32,13 +32,14 @@ def attention_grad(do, q, k, v, *, scale, causal=False, alibi_slopes=None, softc
     """o, lse, dq, dk, dv, and the sums of magnitudes behind each gradient, for error bounds:
 
     what a relative error of every P (``dv_abs``) or dS (``dq_abs``, ``dk_abs``) costs at most, and what an absolute
-    error of delta_i of sum_d |do| (|o| + P |v|) costs (``dq_delta``, ``dk_delta``); ``reach`` is the
-    largest sum_d |scale q_d k_d| of a row."""
+    error of delta_i of sum_d |do| (|o| + P |v|) costs (``dq_delta``, ``dk_delta``); what an absolute error of every P
+    costs (``dv_each``) and one of every dS of |do| |v| of the KV head's largest rows (``dq_each``, ``dk_each``); ``reach``
+    is the largest sum_d |scale q_d k_d| of a row."""
     B, Hq, Lq, D = q.shape
     Hkv, Lk = k.shape[1], k.shape[2]
     G = Hq // Hkv
-    r = {n: np.zeros(q.shape) for n in ("o", "o_abs", "dq", "dq_abs", "dq_delta")}
-    r.update({n: np.zeros(k.shape) for n in ("dk", "dk_abs", "dk_delta", "dv", "dv_abs")})
+    r = {n: np.zeros(q.shape) for n in ("o", "o_abs", "dq", "dq_abs", "dq_delta", "dq_each")}
+    r.update({n: np.zeros(k.shape) for n in ("dk", "dk_abs", "dk_delta", "dk_each", "dv", "dv_abs", "dv_each")})
     r["lse"], r["reach"] = np.full(q.shape[:3], -np.inf), np.zeros(q.shape[:3])
     for b in range(B):
         for h in range(Hq):
@@ -64,6 +65,11 @@ def attention_grad(do, q, k, v, *, scale, causal=False, alibi_slopes=None, softc
             r["dk"][b, kh] += dS.T @ qq
             r["dk_abs"][b, kh] += np.abs(dS).T @ np.abs(qq)
             r["dk_delta"][b, kh] += off.T @ np.abs(qq)
+            most = lambda t: np.sqrt((np.where(np.isfinite(t), t, 0.0) ** 2).sum(-1).max())     # noqa: E731
+            size = abs(scale) * most(do[b, kh * G:(kh + 1) * G]) * most(v[b, kh])
+            r["dv_each"][b, kh] += np.abs(g).sum(0)
+            r["dq_each"][b, h] += size * np.abs(kk).sum(0)
+            r["dk_each"][b, kh] += size * np.abs(qq).sum(0)
     return r
 
 

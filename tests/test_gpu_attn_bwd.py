@@ -32,6 +32,8 @@ CASES = [
     (1, 2, 2, 100, 500, 64, True, False, None, 30),         # keys that no row sees
     (1, 16, 1, 40, 70, 128, True, False, None, None),       # sixteen heads share
     (1, 2, 1, 1100, 1100, 128, True, False, None, None),    # long
+    (1, 1, 1, 50, 33100, 64, True, False, None, None),      # over 256 blocks of keys
+    (1, 2, 2, 33100, 50, 128, False, False, None, None),    # over 256 blocks of rows
 ]
 
 

@@ -35,9 +35,12 @@ def bounds(r, dtype, slopes=None, softcap=None, Lk=0):
     formed with lse, three roundings of 2^-24 of |s|, |lse| and the bias; the cap is off by 2^-21 of itself.  A
     weight's relative error is the error of its exponent (e) and 2^-20 for the exponential.  P and dS are rounded once
     (u), o twice (its weights, itself), dS has dP's fp32 sum as well (in e's 2^-18), and the
-    outputs are rounded once.  fp16's smallest outputs are off by half of 2^-24."""
+    outputs are rounded once.  fp16's smallest outputs are off by half of 2^-24, and so are its smallest weights as they are
+    held: P times 2^15, which is 2^-40 of a P, and dS times 2^(14 - e) with 2^(e - 1) <= 2.02 |do| |v| < 2^e of the KV head's
+    largest rows, which is at most 2^-25 2^(e - 14) <= 2^-38 2.02 |do| |v| of a dS."""
     u = torch.finfo(DT[dtype]).eps / 2
     tiny = 2.0 ** -25 if dtype == "f16" else 0.0
+    each_p, each_ds = (2.0 ** -40, 2.0 ** -38 * 2.03) if dtype == "f16" else (0.0, 0.0)
     lse = np.where(np.isfinite(r["lse"]), np.abs(r["lse"]), 0.0)
     bias = 0.0 if slopes is None else float(slopes.max()) * Lk
     e_row = 2.0 ** -20 * r["reach"] + 2.0 ** -22 * (lse + 1.0) + 2.0 ** -22 * bias + (2.0 ** -21 * softcap if softcap else 0.0)
@@ -46,9 +49,9 @@ def bounds(r, dtype, slopes=None, softcap=None, Lk=0):
     return {
         "lse": e_row * 2 + 2.0 ** -20,
         "o": u * np.abs(r["o"]) * 1.01 + off * r["o_abs"] + tiny,
-        "dv": u * np.abs(r["dv"]) * 1.01 + off * r["dv_abs"] + tiny,
-        "dq": u * np.abs(r["dq"]) * 1.01 + (off + e) * r["dq_abs"] + (2 * off + u) * r["dq_delta"] + tiny,
-        "dk": u * np.abs(r["dk"]) * 1.01 + (off + e) * r["dk_abs"] + (2 * off + u) * r["dk_delta"] + tiny,
+        "dv": u * np.abs(r["dv"]) * 1.01 + off * r["dv_abs"] + each_p * r["dv_each"] + tiny,
+        "dq": u * np.abs(r["dq"]) * 1.01 + (off + e) * r["dq_abs"] + (2 * off + u) * r["dq_delta"] + each_ds * r["dq_each"] + tiny,
+        "dk": u * np.abs(r["dk"]) * 1.01 + (off + e) * r["dk_abs"] + (2 * off + u) * r["dk_delta"] + each_ds * r["dk_each"] + tiny,
     }
 
 
