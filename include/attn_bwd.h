@@ -16,9 +16,9 @@
  *
  * Conventions are those of attn.h (layouts, head groups, masks, return codes): device
  * pointers, work on `stream`, argument errors before anything is enqueued, no atomics and
- * so the same bits for the same call.  Sums are held in fp32, and the probabilities
- * and dS go to the matrix unit in the type of Q.  A row that sees no key (causal, Lq >
- * Lk) has O = 0, lse = -inf and dQ = 0, and its dO is not read.  softcap is at most
+ * so the same bits for the same call.  Sums are held in fp32.  The probabilities
+ * and dS go to the matrix unit in the type of Q, for dQ dS as two values of it.  A row that sees no
+ * key (causal, Lq > Lk) has O = 0, lse = -inf and dQ = 0, and its dO is not read.  softcap is at most
  * ATTN_TRAIN_MAX_SOFTCAP: a capped score is off by 2^-22 of the cap, which the backward pass
  * takes into an exponential.
  */

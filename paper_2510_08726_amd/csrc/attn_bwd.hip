@@ -22,7 +22,11 @@
 // layout in which P and dS go into the second products, in registers alone.
 //
 // Rounding.  P and dS go to the matrix unit in the type of Q: 2^-9 (bf16) or 2^-12 (fp16) relative to
-// each, as much as the outputs' own rounding.  Sums are in fp32.  fp16 holds 5
+// each, as much as the outputs' own rounding.  That holds for dV and dK (1.4 times the error that a
+// result rounded once has).  dQ's sums cancel more, since the dS of a row sum to nothing, and
+// with dS rounded once it was off by 1.5 times that error: there dS goes in as two values of the type, the
+// second what the first leaves (1.00 times, for an eighth more time: 32 heads of 8192 causal rows 1856 us in
+// place of 1649).  Sums are in fp32.  fp16 holds 5
 // exponent bits, and both get small in long rows (dS also with the loss's scale), so there P is
 // held times 2^15 and dS times a power of two from a bound on |dO| |V| of its KV head
 // (bwd_scale), taken out of the fp32 sums at the end.
@@ -140,6 +144,11 @@ template <typename T>
 struct Weights {
   uint32_t w[2][4];
   __device__ __forceinline__ void set(int r, float a, float b) { w[r / 8][(r % 8) / 2] = Elem<T>::pack2(a, b); }
+  // What that leaves of a and b.
+  __device__ __forceinline__ void rest(const Weights& of, int r, float a, float b) {
+    const uint32_t u = of.w[r / 8][(r % 8) / 2];
+    set(r, a - Elem<T>::lo(u), b - Elem<T>::hi(u));
+  }
   __device__ __forceinline__ typename Elem<T>::vec8 operand(int c16) const {
     return __builtin_bit_cast(typename Elem<T>::vec8, make_uint4(w[c16][0], w[c16][1], w[c16][2], w[c16][3]));
   }
@@ -324,8 +333,10 @@ __device__ __forceinline__ void store(const f32x16 (&acc)[D / 32], float f, T* o
 constexpr int kStages = 4;
 template <int D> constexpr int kStage = 2 * TN * D * 2 + 256;
 // Operands of V (of KX a wave) that a key block keeps in LDS behind the ring and not in registers, of which a bias or a cap
-// needs more: spilled by the compiler, they came back from memory through waits for the copies of later tiles.
-template <int D, bool MOD> constexpr int kHome = D == 128 && MOD ? 2 : 0;
+// needs more, and fp16's factor of dS one: spilled by the compiler, they came back from memory through waits for the copies
+// of later tiles (what the one more costs and saves came out even, 268 us either way at 32 / 16 heads of 3001 rows on 4099 keys
+// with a cap).
+template <int D, typename T, bool MOD> constexpr int kHome = D == 128 ? (MOD ? 2 : 0) + (is_half<T> ? 1 : 0) : 0;
 // Operands read ahead of their MFMA (LDS takes about four MFMAs' time, and two waves share a SIMD), and the registers of 16
 // bytes a lane that they pass through: kAhead + 1, and one more beside the first product, where the others are short by it
 // of a whole number of turns.
@@ -400,7 +411,7 @@ __device__ __forceinline__ void dkv_block(const BwdParams& p, char* lds, int ite
 
   // K and V of the wave's keys: lane (n, hh) holds key n, dims 16 kx + 8 hh ...  (A negative scale: K
   // negated, which only the scores see.)
-  constexpr int VL = kHome<D, ALIBI || CAP>;
+  constexpr int VL = kHome<D, T, ALIBI || CAP>;
   vec8 kf[TL::KX], vf[TL::KX - VL];
   const uint32_t home = (uint32_t)(uintptr_t)(lds_void*)lds + kStages * STAGE + wave * VL * 1024;
   {
@@ -731,7 +742,7 @@ __device__ __forceinline__ void dq_block(const BwdParams& p, char* lds, int item
     hi -= j0 + 4 * hh;
     lo -= j0 + 4 * hh;
     const float base = ALIBI ? __builtin_fmaf(sl2, (float)(j0 + 4 * hh - iw - off), add) : add;
-    Weights<T> w;
+    Weights<T> w, rest;
     auto weigh = [&](auto kc) __attribute__((always_inline)) {       // registers 2 k, 2 k + 1
       constexpr int r = 2 * decltype(kc)::value;
 #pragma unroll
@@ -758,6 +769,7 @@ __device__ __forceinline__ void dq_block(const BwdParams& p, char* lds, int item
         if (MASKED && (k > hi || k <= lo)) y[i] = 0.f;
       }
       w.set(r, y[0], y[1]);
+      rest.rest(w, r, y[0], y[1]);
     };
     static_for<NF>([&](auto ic) {
       constexpr int i = decltype(ic)::value;
@@ -768,7 +780,11 @@ __device__ __forceinline__ void dq_block(const BwdParams& p, char* lds, int item
       if constexpr (i == n2) static_for<4>([&](auto kc) { differ(kc); });
       if constexpr (i < n1) s = E::mfma(f, qf[i], s);
       else if constexpr (i < n2) x = E::mfma(f, gf[i - n1], x);
-      else dq[(i - n2) % TL::DB] = E::mfma(f, w.operand((i - n2) / TL::DB), dq[(i - n2) % TL::DB]);
+      else {
+        constexpr int c16 = (i - n2) / TL::DB, db = (i - n2) % TL::DB;
+        dq[db] = E::mfma(f, w.operand(c16), dq[db]);
+        dq[db] = E::mfma(f, rest.operand(c16), dq[db]);
+      }
       // The exponentials beside dP, the last ones in its last place.
       static_for<per>([&](auto uc) {
         constexpr int k = (i - n1 - lag) * per + decltype(uc)::value;
@@ -836,7 +852,7 @@ __device__ __forceinline__ void dq_block(const BwdParams& p, char* lds, int item
 // Both in one launch, the key blocks first: the row blocks fill what they leave free.
 template <int D, typename T, bool CAUSAL, bool ALIBI, bool CAP>
 __global__ __launch_bounds__(kThreads, 2) void bwd_kernel(BwdParams p) {
-  __shared__ __attribute__((aligned(1024))) char lds[kStages * kStage<D> + kWaves * 1024 * kHome<D, ALIBI || CAP>];
+  __shared__ __attribute__((aligned(1024))) char lds[kStages * kStage<D> + kWaves * 1024 * kHome<D, T, ALIBI || CAP>];
   const int units = p.B * p.Hkv, nk = units * p.dkv.list, gk = p.shares ? (nk + kXcds - 1) / kXcds * kXcds : nk;
   const int g = blockIdx.x;
   if (g < gk) {

@@ -117,18 +117,16 @@ BwdPlan plan(int B, int Hq, int Hkv, int Lq, int Lk, int D, bool causal, int win
   const int64_t units = (int64_t)B * Hkv, heads = (int64_t)B * Hq;
   p.shares = units % 8 == 0;
   const int bm = attn::bwd_block_keys() / p.hg, nkb = (int)ceil_div(Lk, attn::bwd_block_keys()), nqb = (int)ceil_div(p.rows, bm);
-  // A tile of a key block is 4 products of 32 x 32 x D a wave, one of a row block 3: the whole call's tiles, for each
-  // workgroup that runs at a time.
+  // The whole call's tiles (either side's are 4 products of 32 x 32 x D a wave), for each workgroup that runs at a time.
   double all = 0.0;
-  for (int i = 0; i < nkb; ++i) all += 4.0 * p.group * query_tiles(p, i);
-  for (int i = 0; i < nqb; ++i) all += 3.0 * (p.group / p.hg) * key_tiles(p, i);
+  for (int i = 0; i < nkb; ++i) all += (double)p.group * query_tiles(p, i);
+  for (int i = 0; i < nqb; ++i) all += (double)(p.group / p.hg) * key_tiles(p, i);
   // A longer block would be the last to end, and is divided.  Three quarters of an even share: 2 x 32 / 8 heads of 2048 rows
-  // (causal) take 297 us, 304 with half of it, 346 with all, 485 undivided; 40 / 2 heads 192, 219, 239 and 2420; 128 rows
-  // of 32 / 8 heads on 8192 keys 99, 96, 92 and 226.  At least 8 tiles: 8 heads of 1024 rows 41 us, 46 with 4, 49 with 16, 58
-  // undivided.
-  const double each = 0.75 * all * units / (2.0 * attn::compute_units());
-  divide(p.dkv, nkb, std::max(each / 4, 8.0), [&](int i) { return p.group * query_tiles(p, i); });
-  divide(p.dq_, nqb, std::max(each / 3, 8.0), [&](int i) { return key_tiles(p, i); });
+  // (causal) take 283 us, 290 with half of it, 280 with all; 40 / 2 heads 181, 194 and 197; 128 rows of 32 / 8 heads on
+  // 8192 keys 92, 100 and 101.  At least 8 tiles: 8 heads of 1024 rows 39 us, with 4 and 16 a tenth to a fifth more.
+  const double share = std::max(0.75 * all * units / (2.0 * attn::compute_units()), 8.0);
+  divide(p.dkv, nkb, share, [&](int i) { return p.group * query_tiles(p, i); });
+  divide(p.dq_, nqb, share, [&](int i) { return key_tiles(p, i); });
   const auto floats = [](int64_t n) { return (n + 63) / 64 * 64; };
   r.stats = floats(heads * p.row_tiles * 64);
   r.peaks = floats(heads * p.row_blocks + units * p.key_blocks);
