@@ -251,6 +251,100 @@ __device__ __forceinline__ uint2 codes8(const double (&z)[8], bool int8) {
 
 struct __attribute__((packed, aligned(1))) Bytes8 { uint2 v; };
 
+// A row of a matrix as its lanes load and store it: chunk i begins 8 i elements behind the multiple of 8 at or before the
+// row, and what a lane does not have, or a row that is not there, needs no branch: the buffer resource ends with the row,
+// loads behind it give zeros, and stores are dropped.  Under branches the compiler's waits could not count what is on its
+// way, and would wait for all of it, the next rows' words and the stores among them.
+template <typename T, bool ODD>
+struct Row {
+  static constexpr int S = sizeof(T);
+  static constexpr int kNowhere = 1 << 30;       // an offset behind any row
+  char* base;
+  int bytes;
+  // The row from element `index` of the matrix on, `shift` behind a multiple of 8.  M = 0: none.
+  __device__ __forceinline__ Row(const void* ptr, int64_t index, int shift, int M)
+      : base(reinterpret_cast<char*>(const_cast<void*>(ptr)) + (index - shift) * S), bytes(ptr && M > 0 ? (shift + M) * S : 0) {}
+  __device__ __forceinline__ __amdgpu_buffer_rsrc_t until(int n) const {
+    return __builtin_amdgcn_make_buffer_rsrc(base, 0, n, 0x00027000);
+  }
+
+  // Half a word at the row's end is no word of its own: last() has it.
+  __device__ __forceinline__ Raw<T> load(int i) const {
+    const __amdgpu_buffer_rsrc_t row = until(bytes & ~3);
+    Raw<T> r;
+#pragma unroll
+    for (int k = 0; k < Raw<T>::W; ++k) r.w[k] = __builtin_amdgcn_raw_buffer_load_b128(row, 8 * S * i + 16 * k, 0, 0);
+    return r;
+  }
+  __device__ __forceinline__ unsigned last() const {
+    if constexpr (!ODD || S == 4) return 0u;
+    else return (unsigned short)__builtin_amdgcn_raw_buffer_load_b16(until(bytes), bytes ? bytes - S : 0, 0, 0);
+  }
+
+  // Chunk i, rounded to T: a whole one at once, of part of a row at most 4, 2 and 1 elements, in as many stores for
+  // every lane.
+  __device__ __forceinline__ void store(int i, const Chunk<ODD>& c, const float (&x)[8]) const {
+    const __amdgpu_buffer_rsrc_t row = until(bytes);
+    const int at = 8 * S * i;
+    words<8>(row, c.whole() ? at : kNowhere, x);
+    if constexpr (ODD) {
+      float y[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) y[k] = x[k];
+      const int n = c.part() ? max(c.hi - c.lo, 0) : 0;
+      if (n > 0) {                               // the row's elements to the front
+#pragma unroll
+        for (int b = 1; b < 8; b *= 2)
+          if (c.lo & b) {
+#pragma unroll
+            for (int k = 0; k + b < 8; ++k) y[k] = y[k + b];
+          }
+      }
+      const int from = at + S * c.lo;
+      words<4>(row, n & 4 ? from : kNowhere, y);
+      const float two[2] = {n & 4 ? y[4] : y[0], n & 4 ? y[5] : y[1]};
+      words<2>(row, n & 2 ? from + S * (n & 4) : kNowhere, two);
+      const float one[1] = {n & 4 ? n & 2 ? y[6] : y[4] : n & 2 ? y[2] : y[0]};
+      words<1>(row, n & 1 ? from + S * (n & 6) : kNowhere, one);
+    }
+  }
+  template <int N, int K>
+  static __device__ __forceinline__ void words(__amdgpu_buffer_rsrc_t row, int at, const float (&x)[K]) {
+    unsigned w[N * S / 4 + 1];
+    if constexpr (S == 4) {
+#pragma unroll
+      for (int k = 0; k < N; ++k) w[k] = __builtin_bit_cast(unsigned, x[k]);
+    } else {
+#pragma unroll
+      for (int k = 0; k < N; k += 2) w[k / 2] = Elem<T>::pack2(x[k], x[k + 1 < N ? k + 1 : k]);
+    }
+    typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+    if constexpr (N * S >= 16) {
+#pragma unroll
+      for (int k = 0; k < N * S / 16; ++k)
+        __builtin_amdgcn_raw_buffer_store_b128(u32x4{w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]}, row, at + 16 * k, 0, 0);
+    } else if constexpr (N * S == 8) {
+      __builtin_amdgcn_raw_buffer_store_b64(u32x2{w[0], w[1]}, row, at, 0, 0);
+    } else if constexpr (N * S == 4) {
+      __builtin_amdgcn_raw_buffer_store_b32(w[0], row, at, 0, 0);
+    } else {
+      __builtin_amdgcn_raw_buffer_store_b16((unsigned short)w[0], row, at, 0, 0);
+    }
+  }
+};
+
+// The values of a chunk as Row loads it, with the row's last element, of a row that ends at column M.
+template <typename T, bool ODD>
+__device__ __forceinline__ void values(const Raw<T>& r, unsigned last, int M, const Chunk<ODD>& c, float (&x)[8]) {
+  values(r, c, x);
+  if constexpr (ODD && sizeof(T) == 2) {
+    if (c.part() && c.lo < c.hi && c.col + c.hi == M) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = i == c.hi - 1 ? Elem<T>::lo(last) : x[i];
+    }
+  }
+}
+
 // The rows that a lane's place in its workgroup takes: from `first` in steps of `step`, those below `last`.  (A run
 // of rows for each XCD instead, so that the words which two rows share pass through one L2, was 3 to 10 % slower, rows
 // of 5119 among them.)
@@ -415,60 +509,67 @@ __global__ __launch_bounds__(kMaxThreads) void rmsnorm_add_kernel(RmsnormParams 
 }
 
 // Gradients.  A workgroup takes rows in turn, and its lanes keep the sum of dY n of their columns over
-// them: [workgroups, M] in fp32, summed by rmsnorm_dweight_kernel in a fixed order.  The next row's words are on their
-// way while a row is worked on.
+// them: [workgroups, M] in fp32, summed by rmsnorm_dweight_kernel in a fixed order.  Two rows of words are on their way while
+// one is worked on (one, in more steps of a lane): 8192 rows of 5120 in bf16 take 66 us, 5.1 TB/s in and out as a
+// large copy has, 87 with one ahead.  8191 of 5119 take 85; 98 with branches at the rows' ends in place of Row.
 template <typename T, typename R, int C, bool ODD>
 __global__ __launch_bounds__(kMaxThreads) void rmsnorm_add_bwd_kernel(RmsnormBwdParams p) {
-  constexpr bool AHEAD = C == 1;               // (more steps have no registers for it)
   __shared__ float sums[2][kMaxWaves];
   __shared__ float joined[C == 1 ? 2048 : 1];      // rpb rows of at most 64 or 128 lanes
   const int lanes = p.lanes, rpb = blockDim.x / lanes;
-  const int sub = threadIdx.x / lanes, t = threadIdx.x % lanes;
+  const int sub = __builtin_amdgcn_readfirstlane(threadIdx.x / lanes), t = threadIdx.x % lanes;
   const int M = p.M;
-  const int64_t end = (int64_t)p.N * M;
   const Turns turns = turns_of(p.N, rpb, sub);
   const int shift = ODD ? (int)(turns.first * M & 7) : 0;       // of all its rows: a lane's columns stay the same
   auto chunk = [&](int c, bool in) __attribute__((always_inline)) { return chunk_of<ODD>(c * lanes + t, shift, in ? M : 0); };
   float dw[C][8];
+  Raw<T> weight[C];
 #pragma unroll
-  for (int c = 0; c < C; ++c)
+  for (int c = 0; c < C; ++c) {
+    const auto k = chunk(c, true);
+    if (p.weight) weight[c] = load<T>(p.weight, k.col, M, k);
 #pragma unroll
     for (int i = 0; i < 8; ++i) dw[c][i] = 0.f;
+  }
   struct Words {
     Raw<T> dy[C];
     Raw<R> h[C], dh[C];
+    unsigned dy_last, h_last, dh_last;
     float rstd;
   };
   auto fetch = [&](int64_t row, Words& w) __attribute__((always_inline)) {
-    const bool in = row < turns.last;
-    const int64_t base = (in ? row : 0) * M;
+    const int m = row < turns.last ? M : 0;
+    const Row<T, ODD> dy(p.dy, row * M, shift, m);
+    const Row<R, ODD> h(p.h, row * M, shift, m);
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      const auto k = chunk(c, in);
-      w.dy[c] = load<T>(p.dy, base + k.col, end, k);
-      w.h[c] = load<R>(p.h, base + k.col, end, k);
-      if (p.dh) w.dh[c] = load<R>(p.dh, base + k.col, end, k);
+      w.dy[c] = dy.load(c * lanes + t);
+      w.h[c] = h.load(c * lanes + t);
     }
-    w.rstd = in ? p.rstd[row] : 0.f;
+    w.dy_last = dy.last();
+    w.h_last = h.last();
+    w.rstd = p.rstd[min(row, turns.last - 1)];
   };
-  Words now, next;
-  fetch(turns.first, now);
+  auto fetch_dh = [&](int64_t row, Words& w) __attribute__((always_inline)) {
+    const Row<R, ODD> dh(p.dh, row * M, shift, row < turns.last ? M : 0);
+#pragma unroll
+    for (int c = 0; c < C; ++c) w.dh[c] = dh.load(c * lanes + t);
+    w.dh_last = dh.last();
+  };
   int turn = 0;
-  for (int64_t row = turns.first; row - sub < turns.last; row += turns.step, turn ^= 1) {
+  // One row.  As its words are taken apart, those of the row `ahead` take their place.
+  auto one = [&](int64_t row, int64_t ahead, Words& now) __attribute__((always_inline)) {
     const bool in = row < turns.last;
-    const int64_t base = (in ? row : 0) * M;
-    const bool more = row - sub + turns.step < turns.last;
-    if (AHEAD && more) fetch(row + turns.step, next);
-    const float r = now.rstd;
+    const float r = in ? now.rstd : 0.f;
     float g[C][8], n[C][8];
     float s = 0.f;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
       const auto k = chunk(c, in);
       float w[8];
-      values(now.dy[c], k, g[c]);
-      values(now.h[c], k, n[c]);
-      if (p.weight) get8<T>(p.weight, k.col, M, k, w);
+      values(now.dy[c], now.dy_last, M, k, g[c]);
+      values(now.h[c], now.h_last, M, k, n[c]);
+      values(weight[c], k, w);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         n[c][i] *= r;
@@ -477,22 +578,42 @@ __global__ __launch_bounds__(kMaxThreads) void rmsnorm_add_bwd_kernel(RmsnormBwd
         s = __builtin_fmaf(g[c][i], n[c][i], s);
       }
     }
+    fetch(ahead, now);
     s = join_row<Sum>(s, lanes, sums[turn]) / (float)M;
+    turn ^= 1;
+    const Row<R, ODD> dresidual(p.dresidual, row * M, shift, in ? M : 0);
+    const Row<T, ODD> dx(p.dx, row * M, shift, in ? M : 0);
 #pragma unroll
     for (int c = 0; c < C; ++c) {
       const auto k = chunk(c, in);
       float d[8];
-      if (p.dh) values(now.dh[c], k, d);
+      values(now.dh[c], now.dh_last, M, k, d);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const float x = r * __builtin_fmaf(-n[c][i], s, g[c][i]);
         d[i] = p.dh ? d[i] + x : x;
       }
-      if (p.dresidual) put8<R>(p.dresidual, base + k.col, k, d);
-      put8<T>(p.dx, base + k.col, k, d);
+      dresidual.store(c * lanes + t, k, d);
+      dx.store(c * lanes + t, k, d);
     }
-    if (AHEAD) now = next;
-    else if (more) fetch(row + turns.step, now);
+    fetch_dh(ahead, now);
+  };
+  Words a, b;
+  int64_t row = turns.first;
+  fetch(row, a);
+  fetch_dh(row, a);
+  if constexpr (C == 1) {
+    // (In this order, for the waits that the loop begins with.)
+    __builtin_amdgcn_sched_barrier(0);
+    fetch(row + turns.step, b);
+    fetch_dh(row + turns.step, b);
+    __builtin_amdgcn_sched_barrier(0);
+    for (; row - sub < turns.last; row += 2 * turns.step) {
+      one(row, row + 2 * turns.step, a);
+      one(row + turns.step, row + 3 * turns.step, b);        // (or none, without a branch)
+    }
+  } else {
+    for (; row - sub < turns.last; row += turns.step) one(row, row + turns.step, a);
   }
   if (!p.ws) return;
   float* at = p.ws + (int64_t)blockIdx.x * M;
@@ -608,11 +729,10 @@ int rows_per_block(const Split& s) { return s.lanes == 64 ? 4 : s.lanes == 128 ?
 
 constexpr int64_t kMaxBlocks = 1 << 20;      // (more rows are taken in turn)
 
-// Workgroups that take rows in turn: as many as 256 compute units hold at a time (20 waves each), a
-// multiple of 8.  (Each is a partial of dweight.)
-int64_t resident(const Split& s) {
+// Workgroups that take rows in turn: as many as 256 compute units hold at a time with `hold` waves each, a multiple of 8.
+int64_t resident(const Split& s, int hold) {
   const int waves = s.lanes * rows_per_block(s) / 64;
-  return 256 * std::max(20 / waves, 1);
+  return 256 * std::max(hold / waves, 1);
 }
 
 }  // namespace
@@ -620,7 +740,8 @@ int64_t resident(const Split& s) {
 int64_t rmsnorm_bwd_partials(int64_t N, int M) {
   const Split s = split(M);
   const int rpb = rows_per_block(s);
-  return std::min((N + rpb - 1) / rpb, resident(s));
+  // 8 waves, or one workgroup: 16384 rows of 4096 100 us (109 with 16), of 1024 29 (34; 34 with 6).
+  return std::min((N + rpb - 1) / rpb, resident(s, 8));
 }
 
 hipError_t launch_rmsnorm_add(const RmsnormParams& p, hipStream_t stream) {
@@ -630,7 +751,7 @@ hipError_t launch_rmsnorm_add(const RmsnormParams& p, hipStream_t stream) {
   q.inv = 1.0 / p.M;
   const int rpb = rows_per_block(s);
   const bool turns = s.steps == 1 && p.M % 8 == 0;
-  const dim3 grid((unsigned)std::min(((int64_t)p.N + rpb - 1) / rpb, turns ? resident(s) : kMaxBlocks)), block(s.lanes * rpb);
+  const dim3 grid((unsigned)std::min(((int64_t)p.N + rpb - 1) / rpb, turns ? resident(s, 20) : kMaxBlocks)), block(s.lanes * rpb);
   with_types(p.dtype, p.wide, [&](auto t, auto r) {
     typedef decltype(t) T;
     typedef decltype(r) R;
