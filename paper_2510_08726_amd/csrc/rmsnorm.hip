@@ -86,11 +86,6 @@ __device__ __forceinline__ void values(const Raw<T>& r, const Chunk<ODD>& c, flo
   }
 }
 
-template <typename T, bool ODD>
-__device__ __forceinline__ void get8(const void* p, int64_t at, int64_t end, const Chunk<ODD>& c, float (&x)[8]) {
-  values<T>(load<T>(p, at, end, c), c, x);
-}
-
 // The chunk's values, rounded to T.
 template <typename T, bool ODD>
 __device__ __forceinline__ void put8(void* ptr, int64_t index, const Chunk<ODD>& c, const float (&x)[8]) {
@@ -308,6 +303,23 @@ struct Row {
       words<1>(row, n & 1 ? from + S * (n & 6) : kNowhere, one);
     }
   }
+  // 8 codes.
+  __device__ __forceinline__ void store(int i, const Chunk<ODD>& c, uint2 codes) const {
+    const __amdgpu_buffer_rsrc_t row = until(bytes);
+    typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+    __builtin_amdgcn_raw_buffer_store_b64(u32x2{codes.x, codes.y}, row, c.whole() ? 8 * i : kNowhere, 0, 0);
+    if constexpr (ODD) {
+      const int n = c.part() ? max(c.hi - c.lo, 0) : 0, from = 8 * i + c.lo;
+      const uint64_t w = ((uint64_t)codes.y << 32 | codes.x) >> (8 * (c.lo & 7));
+      __builtin_amdgcn_raw_buffer_store_b32((unsigned)w, row, n & 4 ? from : kNowhere, 0, 0);
+      __builtin_amdgcn_raw_buffer_store_b16((unsigned short)(w >> (8 * (n & 4))), row, n & 2 ? from + (n & 4) : kNowhere, 0, 0);
+      __builtin_amdgcn_raw_buffer_store_b8((unsigned char)(w >> (8 * (n & 6))), row, n & 1 ? from + (n & 6) : kNowhere, 0, 0);
+    }
+  }
+  // One element; i < 0: none.
+  __device__ __forceinline__ void put(int i, float x) const {
+    __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, x), until(bytes), i < 0 ? kNowhere : S * i, 0, 0);
+  }
   template <int N, int K>
   static __device__ __forceinline__ void words(__amdgpu_buffer_rsrc_t row, int at, const float (&x)[K]) {
     unsigned w[N * S / 4 + 1];
@@ -355,63 +367,70 @@ __device__ __forceinline__ Turns turns_of(int64_t N, int rpb, int sub) {
   return {(int64_t)blockIdx.x * rpb + sub, (int64_t)gridDim.x * rpb, N};
 }
 
-// T: the type of x, the weight and y; R: that of the residual and h.  C: steps of 8 elements a
-// lane.  QUANT: y in 8 bits.  A workgroup takes rows in turn, the next row's words on their way while one is worked on, in
-// one step and without ODD.  (More steps have no registers for it.  With ODD the stores are conditional, and the wait for the
-// next row's words is one for the stores behind them too: 8191 rows of 5119 take 131 us in turns, 101 with a workgroup each.)
+// T: the type of x, the weight and y; R: that of the residual and h.  C: steps of 8 elements a lane.  QUANT: y in 8 bits.  A
+// workgroup takes rows in turn, the words of two rows on their way while one is worked on (of one in more steps: of none until
+// that one's are stored where QUANT leaves no registers, 4096 rows of 16384 with a scale each 163 us, 206 spilled).  8192 rows
+// of 5120 in bf16 take 62 us, 5.4 TB/s in and out (a large copy 5.1), 8191 of 5119 76, 101 with branches at the rows' ends;
+// to 8 bits, 8192 of 8192 93 us with a scale for each 128, 120 with one row ahead.  That is bound by
+// fp64 (the codes are those of the exact quotients), and a scale a row by taking h through it twice: 129.
 template <typename T, typename R, int C, bool QUANT, bool ODD>
 __global__ __launch_bounds__(kMaxThreads) void rmsnorm_add_kernel(RmsnormParams p) {
-  constexpr bool AHEAD = C == 1 && !ODD;
+  constexpr bool LATE = QUANT && C > 1;          // (no registers for it beside the fp64 values)
   __shared__ double sums[2][kMaxWaves];
   __shared__ double tops[2][kMaxWaves];
   const int lanes = p.lanes, rpb = blockDim.x / lanes;
-  const int sub = threadIdx.x / lanes, t = threadIdx.x % lanes;
+  const int sub = __builtin_amdgcn_readfirstlane(threadIdx.x / lanes), t = threadIdx.x % lanes;
   const int M = p.M;
-  const int64_t end = (int64_t)p.N * M;
   const Turns turns = turns_of(p.N, rpb, sub);
-  // (Groups begin at a chunk's first element.)
-  auto shift_of = [&](int64_t row) __attribute__((always_inline)) { return !ODD || (QUANT && p.group) ? 0 : (int)(row * M & 7); };
+  // Of all its rows: a lane's columns stay the same.  (Groups begin at a chunk's first element.)
+  const int shift = !ODD || (QUANT && p.group) ? 0 : (int)(turns.first * M & 7);
+  Raw<T> weight[C];
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    const auto k = chunk_of<ODD>(c * lanes + t, shift, M);
+    if (p.weight) weight[c] = load<T>(p.weight, k.col, M, k);
+  }
   struct Words {
     Raw<T> x[C];
     Raw<R> r[C];
+    unsigned x_last, r_last;
   };
   auto fetch = [&](int64_t row, Words& w) __attribute__((always_inline)) {
-    const bool in = row < turns.last;
-    const int64_t base = (in ? row : 0) * M;
-    const int shift = shift_of(row);
+    const int m = row < turns.last ? M : 0;
+    const Row<T, ODD> x(p.x, row * M, shift, m);
+    const Row<R, ODD> r(p.residual, row * M, shift, m);
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      const auto k = chunk_of<ODD>(c * lanes + t, shift, in ? M : 0);
-      w.x[c] = load<T>(p.x, base + k.col, end, k);
-      if (p.residual) w.r[c] = load<R>(p.residual, base + k.col, end, k);
+      w.x[c] = x.load(c * lanes + t);
+      w.r[c] = r.load(c * lanes + t);
     }
+    w.x_last = x.last();
+    w.r_last = r.last();
   };
-  Words now, next;
   int turn = 0;
-  fetch(turns.first, now);
-  // (All rows of a workgroup take as many turns as its first.)
-  for (int64_t row = turns.first; row - sub < turns.last; row += turns.step, turn ^= 1) {
-    const bool in = row < turns.last;
-    const int m = in ? M : 0;
-    const int64_t base = (in ? row : 0) * M;
-    const int shift = shift_of(row);
+  // One row.  As its words are taken apart, those of the row `ahead` take their place.
+  auto one = [&](int64_t row, int64_t ahead, Words& now) __attribute__((always_inline)) {
+    const int m = row < turns.last ? M : 0;
     auto chunk = [&](int c) __attribute__((always_inline)) { return chunk_of<ODD>(c * lanes + t, shift, m); };
-    const bool more = row - sub + turns.step < turns.last;
-    if (AHEAD && more) fetch(row + turns.step, next);
     float h[C][8];
     double ss = 0.0;
+    const Row<R, ODD> stream(p.residual ? p.h : nullptr, row * M, shift, m);
 #pragma unroll
     for (int c = 0; c < C; ++c) {
       const auto k = chunk(c);
-      values(now.x[c], k, h[c]);
+      float y[8];
+      values(now.x[c], now.x_last, M, k, h[c]);
+      values(now.r[c], now.r_last, M, k, y);
       if (p.residual) {
-        float y[8];
-        values(now.r[c], k, y);
 #pragma unroll
         for (int i = 0; i < 8; ++i) h[c][i] += y[i];
-        put8<R>(p.h, base + k.col, k, h[c]);
-        round8<R>(h[c]);
       }
+    }
+    if constexpr (!LATE) fetch(ahead, now);
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      stream.store(c * lanes + t, chunk(c), h[c]);
+      if (p.residual) round8<R>(h[c]);
     }
 #pragma unroll
     for (int c = 0; c < C; ++c)
@@ -419,17 +438,19 @@ __global__ __launch_bounds__(kMaxThreads) void rmsnorm_add_kernel(RmsnormParams 
       for (int i = 0; i < 8; ++i) ss = __builtin_fma((double)h[c][i], (double)h[c][i], ss);
     ss = join_row<Sum>(ss, lanes, sums[turn]);
     const double rstd = inverse_root(__builtin_fma(ss, p.inv, p.eps));
-    if (p.rstd && in && t == 0) p.rstd[row] = (float)rstd;
+    Row<float, false>(p.rstd, row, 0, m ? 1 : 0).put(t == 0 ? 0 : -1, (float)rstd);
+    turn ^= 1;                                   // (of the tops behind it too)
     if constexpr (!QUANT) {
       const float r = (float)rstd;
+      const Row<T, ODD> out(p.y, row * M, shift, m);
 #pragma unroll
       for (int c = 0; c < C; ++c) {
         const auto k = chunk(c);
         float w[8], y[8];
-        if (p.weight) get8<T>(p.weight, k.col, M, k, w);
+        values(weight[c], k, w);
 #pragma unroll
         for (int i = 0; i < 8; ++i) y[i] = p.weight ? h[c][i] * r * (w[i] + p.offset) : h[c][i] * r;
-        put8<T>(p.y, base + k.col, k, y);
+        out.store(c * lanes + t, k, y);
       }
     } else {
       const double unit = p.int8 ? rstd * (1.0 / 127.0) : rstd * (1.0 / 448.0);
@@ -437,7 +458,7 @@ __global__ __launch_bounds__(kMaxThreads) void rmsnorm_add_kernel(RmsnormParams 
       auto weighed = [&](int c, double (&z)[8]) __attribute__((always_inline)) {    // h (w + offset)
         float w[8];
         if (p.weight) {
-          get8<T>(p.weight, chunk(c).col, M, chunk(c), w);
+          values(weight[c], chunk(c), w);
 #pragma unroll
           for (int i = 0; i < 8; ++i) z[i] = (double)h[c][i] * ((double)w[i] + (double)p.offset);
         } else {
@@ -456,24 +477,21 @@ __global__ __launch_bounds__(kMaxThreads) void rmsnorm_add_kernel(RmsnormParams 
         return __builtin_fabs(a + bad);
       };
       // rstd over the scale of a group whose largest |h (w + offset)| is a; 0 where its codes are zeros.
-      auto scaled = [&](double a, int64_t at, bool writes) __attribute__((always_inline)) {
+      const Row<float, false> scales(p.scales, row * p.groups, 0, m ? p.groups : 0);
+      auto scaled = [&](double a, int at) __attribute__((always_inline)) {
         float s = (float)(a * unit);
         const bool fine = s <= 3.4028234663852886e38f;     // (not an infinity or NaN)
         if (!fine) s = __builtin_nanf("");
-        if (writes) p.scales[at] = s;
+        scales.put(at, s);
         return fine && s > 0.f ? rstd * inverse((double)s) : 0.0;
       };
+      const Row<unsigned char, ODD> codes(p.y, row * M, shift, m);
       auto put = [&](int c, double (&z)[8], double g) __attribute__((always_inline)) {
         const auto k = chunk(c);
 #pragma unroll
         for (int i = 0; i < 8; ++i) z[i] *= g;
         const uint2 w = g == 0.0 ? make_uint2(0u, 0u) : codes8(z, p.int8);
-        unsigned char* at = reinterpret_cast<unsigned char*>(p.y) + base + k.col;
-        if (k.whole()) {
-          reinterpret_cast<Bytes8*>(at)->v = w;
-        } else {
-          for (int i = k.lo; i < k.hi; ++i) at[i] = (unsigned char)((i < 4 ? w.x : w.y) >> (8 * (i & 3)));
-        }
+        codes.store(c * lanes + t, k, w);
       };
       if (G == 0) {
         double top = 0.0;
@@ -484,7 +502,7 @@ __global__ __launch_bounds__(kMaxThreads) void rmsnorm_add_kernel(RmsnormParams 
           top = Most::join(top, largest(z));
         }
         top = join_row<Most>(top, lanes, tops[turn]);
-        const double g = scaled(top, row, in && t == 0);
+        const double g = scaled(top, t == 0 ? 0 : -1);
 #pragma unroll
         for (int c = 0; c < C; ++c) {
           double z[8];
@@ -499,19 +517,36 @@ __global__ __launch_bounds__(kMaxThreads) void rmsnorm_add_kernel(RmsnormParams 
           weighed(c, z);
           double a = largest(z);
           a = join_lanes<Most>(a, G / 8);
-          put(c, z, scaled(a, row * p.groups + col / G, col < m && col % G == 0));
+          put(c, z, scaled(a, col < m && col % G == 0 ? col / G : -1));
         }
       }
     }
-    if (AHEAD) now = next;
-    else if (more) fetch(row + turns.step, now);
+    if constexpr (LATE) fetch(ahead, now);
+  };
+  Words a, b;
+  int64_t row = turns.first;
+  fetch(row, a);
+  if constexpr (C == 1) {
+    __builtin_amdgcn_sched_barrier(0);           // (as below)
+    fetch(row + turns.step, b);
+    __builtin_amdgcn_sched_barrier(0);
+    for (;; row += 2 * turns.step) {             // (all rows of a workgroup take as many turns as its first)
+      one(row, row + 2 * turns.step, a);
+      if (row - sub + turns.step >= turns.last) break;
+      one(row + turns.step, row + 3 * turns.step, b);
+      if (row - sub + 2 * turns.step >= turns.last) break;
+    }
+  } else {
+    for (; row - sub < turns.last; row += turns.step) one(row, row + turns.step, a);
   }
 }
 
 // Gradients.  A workgroup takes rows in turn, and its lanes keep the sum of dY n of their columns over
 // them: [workgroups, M] in fp32, summed by rmsnorm_dweight_kernel in a fixed order.  Two rows of words are on their way while
-// one is worked on (one, in more steps of a lane): 8192 rows of 5120 in bf16 take 66 us, 5.1 TB/s in and out as a
-// large copy has, 87 with one ahead.  8191 of 5119 take 85; 98 with branches at the rows' ends in place of Row.
+// one is worked on: 8192 rows of 5120 in bf16 take 66 us, 5.1 TB/s in and out as a large copy has, 87 with one ahead.
+// 8191 of 5119 take 85; 98 with branches at the rows' ends in place of Row.  In more steps of a lane the next row's words come
+// behind one's stores (4096 rows of 12289 97 us, 2048 of 32768 222; 125 and 387 as soon as that one's are taken apart, which
+// spills).
 template <typename T, typename R, int C, bool ODD>
 __global__ __launch_bounds__(kMaxThreads) void rmsnorm_add_bwd_kernel(RmsnormBwdParams p) {
   __shared__ float sums[2][kMaxWaves];
@@ -578,7 +613,7 @@ __global__ __launch_bounds__(kMaxThreads) void rmsnorm_add_bwd_kernel(RmsnormBwd
         s = __builtin_fmaf(g[c][i], n[c][i], s);
       }
     }
-    fetch(ahead, now);
+    if constexpr (C == 1) fetch(ahead, now);
     s = join_row<Sum>(s, lanes, sums[turn]) / (float)M;
     turn ^= 1;
     const Row<R, ODD> dresidual(p.dresidual, row * M, shift, in ? M : 0);
@@ -596,6 +631,7 @@ __global__ __launch_bounds__(kMaxThreads) void rmsnorm_add_bwd_kernel(RmsnormBwd
       dresidual.store(c * lanes + t, k, d);
       dx.store(c * lanes + t, k, d);
     }
+    if constexpr (C > 1) fetch(ahead, now);
     fetch_dh(ahead, now);
   };
   Words a, b;
@@ -608,9 +644,11 @@ __global__ __launch_bounds__(kMaxThreads) void rmsnorm_add_bwd_kernel(RmsnormBwd
     fetch(row + turns.step, b);
     fetch_dh(row + turns.step, b);
     __builtin_amdgcn_sched_barrier(0);
-    for (; row - sub < turns.last; row += 2 * turns.step) {
+    for (;; row += 2 * turns.step) {
       one(row, row + 2 * turns.step, a);
-      one(row + turns.step, row + 3 * turns.step, b);        // (or none, without a branch)
+      if (row - sub + turns.step >= turns.last) break;
+      one(row + turns.step, row + 3 * turns.step, b);
+      if (row - sub + 2 * turns.step >= turns.last) break;
     }
   } else {
     for (; row - sub < turns.last; row += turns.step) one(row, row + turns.step, a);
@@ -727,8 +765,6 @@ void with_types(int dtype, bool wide, F&& f) {
 // Rows of a workgroup: of at least 256 lanes, where that many divide alike.
 int rows_per_block(const Split& s) { return s.lanes == 64 ? 4 : s.lanes == 128 ? 2 : 1; }
 
-constexpr int64_t kMaxBlocks = 1 << 20;      // (more rows are taken in turn)
-
 // Workgroups that take rows in turn: as many as 256 compute units hold at a time with `hold` waves each, a multiple of 8.
 int64_t resident(const Split& s, int hold) {
   const int waves = s.lanes * rows_per_block(s) / 64;
@@ -750,8 +786,8 @@ hipError_t launch_rmsnorm_add(const RmsnormParams& p, hipStream_t stream) {
   q.lanes = s.lanes;
   q.inv = 1.0 / p.M;
   const int rpb = rows_per_block(s);
-  const bool turns = s.steps == 1 && p.M % 8 == 0;
-  const dim3 grid((unsigned)std::min(((int64_t)p.N + rpb - 1) / rpb, turns ? resident(s, 20) : kMaxBlocks)), block(s.lanes * rpb);
+  // 8 waves a compute unit, or one workgroup: 16384 rows of 4096 94 us, 101 with 16.  To 8 bits 16: 108, with 8 144.
+  const dim3 grid((unsigned)std::min(((int64_t)p.N + rpb - 1) / rpb, resident(s, p.scales ? 16 : 8))), block(s.lanes * rpb);
   with_types(p.dtype, p.wide, [&](auto t, auto r) {
     typedef decltype(t) T;
     typedef decltype(r) R;
@@ -785,7 +821,7 @@ hipError_t launch_rmsnorm_add_bwd(const RmsnormBwdParams& p, float* dweight, hip
 
 hipError_t launch_quant8_load(const Quant8LoadParams& p, hipStream_t stream) {
   const int64_t all = (int64_t)p.N * ((p.M % 8 && !p.group ? p.M + 14 : p.M + 7) / 8);
-  const dim3 grid((unsigned)std::min((all + 255) / 256, kMaxBlocks)), block(256);
+  const dim3 grid((unsigned)std::min((all + 255) / 256, (int64_t)1 << 20)), block(256);     // (more chunks in turn)
   with_types(p.dtype, false, [&](auto t, auto) {
     if (p.M % 8 == 0) hipLaunchKernelGGL((quant8_load_kernel<decltype(t), false>), grid, block, 0, stream, p);
     else hipLaunchKernelGGL((quant8_load_kernel<decltype(t), true>), grid, block, 0, stream, p);
