@@ -36,6 +36,11 @@ Contents
                    (include/rope.h, include/kv4.h): plain definitions, pinned
                    by ``tests/test_serve_oracle.py``.
 
+``train``          attention's gradient, the norm with the residual's addition and
+                   its gradient, 8-bit codes (include/attn_bwd.h,
+                   include/rmsnorm.h): plain definitions, pinned by
+                   ``tests/test_train_oracle.py``.
+
 Parity status: every function here is pinned by ``tests/test_oracle_pins.py``
 and ``tests/test_algorithms.py`` (invariants, closed forms, brute force and
 the CPU float64 ``scaled_dot_product_attention`` of PyTorch as a library
