@@ -325,7 +325,10 @@ struct Row {
     unsigned w[N * S / 4 + 1];
     if constexpr (S == 4) {
 #pragma unroll
-      for (int k = 0; k < N; ++k) w[k] = __builtin_bit_cast(unsigned, x[k]);
+      for (int k = 0; k < N; ++k) {
+        const float f = x[k];
+        w[k] = __builtin_bit_cast(unsigned, f);
+      }
     } else {
 #pragma unroll
       for (int k = 0; k < N; k += 2) w[k / 2] = Elem<T>::pack2(x[k], x[k + 1 < N ? k + 1 : k]);
