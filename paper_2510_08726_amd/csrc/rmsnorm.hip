@@ -375,7 +375,8 @@ __device__ __forceinline__ Turns turns_of(int64_t N, int rpb, int sub) {
 // that one's are stored where QUANT leaves no registers, 4096 rows of 16384 with a scale each 163 us, 206 spilled).  8192 rows
 // of 5120 in bf16 take 62 us, 5.4 TB/s in and out (a large copy 5.1), 8191 of 5119 76, 101 with branches at the rows' ends;
 // to 8 bits, 8192 of 8192 93 us with a scale for each 128, 120 with one row ahead.  That is bound by
-// fp64 (the codes are those of the exact quotients), and a scale a row by taking h through it twice: 129.
+// fp64 (the codes are those of the exact quotients), and a scale a row by its second join as well: 125 (127 with h taken
+// through fp64 twice, as more steps of a lane do).
 template <typename T, typename R, int C, bool QUANT, bool ODD>
 __global__ __launch_bounds__(kMaxThreads) void rmsnorm_add_kernel(RmsnormParams p) {
   constexpr bool LATE = QUANT && C > 1;          // (no registers for it beside the fp64 values)
@@ -497,20 +498,27 @@ __global__ __launch_bounds__(kMaxThreads) void rmsnorm_add_kernel(RmsnormParams 
         codes.store(c * lanes + t, k, w);
       };
       if (G == 0) {
-        double top = 0.0;
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
+        if constexpr (C == 1) {
           double z[8];
-          weighed(c, z);
-          top = Most::join(top, largest(z));
-        }
-        top = join_row<Most>(top, lanes, tops[turn]);
-        const double g = scaled(top, t == 0 ? 0 : -1);
+          weighed(0, z);
+          const double top = join_row<Most>(largest(z), lanes, tops[turn]);
+          put(0, z, scaled(top, t == 0 ? 0 : -1));
+        } else {                                 // (h (w + offset) twice: there are no registers for all of it in 64 bits)
+          double top = 0.0;
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
-          double z[8];
-          weighed(c, z);
-          put(c, z, g);
+          for (int c = 0; c < C; ++c) {
+            double z[8];
+            weighed(c, z);
+            top = Most::join(top, largest(z));
+          }
+          top = join_row<Most>(top, lanes, tops[turn]);
+          const double g = scaled(top, t == 0 ? 0 : -1);
+#pragma unroll
+          for (int c = 0; c < C; ++c) {
+            double z[8];
+            weighed(c, z);
+            put(c, z, g);
+          }
         }
       } else {
 #pragma unroll
