@@ -11,7 +11,7 @@
 //   bwd_kernel       dkv_block: a workgroup owns 128 keys and streams the tiles of 32 queries that see them;
 //                    dq_block: a workgroup owns 128 query rows and streams the tiles of 32 keys
 //   bwd_sum_kernel   adds up the blocks that were divided into parts, where few blocks are long
-// Both kinds of blocks form S and dP, seven products in the place of five.  (One loop for
+// Both kinds of blocks form S and dP, seven products in the place of five (and dQ's in two halves, below).  (One loop for
 // both would need the partial dQ of every key block in memory, 1 KB a row and block of 256 keys
 // against 131 kflop saved: no less time at this card's rates, and a sum over blocks.)
 //
@@ -224,7 +224,8 @@ __device__ __forceinline__ int bwd_scale(const BwdParams& p, int unit, float* sh
 // the row within its tile) over the scale, so that it starts the accumulator of Q K^T (with
 // SoftCap: not over the scale, and with the cap: see capped); then -delta, which starts that of dO V^T.  fp16: the largest square sums of
 // the rows of dO and V in each block of 64.  Rows that see no key (the first Lq - Lk with the causal mask)
-// take no part: their dQ is zero.  One pass over dO and O: bound by memory.
+// take no part: their dQ is zero.  One pass over dO and O: bound by memory, 32 heads of 8192 rows of 128 in bf16 (134 MB) 28 us,
+// 4.8 TB/s.
 template <int D, typename T>
 __global__ __launch_bounds__(kThreads) void bwd_rows_kernel(BwdParams p) {
   constexpr int LANES = D / 8, RPP = kThreads / LANES;     // lanes of a row, rows of a pass
@@ -849,7 +850,10 @@ __device__ __forceinline__ void dq_block(const BwdParams& p, char* lds, int item
   }
 }
 
-// Both in one launch, the key blocks first: the row blocks fill what they leave free.
+// Both in one launch, the key blocks first: the row blocks fill what they leave free.  32 heads of 8192 causal rows of 128 in
+// bf16 take 1856 us, 0.74 PFLOP/s of the formula's five products and 1.18 of the eight that are formed, the matrix unit busy 0.66 of the cycles (at
+// 1.72 GHz under that load); with fp16, a cap and a window of 1025 (32 / 16 heads of 3001 on 4099) 255, the vector unit 0.55
+// and the matrix unit 0.40; 16 heads of 64 dims have the exponentials of twice as many products: 0.44 and 0.28.
 template <int D, typename T, bool CAUSAL, bool ALIBI, bool CAP>
 __global__ __launch_bounds__(kThreads, 2) void bwd_kernel(BwdParams p) {
   __shared__ __attribute__((aligned(1024))) char lds[kStages * kStage<D> + kWaves * 1024 * kHome<D, T, ALIBI || CAP>];
@@ -865,7 +869,7 @@ __global__ __launch_bounds__(kThreads, 2) void bwd_kernel(BwdParams p) {
 }
 
 // The partials of the blocks in several parts, summed in their order and rounded: 1024 values a workgroup,
-// first of dK and dV, then of dQ.
+// first of dK and dV, then of dQ.  Bound by memory: 11 us for 46 MB of them (2 x 32 / 8 heads of 2048 rows).
 template <int D, typename T>
 __global__ __launch_bounds__(256) void bwd_sum_kernel(BwdParams p) {
   constexpr int PER = BLK * D / 1024;                      // workgroups of a piece
