@@ -709,7 +709,7 @@ __global__ __launch_bounds__(256) void rmsnorm_dweight_kernel(const float* ws, f
   }
 }
 
-// What codes stand for: 8 of them a lane.  Bound by memory: 8192 x 8192 to bf16 (210 MB) 35 us, 5.9 TB/s.
+// What codes stand for: 8 of them a lane.  Bound by memory: 8192 x 8192 to bf16 (203 MB) 35 us, 5.8 TB/s.
 template <typename T, bool ODD>
 __global__ __launch_bounds__(256) void quant8_load_kernel(Quant8LoadParams p) {
   const int chunks = (ODD && !p.group ? p.M + 14 : p.M + 7) / 8;

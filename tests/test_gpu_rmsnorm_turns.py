@@ -98,3 +98,45 @@ def test_a_matrix_ends_where_its_memory_does():
                 c = x.clone()
                 dx1, _, dw1 = pa.rmsnorm_add_bwd(c, c.clone(), r, torch.ones(M, dtype=dtype, device="cuda"))
                 assert same(dx, dx1) and same(dw, dw1) and bool(torch.isfinite(dx).all())
+
+
+@pytest.mark.parametrize("M", [8192, 4099])
+def test_offsets_past_32_bits(M):
+    """More than 2^32 bytes and 2^31 elements a matrix: the last rows have the bits that they have alone."""
+    N = (2 ** 31 // M // FEW + 2) * FEW
+    g = torch.Generator("cuda").manual_seed(M)
+    x = torch.empty(N, M, dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+    w = torch.ones(M, dtype=torch.bfloat16, device="cuda")
+    at = slice(N - FEW, N)
+    y, h, rstd = pa.rmsnorm_add(x, x, w)
+    alone = pa.rmsnorm_add(x[at], x[at], w)
+    assert all(same(a[at], b) for a, b in zip((y, h, rstd), alone))
+    del y
+    q, s, _ = pa.rmsnorm_add_quant(x, None, w)
+    alone = pa.rmsnorm_add_quant(x[at], None, w)
+    assert same(q[at], alone[0]) and same(s[at], alone[1])
+    assert same(pa.quant8_load(q, s)[at], pa.quant8_load(q[at], s[at]))
+    del q
+    dx, _, dw = pa.rmsnorm_add_bwd(x, h, rstd, w, x)
+    assert same(dx[at], pa.rmsnorm_add_bwd(x[at], h[at], rstd[at], w, x[at])[0])
+    assert bool(torch.isfinite(dw).all())
+    del x, h, dx
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("M", [5, 37, 771, 8201])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_a_row_that_is_not_finite_stays_alone(M, bad):
+    """Rows whose elements lie in one 16-byte word with those of a row that is not finite."""
+    for dtype in ("bf16", "f32"):
+        x, res, w, dy, dh = draw(19, M, dtype, dtype)
+        rows = [i for i in range(19) if i != 7]
+        good = [*pa.rmsnorm_add(x, res, w), *pa.rmsnorm_add_quant(x, res, w)[:2]]
+        rstd = good[2].clone()
+        good += pa.rmsnorm_add_bwd(dy, good[1], rstd, w, dh)[:1]
+        h = good[1].clone()
+        for t in (x, res, dy, dh, h):
+            t[7] = bad
+        got = [*pa.rmsnorm_add(x, res, w), *pa.rmsnorm_add_quant(x, res, w)[:2], *pa.rmsnorm_add_bwd(dy, h, rstd, w, dh)[:1]]
+        assert all(same(a[rows], b[rows]) for a, b in zip(got, good))
+        assert bool(got[4][7].isnan().all()) and not bool(torch.isfinite(got[0][7].float()).all())
