@@ -23,6 +23,8 @@ namespace {
 
 constexpr int kMaxThreads = 1024;
 constexpr int kMaxWaves = kMaxThreads / 64;
+constexpr int kMaxSteps = 4;
+constexpr int kMaxChunks = kMaxSteps * 8 * kMaxThreads;      // elements of the chunks that a workgroup's lanes hold
 
 // 8 elements as they lie in memory.
 template <typename T>
@@ -123,6 +125,13 @@ __device__ __forceinline__ Chunk<ODD> chunk_of(int i, int shift, int M) {
   if constexpr (!ODD) return {8 * i, 0, 8 * i < M ? 8 : 0};
   const int col = 8 * i - shift;
   return {col, max(-col, 0), max(min(M - col, 8), 0)};
+}
+
+// Elements that a row of M at element `index` of the matrix begins behind a multiple of 8.  Of the few widths of which that
+// would take one chunk more than the lanes hold none: their chunks begin at the row's first element.
+template <int C>
+__device__ __forceinline__ int shift_of(int64_t index, int M) {
+  return C == kMaxSteps && M + 7 > kMaxChunks ? 0 : (int)(index & 7);
 }
 
 // Values as T holds them.
@@ -387,7 +396,7 @@ __global__ __launch_bounds__(kMaxThreads) void rmsnorm_add_kernel(RmsnormParams 
   const int M = p.M;
   const Turns turns = turns_of(p.N, rpb, sub);
   // Of all its rows: a lane's columns stay the same.  (Groups begin at a chunk's first element.)
-  const int shift = !ODD || (QUANT && p.group) ? 0 : (int)(turns.first * M & 7);
+  const int shift = !ODD || (QUANT && p.group) ? 0 : shift_of<C>(turns.first * M, M);
   Raw<T> weight[C];
 #pragma unroll
   for (int c = 0; c < C; ++c) {
@@ -566,7 +575,7 @@ __global__ __launch_bounds__(kMaxThreads) void rmsnorm_add_bwd_kernel(RmsnormBwd
   const int sub = __builtin_amdgcn_readfirstlane(threadIdx.x / lanes), t = threadIdx.x % lanes;
   const int M = p.M;
   const Turns turns = turns_of(p.N, rpb, sub);
-  const int shift = ODD ? (int)(turns.first * M & 7) : 0;       // of all its rows: a lane's columns stay the same
+  const int shift = ODD ? shift_of<C>(turns.first * M, M) : 0;       // of all its rows: a lane's columns stay the same
   auto chunk = [&](int c, bool in) __attribute__((always_inline)) { return chunk_of<ODD>(c * lanes + t, shift, in ? M : 0); };
   float dw[C][8];
   Raw<T> weight[C];
@@ -745,8 +754,8 @@ struct Split {
 // By the row's length alone, so that a row's bits do not depend on how many there are.  One step of a lane
 // up to 8192 elements, by as many waves as it takes.
 Split split(int M) {
-  const int m = M % 8 ? M + 7 : M;             // (a row may begin within a chunk)
-  const int s = (m + 8 * kMaxThreads - 1) / (8 * kMaxThreads), steps = s <= 2 ? s : 4;
+  const int m = M % 8 && M + 7 <= kMaxChunks ? M + 7 : M;      // (a row may begin within a chunk: shift_of)
+  const int s = (m + 8 * kMaxThreads - 1) / (8 * kMaxThreads), steps = s <= 2 ? s : kMaxSteps;
   return {((m + 8 * steps - 1) / (8 * steps) + 63) / 64 * 64, steps};
 }
 
