@@ -49,6 +49,7 @@ constexpr int BLK = TN * kWaves;        // keys (rows) that a workgroup owns
 constexpr int kXcds = 8;
 constexpr int kRowsBlock = 64;          // rows of a workgroup of bwd_rows_kernel
 constexpr int kShift = 15;              // fp16: P is held times 2^kShift
+constexpr double kLog2e64 = 1.4426950408889634;
 
 typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
 typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
@@ -220,9 +221,9 @@ __device__ __forceinline__ int bwd_scale(const BwdParams& p, int unit, float* sh
 }
 
 // A row's part of its scores and of dP, in tiles of 32 rows: [B Hq, tiles, 64] floats,
-// first what is added to a score before its exponential, (2^15's exponent - lse log2 e - the ALiBi bias of
-// the row within its tile) over the scale, so that it starts the accumulator of Q K^T (with
-// SoftCap: not over the scale, and with the cap: see capped); then -delta, which starts that of dO V^T.  fp16: the largest square sums of
+// first what is added to a score before its exponential, (2^15's exponent - lse log2 e) over the scale, so that it starts the
+// accumulator of Q K^T (with SoftCap: not over the scale, and with the cap: see capped; with ALiBi what the bias at
+// the tile's origin leaves of lse, by a difference in 64 bits, for lse is as large as the bias: alibi_origin); then -delta, which starts that of dO V^T.  fp16: the largest square sums of
 // the rows of dO and V in each block of 64.  Rows that see no key (the first Lq - Lk with the causal mask)
 // take no part: their dQ is zero.  One pass over dO and O: bound by memory, 32 heads of 8192 rows of 128 in bf16 (134 MB) 28 us,
 // 4.8 TB/s.
@@ -239,7 +240,8 @@ __global__ __launch_bounds__(kThreads) void bwd_rows_kernel(BwdParams p) {
     const int head = blk / p.row_blocks, b = head / p.Hq, h = head - b * p.Hq;
     const int i0 = (blk - head * p.row_blocks) * kRowsBlock;
     peak_at = p.peaks + blk;
-    const float sl2 = p.slopes ? p.slopes[h] * kLog2e : 0.f;
+    const float slope = p.slopes ? p.slopes[h] : 0.f;
+    const AlibiOrigin o = alibi_origin(slope, p.causal, p.window, p.Lk, p.Lk - p.rows);
     const T* og = reinterpret_cast<const T*>(p.o) + ((size_t)head * p.Lq + p.row0) * D + 8 * lane;
     const T* dg = reinterpret_cast<const T*>(p.d_o) + b * p.do_sb + h * p.do_sh + p.row0 * p.do_sl + 8 * lane;
 #pragma unroll
@@ -266,9 +268,13 @@ __global__ __launch_bounds__(kThreads) void bwd_rows_kernel(BwdParams p) {
         float start = kNegInf, nd = 0.f;
         if (i < p.rows) {
           const float lse = p.lse[(size_t)head * p.Lq + p.row0 + i];
-          float e = (is_half<T> ? (float)kShift : 0.f) - lse * kLog2e;
-          if (p.cap_cl == 0.f) e = (e - sl2 * (float)(i % TN)) / p.c;
-          else e += p.cap_cl;
+          constexpr float shift = is_half<T> ? (float)kShift : 0.f;
+          float e = shift - lse * kLog2e;
+          if (p.slopes) {
+            const double rest = (double)slope * (double)(o.at(i - i % TN) - (p.Lk - p.rows) - i) - (double)lse;
+            e = (float)(rest * kLog2e64 + (double)shift);
+          }
+          e = p.cap_cl == 0.f ? e / p.c : e + p.cap_cl;
           start = lse == kNegInf ? kNegInf : e;
           nd = -dot;
         }
@@ -510,11 +516,11 @@ __device__ __forceinline__ void dkv_block(const BwdParams& p, char* lds, int ite
 
   // One tile: queries i0 .. i0 + 31 of a head against the wave's keys.  The vector work runs beside the MFMAs that do not
   // wait for it: the exponentials beside dP (and the start of dV), dS beside dV (and the start of dK).
-  auto tile = [&](auto masked, uint32_t st, uint32_t next, int i0, float sl2) __attribute__((always_inline)) {
+  auto tile = [&](auto masked, uint32_t st, uint32_t next, int i0, float sl2, AlibiOrigin o) __attribute__((always_inline)) {
     constexpr bool MASKED = decltype(masked)::value;
     // Query i sees this lane's key: lo <= i - i0 - 4 hh < hi.
     const int lo = key - off - i0 - 4 * hh, hi = W > 0 ? lo + W : 1 << 30;
-    const float bias = ALIBI ? sl2 * (float)(key - off - i0) : 0.f;
+    const float bias = ALIBI ? sl2 * (float)(key - o.at(i0)) : 0.f;
     Weights<T> pw, dw;
     uint32_t sx = 0;
     if constexpr (CAP) sx = stats_at(st + 2 * TB, hh);
@@ -607,27 +613,28 @@ __device__ __forceinline__ void dkv_block(const BwdParams& p, char* lds, int ite
   // Runs of tiles of one kind, each its own loop: the kinds side by side in one loop cost moves of the
   // accumulators at every tile.
   int u = u0;
-  auto run = [&](auto kind, int end, float sl2) __attribute__((always_inline)) {      // to tile `end` of the head
+  auto run = [&](auto kind, int end, float sl2, AlibiOrigin o) __attribute__((always_inline)) {      // to tile `end` of the head
     constexpr int KIND = decltype(kind)::value;        // 0: no row sees a key, 1: some, 2: all
     end = min(end, t + u1 - u);
     for (; t < end; ++t, ++u) {
       const uint32_t st = lds0 + (uint32_t)(u - u0) % kStages * STAGE, next = lds0 + (uint32_t)(u + 1 - u0) % kStages * STAGE;
       if constexpr (KIND == 0) prime(next);
-      else tile(std::integral_constant<bool, KIND == 1>{}, st, next, t * TN, sl2);
+      else tile(std::integral_constant<bool, KIND == 1>{}, st, next, t * TN, sl2, o);
       advance(u);
     }
   };
   while (u < u1) {
-    const float sl2 = ALIBI ? p.slopes[h0 + g] * kLog2e : 0.f;
+    const float slope = ALIBI ? p.slopes[h0 + g] : 0.f, sl2 = slope * kLog2e;
+    const AlibiOrigin o = alibi_origin(slope, CAUSAL, W, p.Lk, off);
     if constexpr (CAUSAL) {
-      run(std::integral_constant<int, 0>{}, va, sl2);
+      run(std::integral_constant<int, 0>{}, va, sl2, o);
       for (int k = 0; k < 2; ++k) {      // (in a window a second time behind the whole ones)
-        run(std::integral_constant<int, 1>{}, k ? vb : wa, sl2);
-        run(std::integral_constant<int, 2>{}, wb, sl2);
+        run(std::integral_constant<int, 1>{}, k ? vb : wa, sl2, o);
+        run(std::integral_constant<int, 2>{}, wb, sl2, o);
       }
-      run(std::integral_constant<int, 0>{}, ta + nt, sl2);
+      run(std::integral_constant<int, 0>{}, ta + nt, sl2, o);
     } else {
-      run(std::integral_constant<int, 2>{}, ta + nt, sl2);
+      run(std::integral_constant<int, 2>{}, ta + nt, sl2, o);
     }
     t = ta;
     ++g;
@@ -690,7 +697,8 @@ __device__ __forceinline__ void dq_block(const BwdParams& p, char* lds, int item
   }
   const float* sx = p.stats + (head * p.row_tiles + row / TN) * (2 * TN) + row % TN;
   const float start = sx[0], nd = sx[TN];
-  const float sl2 = ALIBI ? p.slopes[hq] * kLog2e : 0.f;
+  const float slope = ALIBI ? p.slopes[hq] : 0.f, sl2 = slope * kLog2e;
+  const int from = alibi_origin(slope, CAUSAL, W, p.Lk, off).at(iw);
   const float c = p.c, add = CAP ? start : start * c;
 
   const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_void*)lds;
@@ -742,7 +750,7 @@ __device__ __forceinline__ void dq_block(const BwdParams& p, char* lds, int item
     if (CAUSAL && W > 0) lo = row + off - W;
     hi -= j0 + 4 * hh;
     lo -= j0 + 4 * hh;
-    const float base = ALIBI ? __builtin_fmaf(sl2, (float)(j0 + 4 * hh - iw - off), add) : add;
+    const float base = ALIBI ? __builtin_fmaf(sl2, (float)(j0 + 4 * hh - from), add) : add;
     Weights<T> w, rest;
     auto weigh = [&](auto kc) __attribute__((always_inline)) {       // registers 2 k, 2 k + 1
       constexpr int r = 2 * decltype(kc)::value;

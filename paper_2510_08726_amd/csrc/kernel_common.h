@@ -77,6 +77,21 @@ __device__ __forceinline__ float soft_cap(float x, float k2, float cl, float add
 }
 __device__ __forceinline__ float soft_cap(float x, float k2, float cl) { return soft_cap(x, k2, cl, cl); }
 
+// ALiBi's bias of query i for key j, -slope (i + off - j), counted from an origin o of the query's tile, the key at which (nearly)
+// it is largest: slope (j - o) + slope (o - off - i).  The first part is small wherever a weight is not, and what the second one
+// leaves of a row's log-sum-exp is; counted from the query, both are as large as the distance of the farthest key where the mask
+// lets that weigh most, and their fp32 roundings (2^-11 at 8192) come into the exponent.  A slope over 0 favours the
+// last key, with the causal mask the query's own; one under 0 the first one, in a window its lower edge.
+struct AlibiOrigin {
+  int key, moves;       // of a tile whose first query is i: key, + i if it moves
+  __device__ __forceinline__ int at(int i) const { return max(key + (moves ? i : 0), 0); }
+};
+__device__ __forceinline__ AlibiOrigin alibi_origin(float slope, bool causal, int window, int Lk, int off) {
+  const bool down = __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, slope)) < 0;
+  if (down) return {causal && window > 0 ? off + 1 - window : 0, causal && window > 0};
+  return {causal ? off : Lk - 1, causal};
+}
+
 // K and V tiles live in LDS row-major, [keys][D], with the 16-byte chunks of
 // each row XOR-swizzled: chunk c of row r sits at chunk position c ^ swz(r).
 // That keeps the K operand reads (16 consecutive rows at one chunk) and the

@@ -1,5 +1,5 @@
 """The errors of attention's outputs in training, as root mean squares against 64 bits: those of the roundings that the kernels choose
-(train_errors.py)."""
+(train_errors.py), where a log-sum-exp in the thousands stands beside the scores too."""
 
 import math
 
@@ -22,7 +22,7 @@ def run(case, x):
 
 
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
-@pytest.mark.parametrize("case", te.CASES)
+@pytest.mark.parametrize("case", te.CASES + te.FAR)
 def test_errors_are_those_of_the_roundings(case, dtype):
     x = te.inputs(case, dtype)
     want, emulated = te.both64(case, x, dtype)
@@ -40,3 +40,23 @@ def test_errors_are_those_of_the_roundings(case, dtype):
     assert (off <= most).all(), float((off / most).max())
     assert all(s <= te.MORE for s in share.values()), share
     assert not any(math.isnan(s) for s in share.values())
+
+
+def test_a_zero_slope_and_slopes_of_both_signs():
+    """Heads of one call, each with its own origin; a slope of 0 is no bias."""
+    B, H, L, D = 1, 4, 500, 64
+    g = torch.Generator().manual_seed(3)
+    do, q, k, v = [torch.randn((B, H, L, D), generator=g).to(torch.float16).cuda() for _ in range(4)]
+    for causal in (False, True):
+        slopes = torch.tensor([0.5, 0.0, -0.0, -0.5], device="cuda")
+        o, lse = pa.attn_fwd_lse(q, k, v, causal=causal, alibi_slopes=slopes)
+        grads = pa.attn_bwd(do, q, k, v, o, lse, causal=causal, alibi_slopes=slopes)
+        for h in range(H):
+            one = [t[:, h:h + 1].contiguous() for t in (do, q, k, v)]
+            how = dict(causal=causal, alibi_slopes=slopes[h:h + 1].clone())
+            o1, lse1 = pa.attn_fwd_lse(*one[1:], **how)
+            alone = (o1, lse1, *pa.attn_bwd(*one, o1, lse1, **how))
+            for a, b in zip((o, lse, *grads), alone):
+                # (Another division of the blocks sums in another order, and fp16's power of two may differ.)
+                d = (a[:, h:h + 1].float() - b.float()).abs().max()
+                assert d <= 2.0 ** -9 * b.float().abs().max(), (causal, h)

@@ -22,6 +22,14 @@ CASES = [
     (1, 4, 2, 300, 300, 64, True, None, 30.0, 100),
     (2, 4, 4, 200, 333, 128, True, (0.5, 0.25, 0.0625, 0.01), None, None),
 ]
+# Biases that make the log-sum-exp of a row as large as the distance of its farthest key: thousands.
+FAR = [
+    (1, 2, 1, 8192, 300, 128, False, (0.84, 0.25), None, None),
+    (1, 2, 2, 8192, 150, 64, False, (0.84, 0.25), None, None),
+    (1, 2, 2, 40, 8192, 64, False, (-0.84, -0.25), None, None),
+    (1, 2, 1, 2500, 2500, 64, True, (-0.84, -0.25), None, None),
+    (1, 2, 2, 2100, 2500, 128, True, (-0.84, -0.25), None, 1700),
+]
 
 
 def to(x, dtype):
