@@ -39,9 +39,9 @@ extern "C" {
  * attn_fwd_mod that also writes lse [B, Hq, Lq] (fp32, natural units).  The sums of
  * exponentials are those before their rounding to the type of Q (attn_fwd's are of
  * the rounded ones), so O may differ from attn_fwd's in the last bit.  One kernel, at any Lq (the keys of
- * few rows are not divided over workgroups).
+ * few rows are not divided over workgroups).  Q, K, V and O are 16-byte aligned.
  * Errors: as attn_fwd_mod; ATTN_ERR_NULL (lse), ATTN_ERR_SHAPE for outputs that share memory with another
- * operand, ATTN_ERR_UNSUPPORTED for a softcap over ATTN_TRAIN_MAX_SOFTCAP.
+ * operand and for tensors that are not aligned, ATTN_ERR_UNSUPPORTED for a softcap over ATTN_TRAIN_MAX_SOFTCAP.
  */
 int attn_fwd_lse(const void* Q, const void* K, const void* V, void* O, float* lse,
                  int B, int Hq, int Hkv, int Lq, int Lk, int D,

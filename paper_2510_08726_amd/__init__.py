@@ -906,7 +906,8 @@ def attn_fwd_lse(q, k, v, o=None, lse=None, *, causal=False, scale=None, alibi_s
     q [B, Hq, Lq, D], k and v [B, Hkv, Lk, D] and the other arguments as for
     attn_fwd; ``softcap`` at most 1024.  ``lse`` [B, Hq, Lq] float32: log sum_j
     exp(s_ij) of the row's scores (scaled, capped, with the bias), -inf for a row
-    that sees no key.  Neither output may share memory with another operand.
+    that sees no key.  q, k, v and o are 16-byte aligned; neither output may share memory
+    with another operand.
     Nothing is recorded for autograd: a program that trains calls attn_bwd.
     Returns (o, lse).
     """

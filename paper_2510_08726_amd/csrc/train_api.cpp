@@ -195,6 +195,9 @@ int attn_fwd_lse(const void* Q, const void* K, const void* V, void* O, float* ls
                  attn_dtype dtype, hipStream_t stream) {
   if (!Q || !K || !V || !O || !lse) return ATTN_ERR_NULL;
   if (int rc = check(B, Hq, Hkv, Lq, Lk, D, causal, scale, alibi_slopes, softcap, window, dtype); rc != ATTN_OK) return rc;
+  // (Copies to LDS of 16 bytes a lane; attn_bwd takes no others either.)
+  for (const void* x : {Q, K, V, (const void*)O})
+    if (misaligned(x)) return ATTN_ERR_SHAPE;
   const int64_t nqb = ceil_div(Lq, attn::prefill_block_rows());
   if (nqb * 4 * B * Hq > kMaxInt) return ATTN_ERR_SHAPE;
   const int64_t q = 2LL * B * Hq * Lq * D, k = 2LL * B * Hkv * Lk * D, l = 4LL * B * Hq * Lq;
