@@ -241,7 +241,7 @@ __global__ __launch_bounds__(kThreads) void bwd_rows_kernel(BwdParams p) {
     const int i0 = (blk - head * p.row_blocks) * kRowsBlock;
     peak_at = p.peaks + blk;
     const float slope = p.slopes ? p.slopes[h] : 0.f;
-    const AlibiOrigin o = alibi_origin(slope, p.causal, p.window, p.Lk, p.Lk - p.rows);
+    const AlibiOrigin o = alibi_origin(slope, p.causal, p.window, p.Lk);
     const T* og = reinterpret_cast<const T*>(p.o) + ((size_t)head * p.Lq + p.row0) * D + 8 * lane;
     const T* dg = reinterpret_cast<const T*>(p.d_o) + b * p.do_sb + h * p.do_sh + p.row0 * p.do_sl + 8 * lane;
 #pragma unroll
@@ -271,7 +271,8 @@ __global__ __launch_bounds__(kThreads) void bwd_rows_kernel(BwdParams p) {
           constexpr float shift = is_half<T> ? (float)kShift : 0.f;
           float e = shift - lse * kLog2e;
           if (p.slopes) {
-            const double rest = (double)slope * (double)(o.at(i - i % TN) - (p.Lk - p.rows) - i) - (double)lse;
+            const int at = p.Lk - p.rows + i;     // off + i
+            const double rest = (double)slope * (double)-from_origin(at, at - i % TN, o, p.causal) - (double)lse;
             e = (float)(rest * kLog2e64 + (double)shift);
           }
           e = p.cap_cl == 0.f ? e / p.c : e + p.cap_cl;
@@ -520,7 +521,7 @@ __device__ __forceinline__ void dkv_block(const BwdParams& p, char* lds, int ite
     constexpr bool MASKED = decltype(masked)::value;
     // Query i sees this lane's key: lo <= i - i0 - 4 hh < hi.
     const int lo = key - off - i0 - 4 * hh, hi = W > 0 ? lo + W : 1 << 30;
-    const float bias = ALIBI ? sl2 * (float)(key - o.at(i0)) : 0.f;
+    const float bias = ALIBI ? sl2 * (float)(key + here(from_origin(0, off + i0, o, CAUSAL))) : 0.f;
     Weights<T> pw, dw;
     uint32_t sx = 0;
     if constexpr (CAP) sx = stats_at(st + 2 * TB, hh);
@@ -625,7 +626,7 @@ __device__ __forceinline__ void dkv_block(const BwdParams& p, char* lds, int ite
   };
   while (u < u1) {
     const float slope = ALIBI ? p.slopes[h0 + g] : 0.f, sl2 = slope * kLog2e;
-    const AlibiOrigin o = alibi_origin(slope, CAUSAL, W, p.Lk, off);
+    const AlibiOrigin o = alibi_origin(slope, CAUSAL, W, p.Lk);
     if constexpr (CAUSAL) {
       run(std::integral_constant<int, 0>{}, va, sl2, o);
       for (int k = 0; k < 2; ++k) {      // (in a window a second time behind the whole ones)
@@ -698,7 +699,7 @@ __device__ __forceinline__ void dq_block(const BwdParams& p, char* lds, int item
   const float* sx = p.stats + (head * p.row_tiles + row / TN) * (2 * TN) + row % TN;
   const float start = sx[0], nd = sx[TN];
   const float slope = ALIBI ? p.slopes[hq] : 0.f, sl2 = slope * kLog2e;
-  const int from = alibi_origin(slope, CAUSAL, W, p.Lk, off).at(iw);
+  const int from = -from_origin(0, off + iw, alibi_origin(slope, CAUSAL, W, p.Lk), CAUSAL);
   const float c = p.c, add = CAP ? start : start * c;
 
   const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_void*)lds;

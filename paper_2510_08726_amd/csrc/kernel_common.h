@@ -83,13 +83,17 @@ __device__ __forceinline__ float soft_cap(float x, float k2, float cl) { return 
 // lets that weigh most, and their fp32 roundings (2^-11 at 8192) come into the exponent.  A slope over 0 favours the
 // last key, with the causal mask the query's own; one under 0 the first one, in a window its lower edge.
 struct AlibiOrigin {
-  int key, moves;       // of a tile whose first query is i: key, + i if it moves
-  __device__ __forceinline__ int at(int i) const { return max(key + (moves ? i : 0), 0); }
+  int key;              // the origin; with the causal mask how far before the tile's first query it lies, where that many keys do
 };
-__device__ __forceinline__ AlibiOrigin alibi_origin(float slope, bool causal, int window, int Lk, int off) {
+__device__ __forceinline__ AlibiOrigin alibi_origin(float slope, bool causal, int window, int Lk) {
   const bool down = __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, slope)) < 0;
-  if (down) return {causal && window > 0 ? off + 1 - window : 0, causal && window > 0};
-  return {causal ? off : Lk - 1, causal};
+  if (causal) return {!down ? 0 : window > 0 ? window - 1 : 0x7fffffff};
+  return {down ? 0 : Lk - 1};
+}
+// j - o in a tile whose first query is i, at = off + i.  (Counted back from the query, as what masks are made of is: with the
+// origin itself formed in every tile, the gradient of 16 heads of 4096 rows of 64, window 1000, takes 106 us and not 98.)
+__device__ __forceinline__ int from_origin(int j, int at, const AlibiOrigin& o, bool causal) {
+  return causal ? j - at + min(at, o.key) : j - o.key;
 }
 
 // K and V tiles live in LDS row-major, [keys][D], with the 16-byte chunks of

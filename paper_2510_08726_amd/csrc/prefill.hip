@@ -1045,7 +1045,7 @@ __global__ __launch_bounds__(kThreads, kWgPerCu) __attribute__((amdgpu_num_vgpr(
     ta.sl2 = ALIBI ? p.slopes[cur.hq] * kLog2e : 0.f;
     // Where the tiles' biases count from.  (attn_fwd's: the wave's first row.)
     [[maybe_unused]] AlibiOrigin origin;
-    if constexpr (ALIBI && kLse) origin = alibi_origin(ta.sl2, CAUSAL, W, Lk, off);
+    if constexpr (ALIBI && kLse) origin = alibi_origin(ta.sl2, CAUSAL, W, Lk);
     if constexpr (PF::ACCB) {
       // c (s + kb) + base = c s + slope log2(e) kconst(r) + base.  A zero
       // scale takes a tiny c instead, whose product with s vanishes.
@@ -1062,7 +1062,7 @@ __global__ __launch_bounds__(kThreads, kWgPerCu) __attribute__((amdgpu_num_vgpr(
     // Per-tile softmax parameters of tile(j).
     auto set_tile = [&](int j) __attribute__((always_inline)) {
       const int j0 = tile(j) * BN;
-      if constexpr (ALIBI && kLse) ta.abase = ta.sl2 * (float)(j0 + 4 * hh - origin.at(iw));
+      if constexpr (ALIBI && kLse) ta.abase = ta.sl2 * (float)from_origin(j0 + 4 * hh, iw + off, origin, CAUSAL);
       else ta.abase = ALIBI ? ta.sl2 * (float)(j0 + 4 * hh - iw - off) : 0.f;
       int l = Lk - 1 - j0 - 4 * hh;
       if (CAUSAL) l = min(l, row + off - j0 - 4 * hh);
@@ -1216,7 +1216,7 @@ __global__ __launch_bounds__(kThreads, kWgPerCu) __attribute__((amdgpu_num_vgpr(
         // comes back here, in 64 bits.  (-inf for a row that sees no key.)
         const float x = st.mc + __builtin_amdgcn_logf(lt);
         float y = x * kLn2;
-        if constexpr (ALIBI) y = (float)((double)x * 0.6931471805599453 + (double)p.slopes[cur.hq] * (double)(origin.at(iw) - off - iw - n2));
+        if constexpr (ALIBI) y = (float)((double)x * 0.6931471805599453 + (double)p.slopes[cur.hq] * (double)-from_origin(off + iw + n2, off + iw, origin, CAUSAL));
         if (h2 == 0 && iw + n2 < Lq) lse_of(p)[(size_t)cur.head * Lq + iw + n2] = lt == 0.f ? kNegInf : y;
       }
       constexpr int RPI = 64 / CPR;   // rows per store instruction
