@@ -11,8 +11,10 @@
  * return codes, the same bits for the same call.  X, weight and Y have one type (norm_dtype);
  * the residual, H and the gradients dH have that type or fp32 (stream_dtype).  N >= 1, 1 <= M
  * <= RMSNORM_MAX_M, N * M < 2^40; rows need no alignment.  weight NULL: y = h rstd.  residual
- * NULL: h = x, H is not written (and may be NULL), stream_dtype is that of X.  An output may be one of the inputs of the
- * same type and shape, itself (in place); otherwise what is written shares memory with nothing else.
+ * NULL: h = x, H is not written (and may be NULL), stream_dtype is that of X.  In place: Y may be X itself, H the residual, dX
+ * dY or a dH of its type, and dresidual dH; otherwise what is written shares memory with nothing else.  rstd is fp32 and y
+ * and the gradients are formed with it: under 2^-126 it has fewer bits (rows of a root mean square over 2^126), and rows under 2^-128 with
+ * an eps of 0 have an infinite one (the 8-bit form takes its own, in 64 bits).
  */
 #ifndef RMSNORM_H
 #define RMSNORM_H
