@@ -860,7 +860,7 @@ __device__ __forceinline__ void dq_block(const BwdParams& p, char* lds, int item
 }
 
 // Both in one launch, the key blocks first: the row blocks fill what they leave free.  32 heads of 8192 causal rows of 128 in
-// bf16 take 1856 us, 0.74 PFLOP/s of the formula's five products and 1.18 of the eight that are formed, the matrix unit busy 0.66 of the cycles (at
+// bf16 take 1856 us (here and below up to 6 % more on other GPUs), 0.74 PFLOP/s of the formula's five products and 1.18 of the eight that are formed, the matrix unit busy 0.66 of the cycles (at
 // 1.72 GHz under that load); with fp16, a cap and a window of 1025 (32 / 16 heads of 3001 on 4099) 255, the vector unit 0.55
 // and the matrix unit 0.40; 16 heads of 64 dims have the exponentials of twice as many products: 0.44 and 0.28.
 template <int D, typename T, bool CAUSAL, bool ALIBI, bool CAP>

@@ -381,9 +381,10 @@ __device__ __forceinline__ Turns turns_of(int64_t N, int rpb, int sub) {
 
 // T: the type of x, the weight and y; R: that of the residual and h.  C: steps of 8 elements a lane.  QUANT: y in 8 bits.  A
 // workgroup takes rows in turn, the words of two rows on their way while one is worked on (of one in more steps: of none until
-// that one's are stored where QUANT leaves no registers, 4096 rows of 16384 with a scale each 163 us, 206 spilled).  8192 rows
+// that one's are stored where QUANT leaves no registers: 4096 rows of 16384 with a scale each 163 us, 206 with them).  For 1024
+// lanes there are 128 registers: none is spilled in one step, 22 to 25 in two to 8 bits, 12 to 268 in four.  8192 rows
 // of 5120 in bf16 take 62 us, 5.4 TB/s in and out (a large copy 5.1), 8191 of 5119 76, 101 with branches at the rows' ends;
-// to 8 bits, 8192 of 8192 93 us with a scale for each 128, 120 with one row ahead.  That is bound by
+// to 8 bits, 8192 of 8192 95 us with a scale for each 128 (102 to 108 under a profiler, which keeps the calls apart), 120 with one row ahead.  That is bound by
 // fp64 (the codes are those of the exact quotients), and a scale a row by its second join as well: 125 (127 with h taken
 // through fp64 twice, as more steps of a lane do).
 template <typename T, typename R, int C, bool QUANT, bool ODD>
@@ -566,7 +567,7 @@ __global__ __launch_bounds__(kMaxThreads) void rmsnorm_add_kernel(RmsnormParams 
 // one is worked on: 8192 rows of 5120 in bf16 take 66 us, 5.1 TB/s in and out as a large copy has, 87 with one ahead.
 // 8191 of 5119 take 85; 98 with branches at the rows' ends in place of Row.  In more steps of a lane the next row's words come
 // behind one's stores (4096 rows of 12289 97 us, 2048 of 32768 222; 125 and 387 as soon as that one's are taken apart, which
-// spills).
+// spills more: as it is 3 to 5 registers in two steps of odd widths, 69 to 404 in four).
 template <typename T, typename R, int C, bool ODD>
 __global__ __launch_bounds__(kMaxThreads) void rmsnorm_add_bwd_kernel(RmsnormBwdParams p) {
   __shared__ float sums[2][kMaxWaves];
